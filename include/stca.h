@@ -25,7 +25,8 @@
  *  - Weights are stacked per layer: wq, wk, wv, wo [n_layers][d][d],
  *    w1 [n_layers][d][ffn_hidden], w2 [n_layers][ffn_hidden][d].
  *  - Storage dtype (STCA_F32 or STCA_BF16) applies to hist, tgt, the weights,
- *    out and dout; accumulation is always fp32; gradients are fp32.
+ *    out and dout; accumulation is always fp32; gradients are fp32 (of the
+ *    stand-alone attention: in the storage dtype, its bias table's fp32).
  *  - Range of the bf16 path.  bf16 storage keeps two bytes per value inside
  *    the kernels as well, but in fp16 (three more mantissa bits, which the
  *    attention's accuracy needs): the projected K and V, the queries, the
@@ -47,7 +48,8 @@
  *  - Request r owns hist rows [hist_off[r], hist_off[r+1]) and tgt rows
  *    [tgt_off[r], tgt_off[r+1]).  offsets[0] = 0, non-decreasing,
  *    offsets[R] = n_hist / n_tgt.  A request with targets must have at least
- *    one history row; a request with no targets is legal and produces nothing.
+ *    one history row (the stand-alone attention takes it without); a request
+ *    with no targets is legal and produces nothing.
  *  - The caller owns every buffer.  The library never allocates, frees or
  *    synchronises: all work is enqueued on `stream`, and calls return before it
  *    runs.  Calls on different streams need distinct workspaces.
@@ -407,6 +409,161 @@ stca_status_t stca_forward_paper_profiled(const stca_dims_t* dims, const stca_ba
                                           const void* hist, const void* tgt, const stca_paper_weights_t* w,
                                           void* z, void* saved, void* ws, size_t ws_bytes, hipStream_t stream,
                                           hipEvent_t* events, int n_events, const char** labels);
+
+/* ---- Stand-alone attention (the operator without the layer around it):
+ * ragged target-to-history cross attention with capped scores, a learned bias
+ * by buckets of distance and a mask to the part of the history that a target
+ * may see, and its gradients.  For target t, query head h of kv head
+ * g = h / (n_heads / n_kv_heads) and history row j of t's request:
+ *   z = scale q_{t,h} . k_{j,g}
+ *   y = softcap tanh(z / softcap)                  (softcap > 0; y = z for 0)
+ *   x = y + bias[h][b(D)],  D = tgt_pos[t] - hist_pos[j]
+ *   out_{t,h} = sum_j softmax_j(x) v_{j,g}          over the visible rows j
+ * b(D) is the number of edges that are at most max(D, 0); a row is hidden when
+ * `masked` and D < 0, or when its bucket's bias is minus infinity.  Hidden rows
+ * contribute nothing, whatever their K and V hold; a target that sees no row
+ * (its request may have none) has the output 0, and no part in any gradient.
+ * D saturates at the ends of int32.  Sums, maxima and weights are fp32; with
+ * bf16 storage the weights enter the matrix cores as two bf16 terms.
+ *
+ * Calls of one batch on different streams need distinct workspaces.  Targets
+ * of a request without history are legal here. */
+typedef struct {
+  int32_t n_heads;           /* query heads, a multiple of n_kv_heads (at most 64 times as many) */
+  int32_t n_kv_heads;        /* heads of K and V, each shared by n_heads / n_kv_heads query heads */
+  int32_t d_head;            /* 32, 64 or 128; n_heads d_head at most 65536 */
+  int32_t dtype;             /* stca_dtype_t of q, k, v, out, dout, dq, dk, dv */
+  float scale;               /* finite */
+  float softcap;             /* >= 0, 0 = none */
+  int32_t masked;            /* nonzero: rows with hist_pos > tgt_pos are hidden */
+  int32_t n_buckets;         /* 0 = no bias; at most 128 */
+  const int32_t* edges_host; /* host [n_buckets - 1], strictly ascending, the first >= 1; read by the call */
+} stca_attn_t;
+
+/* Positions and tables of bias, and a cache's pos, need 4-byte alignment only.
+ * Rows of q, k, v hold their heads one after the other; ld* are row strides in
+ * elements (0 = dense; a multiple of 16 bytes).  tgt_pos is needed with a mask
+ * or a bias; hist_pos NULL: a row's position is its index in its request. */
+typedef struct {
+  const void* q;            /* [n_tgt][n_heads][d_head] */
+  const void* k;            /* [n_hist][n_kv_heads][d_head] */
+  const void* v;            /* [n_hist][n_kv_heads][d_head] */
+  int64_t ldq, ldk, ldv;
+  const int32_t* tgt_pos;   /* device [n_tgt] */
+  const int32_t* hist_pos;  /* device [n_hist], any order */
+  const float* bias;        /* device [n_heads][n_buckets], fp32 */
+} stca_attn_in_t;
+
+typedef struct {
+  void* dq;      /* shapes and strides as q, k, v, storage dtype; overwritten */
+  void* dk;
+  void* dv;
+  int64_t lddq, lddk, lddv;
+  float* dbias;  /* [n_heads][n_buckets], fp32, overwritten; NULL without a bias */
+} stca_attn_grads_t;
+
+/* Byte offsets into the buffer that a forward saves for its backward, fp32:
+ * a [n_tgt][n_heads][d_head] (the output before rounding), and per target and
+ * head the largest score and the sum of exp(x - largest) [n_tgt][n_heads]. */
+typedef struct {
+  size_t a, max, sum;
+  size_t total;
+} stca_attn_saved_layout_t;
+
+/* Sizes; 0 for invalid or unsupported arguments. */
+size_t stca_attn_workspace_size(const stca_attn_t* attn, const stca_batch_t* batch, int with_backward);
+size_t stca_attn_saved_size(const stca_attn_t* attn, const stca_batch_t* batch);
+stca_status_t stca_attn_saved_layout(const stca_attn_t* attn, const stca_batch_t* batch,
+                                     stca_attn_saved_layout_t* layout);
+
+/* out [n_tgt][n_heads][d_head] (dense, storage dtype); saved nullable. */
+stca_status_t stca_attn_forward(const stca_attn_t* attn, const stca_batch_t* batch, const stca_attn_in_t* in,
+                                void* out, void* saved, void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* Gradients of f = sum <dout, out>, from the inputs of a forward and what it
+ * saved.  dout as out.  Gradients of shared heads are summed over the sharing
+ * heads; nothing is added in order of arrival, so results repeat bitwise.
+ * ws_bytes >= stca_attn_workspace_size(attn, batch, 1). */
+stca_status_t stca_attn_backward(const stca_attn_t* attn, const stca_batch_t* batch, const stca_attn_in_t* in,
+                                 const void* saved, const void* dout, const stca_attn_grads_t* grads, void* ws,
+                                 size_t ws_bytes, hipStream_t stream);
+
+/* Bucket edges as distances grow: 1, 2, ..., n_exact, then a geometric series
+ * to max_distance (each at least one more than the last), n_buckets - 1 in all.
+ * Host function.  1 <= n_exact < n_buckets <= 128, max_distance >= n_buckets. */
+stca_status_t stca_bias_edges(int32_t n_buckets, int32_t n_exact, int32_t max_distance, int32_t* edges);
+
+/* ---- Paged history cache.  K and V of a history row do not depend on the
+ * targets, so they can be kept from one request of a user to the next.  Rows
+ * live in pages of page_size slots; a request's table lists its pages, and its
+ * row i is slot i % page_size of page table[i / page_size].
+ *   k [n_pages][n_kv_heads][page_size][d_head]
+ *   v [n_pages][n_kv_heads][d_head][page_size]
+ * in bf16 (STCA_CACHE_BF16), or as int8 with a power-of-two step per row and kv
+ * head (STCA_CACHE_INT8): step = 2^max(floor(log2 max|x|) - 6, -126),
+ * n = x / step rounded to nearest even, at most 127 in magnitude, and
+ * k_exp, v_exp [n_pages][n_kv_heads][page_size] hold log2(step) + 127.  A row
+ * with a value that is not finite is stored as 255 and reads as NaN.
+ * pos (optional) [n_pages][page_size]: the rows' positions. */
+typedef enum { STCA_CACHE_BF16 = 0, STCA_CACHE_INT8 = 1 } stca_cache_format_t;
+typedef struct {
+  int32_t n_pages;
+  int32_t page_size;   /* 16, 32, 64, 128 or 256 */
+  int32_t n_kv_heads;
+  int32_t d_head;      /* 32, 64 or 128 */
+  int32_t format;      /* stca_cache_format_t */
+  void* k;
+  void* v;
+  uint8_t* k_exp;      /* STCA_CACHE_INT8 only */
+  uint8_t* v_exp;
+  int32_t* pos;        /* nullable */
+} stca_cache_t;
+
+/* Packed rows of several requests and where they lie in the cache: request r's
+ * rows [row_off[r], row_off[r+1]) are its cache rows start[r], start[r] + 1, ... */
+typedef struct {
+  int32_t n_requests;
+  int64_t n_rows;          /* row_off[n_requests] */
+  const int32_t* row_off;  /* device [n_requests + 1] */
+  const int32_t* start;    /* device [n_requests] */
+  const int32_t* table;    /* device [n_requests][table_ld] */
+  int32_t table_ld;
+} stca_cache_rows_t;
+
+/* Writes rows k, v [n_rows][n_kv_heads][d_head] (dtype; row strides ldk, ldv,
+ * 0 = dense) into their slots, and pos [n_rows] where both it and the cache's
+ * are given.  Other slots keep what they hold.  A slot may be written once per
+ * call.  The read is the reverse, rounded to dtype.  Rows without a page (an
+ * entry of the table outside the pages) are left out.  ws (nullable): 256 device
+ * bytes whose status stca_device_status reads: STCA_ERR_INVALID_ARG for bad
+ * offsets, starts or pages. */
+#define STCA_CACHE_WS_BYTES ((size_t)256)
+stca_status_t stca_cache_write(const stca_cache_t* cache, const stca_cache_rows_t* rows, int32_t dtype,
+                               const void* k, const void* v, int64_t ldk, int64_t ldv, const int32_t* pos,
+                               void* ws, hipStream_t stream);
+stca_status_t stca_cache_read(const stca_cache_t* cache, const stca_cache_rows_t* rows, int32_t dtype, void* k,
+                              void* v, int64_t ldk, int64_t ldv, int32_t* pos, void* ws, hipStream_t stream);
+
+/* Attention of the requests' new targets over their first lens[r] cached rows,
+ * otherwise as stca_attn_forward (positions from the cache's pos, or row
+ * indices; attn->dtype must be STCA_BF16).  lens may change between calls up to
+ * max_len, on which sizes and launches depend.  Rows without a page are hidden.
+ * Offsets, lengths and pages are checked on the device (stca_device_status). */
+typedef struct {
+  int32_t n_requests;
+  int64_t n_tgt;
+  const int32_t* tgt_off;       /* device [n_requests + 1] */
+  const int32_t* tgt_off_host;  /* optional host copy: host checks and exact sizing */
+  const int32_t* lens;          /* device [n_requests], 0..max_len */
+  int32_t max_len;
+  const int32_t* table;         /* device [n_requests][table_ld], table_ld page_size >= max_len */
+  int32_t table_ld;
+} stca_cache_batch_t;
+size_t stca_cache_attn_workspace_size(const stca_attn_t* attn, const stca_cache_t* cache,
+                                      const stca_cache_batch_t* batch);
+stca_status_t stca_cache_attn(const stca_attn_t* attn, const stca_cache_t* cache, const stca_cache_batch_t* batch,
+                              const void* q, int64_t ldq, const int32_t* tgt_pos, const float* bias, void* out,
+                              void* ws, size_t ws_bytes, hipStream_t stream);
 
 /* Reads (synchronising on `stream`) the status the kernels recorded in `ws`
  * during the last call that used it: STCA_ERR_INVALID_ARG when the device

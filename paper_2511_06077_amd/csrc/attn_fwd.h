@@ -1,0 +1,618 @@
+// Forward of the stand-alone target-to-history attention, over packed rows or
+// over a paged cache:
+//   x = cap(scale q.k) + bias[h][bucket(p_t - p_j)];  out = softmax(x) v.
+//
+// One workgroup of four waves takes one chunk of one request's history for one
+// kv head and up to 16 MT rows (target, query head of the kv head's group);
+// its waves take the chunk's blocks of 16 NT history rows in turn, each with
+// softmax statistics and an output of its own, joined in LDS at the end.
+// Several chunks leave (output, maximum, sum) partials for attn_merge.
+//
+// Everything of a block stays in one wave's registers.  Scores are formed
+// transposed, S^T = K Q^T (v_mfma 16x16x32 bf16, or 16x16x4 fp32), so that the
+// result registers of a lane (column t = lane % 16, rows 4 (lane / 16) + i)
+// are the operand of O^T = V^T P^T as they stand: the history row of S^T's
+// tile i, row r, is j = 4 NT (r / 4) + 4 i + r % 4, which gives lane group g
+// the 4 NT consecutive rows 4 NT g ..., the ones that its V operand holds.
+// V of packed rows is read a row at a time, DH / 16 elements a lane, and pairs
+// of rows are merged by byte permutes; V pages hold rows along the fast axis.
+// A row's maximum is only raised (and O rescaled) when a score passes it by
+// kSlack: a vote per block instead of a reduction across lanes.
+//
+// P is split into two bf16 terms: one term's rounding would show in the
+// output as a second rounding of its size (1.7e-3 -> 2.4e-3 relative to 64
+// bits on normal inputs); the matrix cores have the time.
+//
+// Distances of most blocks lie in one bucket for every lane: each lane keeps
+// its bucket's interval and bias, a vote tells whether a block is inside, and
+// only the others look buckets and masks up score by score.
+#pragma once
+
+#include "attn_ops.h"
+
+namespace stca {
+namespace ops {
+
+constexpr int kRagged = 0, kPagedBf16 = 1, kPagedInt8 = 2;
+constexpr float kSlack = 6.f;  // e^6: sums and products stay far inside fp32 and bf16 ranges
+
+template <int KV> constexpr int kTilesOf = KV == kPagedInt8 ? 4 : 2;
+
+// LDS of a workgroup before the dynamic part's tables.
+template <int DH> constexpr int kCombineFloats = kWaves * 16 * (DH + 2);
+
+template <typename T, int KV, int DH, int NT>
+struct Block {
+  static constexpr bool kF32 = !Elem<T>::bf16;
+  static constexpr int KS = DH / 32;   // k steps of 32 features
+  static constexpr int NE = DH / 16;   // output tiles; lane c holds features NE c + e
+  static constexpr int NJ = 4 * NT;    // history rows of a lane
+  // K operand of tile i, step s
+  f32x4 kf[kF32 ? NT : 1][kF32 ? 2 * KS : 1];
+  bf16x8 kb[KV == kRagged && kF32 ? 1 : (KV == kPagedInt8 ? 1 : NT)][KS];
+  uint2 k8[KV == kPagedInt8 ? NT : 1][KV == kPagedInt8 ? KS : 1];
+  // V as loaded
+  uint32_t vw[KV == kRagged ? NJ : 1][KV == kRagged ? (kF32 ? NE : NE / 2) : 1];
+  uint4 vp[KV == kRagged ? 1 : NE];
+  uint4 ke, ve;                        // 16 exponents each
+};
+
+template <int N>
+__device__ __forceinline__ void load_words(const char* p, uint32_t* w) {
+  typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+  typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+  if constexpr (N >= 4) {
+#pragma unroll
+    for (int i = 0; i < N / 4; ++i) {
+      const u32x4 x = reinterpret_cast<const u32x4*>(p)[i];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) w[4 * i + k] = x[k];
+    }
+  } else if constexpr (N == 2) {
+    const u32x2 x = *reinterpret_cast<const u32x2*>(p);
+    w[0] = x[0];
+    w[1] = x[1];
+  } else {
+    w[0] = *reinterpret_cast<const uint32_t*>(p);
+  }
+}
+
+// First feature of lane group g's eight of step s.
+template <int KV, int DH>
+__device__ __forceinline__ int feature(int s, int g) {
+  if constexpr (KV == kPagedInt8 && DH >= 64) return 64 * (s / 2) + 16 * g + 8 * (s % 2);
+  else return 32 * s + 8 * g;
+}
+
+__device__ __forceinline__ float int8_f32(uint32_t w, int k) {
+  return static_cast<float>(static_cast<int8_t>(w >> (8 * k)));
+}
+// Eight int8 of two words as bf16 (exact: 8 significant bits hold 0..127).
+__device__ __forceinline__ bf16x8 int8_bf16(uint32_t a, uint32_t b) {
+  uint32_t r[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t w = i < 2 ? a : b;
+    const float x = int8_f32(w, 2 * (i % 2)), y = int8_f32(w, 2 * (i % 2) + 1);
+    r[i] = __builtin_amdgcn_perm(__float_as_uint(y), __float_as_uint(x), 0x07060302u);
+  }
+  return __builtin_bit_cast(bf16x8, make_uint4(r[0], r[1], r[2], r[3]));
+}
+__device__ __forceinline__ float exp_byte(uint32_t w, int k) {  // 2^(byte - 127); 255: infinity
+  return __uint_as_float(((w >> (8 * k)) & 0xffu) << 23);
+}
+__device__ __forceinline__ uint32_t word(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
+
+__device__ __forceinline__ bool odd_bf16(uint32_t w) {  // a half of w is not finite
+  return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u;
+}
+
+template <typename T, int KV, int DH, int MT>
+__global__ __launch_bounds__(kThreads) void attn_fwd_kernel(const AttnArgs a) {
+  constexpr bool kF32 = !Elem<T>::bf16;
+  constexpr bool kPaged = KV != kRagged;
+  constexpr int NT = kTilesOf<KV>;
+  constexpr int BJ = 16 * NT;
+  constexpr int KS = DH / 32, NE = DH / 16, NJ = 4 * NT;
+  using Blk = Block<T, KV, DH, NT>;
+  extern __shared__ __align__(16) unsigned char smem[];
+  float* comb = reinterpret_cast<float*>(smem);
+  int32_t* s_edges = reinterpret_cast<int32_t*>(comb + kCombineFloats<DH>);
+  uint8_t* s_cell = reinterpret_cast<uint8_t*>(s_edges + kMaxBuckets);
+  float* s_bias = reinterpret_cast<float*>(s_cell + 128);
+  int32_t* s_table = reinterpret_cast<int32_t*>(s_bias + a.G * a.b.n);
+
+  const int tid = threadIdx.x, lane = tid & 63, c16 = lane & 15, g4 = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+
+  if (blockIdx.x == gridDim.x - 1) {
+    check_call(a, kPaged);
+    return;
+  }
+  // every kv head and row group of a chunk on one XCD: heads share cache lines
+  // of packed rows, row groups share everything
+  const int per = a.Hk * a.zgroups;
+  const int unit = static_cast<int>(blockIdx.x) / kXcds / per * kXcds + static_cast<int>(blockIdx.x) % kXcds;
+  if (unit >= a.units) return;
+  const int rem = static_cast<int>(blockIdx.x) / kXcds % per;
+  const int g = rem % a.Hk, z = rem / a.Hk;
+
+  int r, c, len;
+  int64_t h0 = 0;
+  if constexpr (kPaged) {
+    r = unit / a.max_chunks;
+    c = unit % a.max_chunks;
+    len = min(max(a.lens[r], 0), a.max_len);
+  } else {
+    r = find_request(a.hist_off, a.R, a.n_hist, a.chunk, unit);
+    h0 = clamp_off(a.hist_off[r], a.n_hist);
+    len = max(0, static_cast<int>(clamp_off(a.hist_off[r + 1], a.n_hist) - h0));
+    c = unit - static_cast<int>(h0 / a.chunk + r);
+  }
+  if (c < 0 || c >= a.max_chunks || (c > 0 && static_cast<int64_t>(c) * a.chunk >= len)) return;
+  const int j0 = c * a.chunk;
+  const int t0 = clamp_off(a.tgt_off[r], a.n_tgt), m = clamp_off(a.tgt_off[r + 1], a.n_tgt) - t0;
+  const int rows = m * a.G;
+  if (z * 16 * MT >= rows) return;
+  const bool split = len > a.chunk;
+  int j1 = min(len, j0 + a.chunk);
+
+  // tables
+  for (int i = tid; i < a.b.n; i += kThreads) s_edges[i] = a.b.edges[i];
+  if (a.b.n) {
+    if (tid < 128) s_cell[tid] = a.b.cell[tid];
+    for (int i = tid; i < a.G * a.b.n; i += kThreads) s_bias[i] = a.bias[static_cast<int64_t>(g) * a.G * a.b.n + i];
+  }
+  bool holes = false;
+  if constexpr (kPaged) {
+    const int p0 = j0 >> a.page_shift, p1 = (j1 + (1 << a.page_shift) - 1) >> a.page_shift;
+    for (int i = p0 + tid; i < p1; i += kThreads) {
+      const int p = a.table[static_cast<int64_t>(r) * a.table_ld + i];
+      const bool bad = p < 0 || p >= a.n_pages;
+      s_table[i - p0] = bad ? -1 : p;
+      holes |= bad;
+    }
+    holes = __syncthreads_or(holes);
+  } else {
+    __syncthreads();
+  }
+  const BucketLds bl{s_edges, s_cell, s_bias, a.b.n};
+
+  for (int zz = z; zz * 16 * MT < rows; zz += a.zgroups) {
+    // ---- this lane's rows: column c16 of each tile
+    int tpos[MT], head[MT];
+    int64_t trow[MT];
+    bool have[MT];
+    bf16x8 qb[kF32 ? 1 : MT][KS];
+    f32x4 qf[kF32 ? MT : 1][kF32 ? 2 * KS : 1];
+    int seen_max = -2147483647 - 1;
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+      const int row = (zz * MT + mt) * 16 + c16;
+      have[mt] = row < rows;
+      const int t = have[mt] ? row / a.G : 0;
+      head[mt] = have[mt] ? row % a.G : 0;
+      trow[mt] = t0 + t;
+      tpos[mt] = a.placed ? a.tgt_pos[trow[mt]] : 0;
+      if (have[mt]) seen_max = max(seen_max, tpos[mt]);
+      const T* qp = static_cast<const T*>(a.q) + trow[mt] * a.ldq + (static_cast<int64_t>(g) * a.G + head[mt]) * DH;
+#pragma unroll
+      for (int s = 0; s < KS; ++s) {
+        const T* p = qp + feature<KV, DH>(s, g4);
+        if constexpr (kF32) {
+          qf[mt][2 * s] = have[mt] ? reinterpret_cast<const f32x4*>(p)[0] : f32x4{};
+          qf[mt][2 * s + 1] = have[mt] ? reinterpret_cast<const f32x4*>(p)[1] : f32x4{};
+        } else {
+          qb[mt][s] = have[mt] ? *reinterpret_cast<const bf16x8*>(p) : bf16x8{};
+        }
+      }
+    }
+    // rows past every target's own index are hidden from all of them
+    int jend = j1;
+    if (a.masked && !a.hist_pos) {
+#pragma unroll
+      for (int o = 1; o < 16; o <<= 1) seen_max = max(seen_max, __shfl_xor(seen_max, o));
+      jend = static_cast<int>(min<int64_t>(jend, static_cast<int64_t>(seen_max) + 1));
+      jend = __builtin_amdgcn_readfirstlane(jend);
+    }
+
+    float mx[MT], sum[MT], bias[MT];
+    int blo[MT], bhi[MT];  // distances of the bucket held
+    f32x4 o[MT][NE];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+      mx[mt] = -INFINITY;
+      sum[mt] = 0.f;
+      bias[mt] = 0.f;
+      blo[mt] = a.masked ? 0 : -2147483647 - 1;
+      bhi[mt] = 2147483647;
+      if (a.b.n) bhi[mt] = -2147483647 - 1;  // none yet
+#pragma unroll
+      for (int e = 0; e < NE; ++e) o[mt][e] = f32x4{};
+    }
+
+    auto load = [&](Blk& b, int jb) {
+      const int last = len - 1 - jb;  // clamped: rows past the end are hidden below
+      if constexpr (!kPaged) {
+        const char* kp = static_cast<const char*>(a.k) + ((h0 + jb) * a.ldk + static_cast<int64_t>(g) * DH) * sizeof(T);
+        const char* vp = static_cast<const char*>(a.v) + ((h0 + jb) * a.ldv + static_cast<int64_t>(g) * DH) * sizeof(T);
+        const int lk = static_cast<int>(a.ldk * sizeof(T)), lv = static_cast<int>(a.ldv * sizeof(T));
+#pragma unroll
+        for (int i = 0; i < NT; ++i) {
+          const int jr = min(NJ * (c16 >> 2) + 4 * i + (c16 & 3), last);
+#pragma unroll
+          for (int s = 0; s < KS; ++s) {
+            const char* p = kp + jr * lk + feature<KV, DH>(s, g4) * sizeof(T);
+            if constexpr (kF32) {
+              b.kf[i][2 * s] = reinterpret_cast<const f32x4*>(p)[0];
+              b.kf[i][2 * s + 1] = reinterpret_cast<const f32x4*>(p)[1];
+            } else {
+              b.kb[i][s] = *reinterpret_cast<const bf16x8*>(p);
+            }
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < NJ; ++i) {
+          const int jr = min(NJ * g4 + i, last);
+          load_words<(kF32 ? NE : NE / 2)>(vp + jr * lv + c16 * NE * static_cast<int>(sizeof(T)), b.vw[i]);
+        }
+      } else {
+        const int P = 1 << a.page_shift, ps = a.page_shift, p0 = j0 >> ps;
+        constexpr int ES = KV == kPagedInt8 ? 1 : 2;
+#pragma unroll
+        for (int i = 0; i < NT; ++i) {
+          const int j = jb + min(NJ * (c16 >> 2) + 4 * i + (c16 & 3), last);
+          const int64_t page = max(s_table[(j >> ps) - p0], 0);
+          const char* p = static_cast<const char*>(a.k) + ((page * a.Hk + g) * P + (j & (P - 1))) * (DH * ES);
+#pragma unroll
+          for (int s = 0; s < KS; ++s) {
+            if constexpr (KV == kPagedInt8) {
+              b.k8[i][s] = *reinterpret_cast<const uint2*>(p + feature<KV, DH>(s, g4));
+            } else {
+              b.kb[i][s] = *reinterpret_cast<const bf16x8*>(p + 2 * feature<KV, DH>(s, g4));
+            }
+          }
+        }
+        // this lane group's NJ rows lie in one page
+        const int j = min(jb + NJ * g4, (len - 1) & ~(NJ - 1));
+        const int64_t page = max(s_table[(j >> ps) - p0], 0), slot = j & (P - 1);
+#pragma unroll
+        for (int e = 0; e < NE; ++e)
+          b.vp[e] = *reinterpret_cast<const uint4*>(static_cast<const char*>(a.v) +
+                                                    (((page * a.Hk + g) * DH + NE * c16 + e) * P + slot) * ES);
+        if constexpr (KV == kPagedInt8) {
+          b.ke = *reinterpret_cast<const uint4*>(a.ke + (page * a.Hk + g) * P + slot);
+          b.ve = *reinterpret_cast<const uint4*>(a.ve + (page * a.Hk + g) * P + slot);
+        }
+      }
+    };
+
+    auto compute = [&](const Blk& b, int jb) {
+      // V operand of O^T: rows NJ g4 + 8 s + 0..7, feature NE c16 + e
+      bf16x8 vb[kF32 ? 1 : NT / 2][kF32 ? 1 : NE];
+      if constexpr (KV == kRagged && !kF32) {
+#pragma unroll
+        for (int e2 = 0; e2 < NE / 2; ++e2) {
+          uint32_t lo[4], hi[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            lo[i] = __builtin_amdgcn_perm(b.vw[2 * i + 1][e2], b.vw[2 * i][e2], 0x05040100u);
+            hi[i] = __builtin_amdgcn_perm(b.vw[2 * i + 1][e2], b.vw[2 * i][e2], 0x07060302u);
+          }
+          vb[0][2 * e2] = __builtin_bit_cast(bf16x8, make_uint4(lo[0], lo[1], lo[2], lo[3]));
+          vb[0][2 * e2 + 1] = __builtin_bit_cast(bf16x8, make_uint4(hi[0], hi[1], hi[2], hi[3]));
+        }
+      } else if constexpr (KV == kPagedBf16) {
+#pragma unroll
+        for (int e = 0; e < NE; ++e) vb[0][e] = __builtin_bit_cast(bf16x8, b.vp[e]);
+      } else if constexpr (KV == kPagedInt8) {
+#pragma unroll
+        for (int e = 0; e < NE; ++e) {
+          vb[0][e] = int8_bf16(b.vp[e].x, b.vp[e].y);
+          vb[1][e] = int8_bf16(b.vp[e].z, b.vp[e].w);
+        }
+      }
+      bf16x8 kc[KV == kPagedInt8 ? NT : 1][KV == kPagedInt8 ? KS : 1];
+      if constexpr (KV == kPagedInt8) {
+#pragma unroll
+        for (int i = 0; i < NT; ++i)
+#pragma unroll
+          for (int s = 0; s < KS; ++s) kc[i][s] = int8_bf16(b.k8[i][s].x, b.k8[i][s].y);
+      }
+      // positions of this lane's rows
+      const bool tail = jb + BJ > jend || holes;
+      int pj[NJ];
+      int pmin = 0, pmax = 0;
+      if (a.placed) {
+        if (a.hist_pos) {
+          const int32_t* hp;
+          if constexpr (kPaged) {
+            const int j = min(jb + NJ * g4, (len - 1) & ~(NJ - 1));
+            hp = a.hist_pos + (static_cast<int64_t>(max(s_table[(j >> a.page_shift) - (j0 >> a.page_shift)], 0))
+                               << a.page_shift) + (j & ((1 << a.page_shift) - 1));
+#pragma unroll
+            for (int i = 0; i < NJ; ++i) pj[i] = hp[i];
+          } else {
+            hp = a.hist_pos + h0 + jb;
+            const int last = len - 1 - jb;
+#pragma unroll
+            for (int i = 0; i < NJ; ++i) pj[i] = hp[min(NJ * g4 + i, last)];
+          }
+          pmin = pmax = pj[0];
+#pragma unroll
+          for (int i = 1; i < NJ; ++i) {
+            pmin = min(pmin, pj[i]);
+            pmax = max(pmax, pj[i]);
+          }
+        } else {
+          pmin = jb + NJ * g4;
+          pmax = pmin + NJ - 1;
+        }
+      }
+      float ks[KV == kPagedInt8 ? NJ : 1], vs[KV == kPagedInt8 ? NJ : 1];
+      if constexpr (KV == kPagedInt8) {
+#pragma unroll
+        for (int i = 0; i < NJ; ++i) {
+          ks[i] = exp_byte(word(b.ke, i / 4), i % 4);
+          vs[i] = exp_byte(word(b.ve, i / 4), i % 4);
+        }
+      }
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) {
+        float x[NJ];
+#pragma unroll
+        for (int i = 0; i < NT; ++i) {
+          f32x4 s = {};
+          if constexpr (kF32) {
+#pragma unroll
+            for (int k = 0; k < 2 * KS; ++k)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) s = mfma_f32(b.kf[i][k][e], qf[mt][k][e], s);
+          } else {
+#pragma unroll
+            for (int k = 0; k < KS; ++k) {
+              if constexpr (KV == kPagedInt8) s = mfma_bf16(kc[i][k], qb[mt][k], s);
+              else s = mfma_bf16(b.kb[i][k], qb[mt][k], s);
+            }
+          }
+#pragma unroll
+          for (int k = 0; k < 4; ++k) x[4 * i + k] = s[k];
+        }
+#pragma unroll
+        for (int i = 0; i < NJ; ++i) {
+          if constexpr (KV == kPagedInt8) x[i] *= ks[i];
+          x[i] *= a.scale;
+        }
+        if (a.cap > 0.f) {
+          const float inv = 1.f / a.cap;
+#pragma unroll
+          for (int i = 0; i < NJ; ++i) x[i] = a.cap * (kF32 ? tanhf(x[i] / a.cap) : tanh_fast(x[i] * inv));
+        }
+        uint32_t hid = 0;
+        const bool slow = __ballot(tail || sub_sat(tpos[mt], pmax) < blo[mt] || sub_sat(tpos[mt], pmin) > bhi[mt]) != 0;
+        if (!slow) {
+#pragma unroll
+          for (int i = 0; i < NJ; ++i) x[i] += bias[mt];
+        } else {
+          int k = 0;
+#pragma unroll
+          for (int i = 0; i < NJ; ++i) {
+            const int j = jb + NJ * g4 + i;
+            const int d = a.placed ? sub_sat(tpos[mt], a.hist_pos ? pj[i] : j) : 0;
+            bool vis = j < jend && !(a.masked && d < 0);
+            if constexpr (kPaged)
+              if (holes) vis = vis && s_table[(min(j, len - 1) >> a.page_shift) - (j0 >> a.page_shift)] >= 0;
+            if (a.b.n) {
+              k = bucket_of(bl, d);
+              const float bv = s_bias[head[mt] * a.b.n + k];
+              x[i] += bv;
+              vis = vis && bv != -INFINITY;
+            }
+            if (!vis) {
+              x[i] = -INFINITY;
+              hid |= 1u << i;
+            }
+          }
+          if (a.b.n) {  // hold the bucket of the lane's last row
+            bias[mt] = s_bias[head[mt] * a.b.n + k];
+            const int edge = k ? s_edges[k - 1] : (a.masked ? 0 : -2147483647 - 1);
+            blo[mt] = bias[mt] == -INFINITY ? 2147483647 : edge;
+            bhi[mt] = k == a.b.n - 1 ? 2147483647 : s_edges[k] - 1;
+          }
+          if (__ballot(hid != (1u << NJ) - 1u) == 0) continue;  // nothing of this block is seen
+        }
+        // running maximum
+        float top = x[0];
+#pragma unroll
+        for (int i = 1; i < NJ; ++i) top = fmaxf(top, x[i]);
+        if (__ballot(top > mx[mt] + kSlack)) {
+          top = fmaxf(top, __shfl_xor(top, 16));
+          top = fmaxf(top, __shfl_xor(top, 32));
+          const float mn = fmaxf(mx[mt], top);
+          const float f = mx[mt] == -INFINITY ? 0.f : exp_nat(mx[mt] - mn);
+          mx[mt] = mn;
+          sum[mt] *= f;
+#pragma unroll
+          for (int e = 0; e < NE; ++e) o[mt][e] *= f;
+        }
+        const float base = mx[mt] == -INFINITY ? 0.f : mx[mt];
+#pragma unroll
+        for (int i = 0; i < NJ; ++i) {
+          x[i] = exp_nat(x[i] - base);
+          sum[mt] += x[i];
+        }
+        if constexpr (KV == kPagedInt8) {
+#pragma unroll
+          for (int i = 0; i < NJ; ++i) x[i] *= vs[i];
+          if (hid) {
+#pragma unroll
+            for (int i = 0; i < NJ; ++i) x[i] = (hid >> i) & 1 ? 0.f : x[i];  // (a hidden row's scale may be infinite)
+          }
+        }
+        if constexpr (kF32) {
+          bool odd = false;
+          if (slow) {
+#pragma unroll
+            for (int i = 0; i < NJ; ++i)
+#pragma unroll
+              for (int e = 0; e < NE; ++e) odd |= (b.vw[i][e] & 0x7f800000u) == 0x7f800000u;
+          }
+          if (!slow || !__ballot(odd)) {
+#pragma unroll
+            for (int i = 0; i < NJ; ++i)
+#pragma unroll
+              for (int e = 0; e < NE; ++e) o[mt][e] = mfma_f32(__uint_as_float(b.vw[i][e]), x[i], o[mt][e]);
+          } else {
+            for (int col = 0; col < 16; ++col) {
+              const uint32_t h = __shfl(hid, col + 16 * g4);
+#pragma unroll
+              for (int e = 0; e < NE; ++e) {
+                f32x4 n = o[mt][e];
+#pragma unroll
+                for (int i = 0; i < NJ; ++i)
+                  n = mfma_f32((h >> i) & 1 ? 0.f : __uint_as_float(b.vw[i][e]), x[i], n);
+                if (c16 == col) o[mt][e] = n;
+              }
+            }
+          }
+        } else {
+          bf16x8 ph[NT / 2], pl[NT / 2];
+#pragma unroll
+          for (int s = 0; s < NT / 2; ++s) {
+            uint32_t hi[4], lo[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) split_bf16(x[8 * s + 2 * k], x[8 * s + 2 * k + 1], hi[k], lo[k]);
+            ph[s] = __builtin_bit_cast(bf16x8, make_uint4(hi[0], hi[1], hi[2], hi[3]));
+            pl[s] = __builtin_bit_cast(bf16x8, make_uint4(lo[0], lo[1], lo[2], lo[3]));
+          }
+          // a hidden row's value may be infinite or NaN, and 0 times it is
+          // not 0: such blocks take the columns one by one, each with the
+          // values it may not see cleared
+          bool odd = false;
+          if (KV != kPagedInt8 && slow) {
+#pragma unroll
+            for (int e = 0; e < NE; ++e) {
+              const uint4 w = __builtin_bit_cast(uint4, vb[0][e]);
+              odd |= odd_bf16(w.x) || odd_bf16(w.y) || odd_bf16(w.z) || odd_bf16(w.w);
+            }
+          }
+          if (KV == kPagedInt8 || !slow || !__ballot(odd)) {
+#pragma unroll
+            for (int s = 0; s < NT / 2; ++s)
+#pragma unroll
+              for (int e = 0; e < NE; ++e) {
+                o[mt][e] = mfma_bf16(vb[s][e], ph[s], o[mt][e]);
+                o[mt][e] = mfma_bf16(vb[s][e], pl[s], o[mt][e]);
+              }
+          } else {
+            for (int col = 0; col < 16; ++col) {
+              const uint32_t h = __shfl(hid, col + 16 * g4);
+#pragma unroll
+              for (int e = 0; e < NE; ++e) {
+                uint4 w = __builtin_bit_cast(uint4, vb[0][e]);
+                auto keep = [&](uint32_t v, int i) {
+                  return v & (((h >> i) & 1 ? 0u : 0xffffu) | ((h >> (i + 1)) & 1 ? 0u : 0xffff0000u));
+                };
+                w = make_uint4(keep(w.x, 0), keep(w.y, 2), keep(w.z, 4), keep(w.w, 6));
+                const bf16x8 vz = __builtin_bit_cast(bf16x8, w);
+                const f32x4 n = mfma_bf16(vz, pl[0], mfma_bf16(vz, ph[0], o[mt][e]));
+                if (c16 == col) o[mt][e] = n;
+              }
+            }
+          }
+        }
+      }
+    };
+
+    int jb = j0 + wave * BJ;
+    if (jb < jend) {
+      Blk cur;
+      load(cur, jb);
+      for (; jb < jend; jb += kWaves * BJ) {
+        Blk nxt;
+        const bool more = jb + kWaves * BJ < jend;
+        if (more) load(nxt, jb + kWaves * BJ);
+        compute(cur, jb);
+        if (more) cur = nxt;
+      }
+    }
+
+    // ---- join the waves: lane group g4 of wave w holds features NE (4 g4 + i) + e of column c16
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+      if ((zz * MT + mt) * 16 >= rows) break;
+      float l = sum[mt];
+      l += __shfl_xor(l, 16);
+      l += __shfl_xor(l, 32);
+      float* cw = comb + wave * 16 * (DH + 2);
+      if (g4 == 0) {
+        cw[16 * DH + 2 * c16] = mx[mt];
+        cw[16 * DH + 2 * c16 + 1] = l;
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int e = 0; e < NE; ++e) cw[(NE * (4 * g4 + i) + e) * 16 + c16] = o[mt][e][i];
+      __syncthreads();
+      // thread: column tid / 16, DH / 16 consecutive features
+      const int col = tid >> 4, f0 = (tid & 15) * NE;
+      float M = -INFINITY, L = 0.f, acc[NE];
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) M = fmaxf(M, comb[w * 16 * (DH + 2) + 16 * DH + 2 * col]);
+#pragma unroll
+      for (int e = 0; e < NE; ++e) acc[e] = 0.f;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        const float* p = comb + w * 16 * (DH + 2);
+        const float mw = p[16 * DH + 2 * col], lw = p[16 * DH + 2 * col + 1];
+        // (a NaN sum without a maximum is a row of NaN scores)
+        const float f = mw == -INFINITY ? (lw != lw ? lw : 0.f) : exp_nat(mw - M);
+        L += f * lw;
+#pragma unroll
+        for (int e = 0; e < NE; ++e) acc[e] += f * p[(f0 + e) * 16 + col];
+      }
+      __syncthreads();
+      const int row = (zz * MT + mt) * 16 + col;
+      if (row >= rows) continue;
+      const int64_t t = t0 + row / a.G;
+      const int h = g * a.G + row % a.G;
+      if (split) {
+        const int64_t at = (static_cast<int64_t>(c) * a.n_tgt + t) * a.H + h;
+#pragma unroll
+        for (int e = 0; e < NE; ++e) a.part_o[at * DH + f0 + e] = acc[e];
+        if (f0 == 0) {
+          a.part_ml[2 * at] = M;
+          a.part_ml[2 * at + 1] = L;
+        }
+      } else {
+        const float inv = L == 0.f ? 0.f : 1.f / L;
+        T* op = static_cast<T*>(a.out) + (t * a.H + h) * DH + f0;
+#pragma unroll
+        for (int e = 0; e < NE; ++e) {
+          const float y = acc[e] * inv;
+          op[e] = from_f32<T>(y);
+          if (a.sa) a.sa[(t * a.H + h) * DH + f0 + e] = y;
+        }
+        if (a.sm && f0 == 0) {
+          a.sm[t * a.H + h] = M;
+          a.sl[t * a.H + h] = L;
+        }
+      }
+    }
+  }
+}
+
+template <typename T, int KV, int DH, int MT>
+hipError_t launch_fwd(const AttnArgs& a, hipStream_t st) {
+  const int64_t pages = KV == kRagged ? 0 : (a.chunk >> a.page_shift) + 1;
+  const size_t lds = 4 * (kCombineFloats<DH> + kMaxBuckets + 32 + static_cast<int64_t>(a.G) * a.b.n + pages);
+  const int64_t grid = round_up(a.units, kXcds) * a.Hk * a.zgroups + 1;
+  if (grid > 0x7fffffff) return hipErrorInvalidValue;
+  const hipError_t e = allow_lds<&attn_fwd_kernel<T, KV, DH, MT>>(lds);
+  if (e != hipSuccess) return e;
+  attn_fwd_kernel<T, KV, DH, MT><<<static_cast<unsigned>(grid), kThreads, lds, st>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace ops
+}  // namespace stca

@@ -33,7 +33,11 @@ EXPORTED = ("stca_workspace_size", "stca_saved_size", "stca_saved_layout", "stca
             "stca_sl_beta", "stca_sl_sample", "stca_sl_allocate", "stca_sl_pack",
             "stca_paper_workspace_size", "stca_paper_saved_size", "stca_paper_saved_layout", "stca_forward_paper",
             "stca_paper_launch_count", "stca_forward_paper_profiled", "stca_train_record_size", "stca_forward_train",
-            "stca_backward_record", "stca_forward_noalloc")
+            "stca_backward_record", "stca_forward_noalloc", "stca_attn_workspace_size", "stca_attn_saved_size",
+            "stca_attn_saved_layout", "stca_attn_forward", "stca_attn_backward", "stca_bias_edges",
+            "stca_cache_write", "stca_cache_read", "stca_cache_attn_workspace_size", "stca_cache_attn")
+STCA_CACHE_BF16, STCA_CACHE_INT8 = 0, 1
+CACHE_WS_BYTES = 256  # STCA_CACHE_WS_BYTES
 NOALLOC_SCRATCH_BYTES = 256 << 20  # STCA_NOALLOC_SCRATCH_BYTES
 PAPER_WEIGHT_FIELDS = ("ffn_u", "ffn_v", "ffn_o", "wq", "wk", "wv", "wo", "wc", "wz", "z_u", "z_v", "z_o")
 
@@ -68,6 +72,45 @@ class stca_paper_weights_t(ctypes.Structure):
 
 class stca_paper_saved_layout_t(ctypes.Structure):
     _fields_ = [(k, ctypes.c_size_t) for k in ("q", "a", "o", "lse", "xt", "total")]
+
+
+class stca_attn_t(ctypes.Structure):
+    _fields_ = [("n_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("d_head", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("scale", ctypes.c_float), ("softcap", ctypes.c_float),
+                ("masked", ctypes.c_int32), ("n_buckets", ctypes.c_int32), ("edges_host", ctypes.c_void_p)]
+
+
+class stca_attn_in_t(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("ldq", ctypes.c_int64),
+                ("ldk", ctypes.c_int64), ("ldv", ctypes.c_int64), ("tgt_pos", ctypes.c_void_p),
+                ("hist_pos", ctypes.c_void_p), ("bias", ctypes.c_void_p)]
+
+
+class stca_attn_grads_t(ctypes.Structure):
+    _fields_ = [("dq", ctypes.c_void_p), ("dk", ctypes.c_void_p), ("dv", ctypes.c_void_p), ("lddq", ctypes.c_int64),
+                ("lddk", ctypes.c_int64), ("lddv", ctypes.c_int64), ("dbias", ctypes.c_void_p)]
+
+
+class stca_attn_saved_layout_t(ctypes.Structure):
+    _fields_ = [(k, ctypes.c_size_t) for k in ("a", "max", "sum", "total")]
+
+
+class stca_cache_t(ctypes.Structure):
+    _fields_ = [("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+                ("d_head", ctypes.c_int32), ("format", ctypes.c_int32), ("k", ctypes.c_void_p),
+                ("v", ctypes.c_void_p), ("k_exp", ctypes.c_void_p), ("v_exp", ctypes.c_void_p),
+                ("pos", ctypes.c_void_p)]
+
+
+class stca_cache_rows_t(ctypes.Structure):
+    _fields_ = [("n_requests", ctypes.c_int32), ("n_rows", ctypes.c_int64), ("row_off", ctypes.c_void_p),
+                ("start", ctypes.c_void_p), ("table", ctypes.c_void_p), ("table_ld", ctypes.c_int32)]
+
+
+class stca_cache_batch_t(ctypes.Structure):
+    _fields_ = [("n_requests", ctypes.c_int32), ("n_tgt", ctypes.c_int64), ("tgt_off", ctypes.c_void_p),
+                ("tgt_off_host", ctypes.c_void_p), ("lens", ctypes.c_void_p), ("max_len", ctypes.c_int32),
+                ("table", ctypes.c_void_p), ("table_ld", ctypes.c_int32)]
 
 
 class StcaError(RuntimeError):
@@ -169,6 +212,23 @@ def lib():
                                                   P(stca_paper_weights_t), ctypes.c_void_p, ctypes.c_void_p,
                                                   ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p,
                                                   P(ctypes.c_void_p), ctypes.c_int, P(ctypes.c_char_p)]
+        V, SZ, I64 = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int64
+        A, B = P(stca_attn_t), P(stca_batch_t)
+        for name, res, args in (
+                ("stca_attn_workspace_size", SZ, [A, B, ctypes.c_int]),
+                ("stca_attn_saved_size", SZ, [A, B]),
+                ("stca_attn_saved_layout", ctypes.c_int, [A, B, P(stca_attn_saved_layout_t)]),
+                ("stca_attn_forward", ctypes.c_int, [A, B, P(stca_attn_in_t), V, V, V, SZ, V]),
+                ("stca_attn_backward", ctypes.c_int, [A, B, P(stca_attn_in_t), V, V, P(stca_attn_grads_t), V, SZ, V]),
+                ("stca_bias_edges", ctypes.c_int, [ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, I32P]),
+                ("stca_cache_write", ctypes.c_int,
+                 [P(stca_cache_t), P(stca_cache_rows_t), ctypes.c_int32, V, V, I64, I64, V, V, V]),
+                ("stca_cache_read", ctypes.c_int,
+                 [P(stca_cache_t), P(stca_cache_rows_t), ctypes.c_int32, V, V, I64, I64, V, V, V]),
+                ("stca_cache_attn_workspace_size", SZ, [A, P(stca_cache_t), P(stca_cache_batch_t)]),
+                ("stca_cache_attn", ctypes.c_int,
+                 [A, P(stca_cache_t), P(stca_cache_batch_t), V, I64, V, V, V, V, SZ, V])):
+            getattr(L, name).restype, getattr(L, name).argtypes = res, args
         _lib = L
     return _lib
 
@@ -356,6 +416,101 @@ def stca_forward_paper_profiled(d, b, hist, tgt, w, z, saved, ws, ws_bytes: int,
     if st != STCA_OK:
         raise StcaError(st, "stca_forward_paper_profiled")
     return st
+
+
+# ---- stand-alone attention and paged history cache
+def _checked(name: str, check: bool, *args) -> int:
+    st = getattr(lib(), name)(*args)
+    if check and st != STCA_OK:
+        raise StcaError(st, name)
+    return st
+
+
+def attn(n_heads: int, n_kv_heads: int, d_head: int, dtype: int, scale: float, softcap: float = 0.0,
+         masked: bool = False, n_buckets: int = 0, edges=None) -> stca_attn_t:
+    """edges: contiguous int32 numpy array [n_buckets - 1], kept alive by the caller."""
+    return stca_attn_t(n_heads, n_kv_heads, d_head, dtype, scale, softcap, int(masked), n_buckets,
+                       None if edges is None else edges.ctypes.data)
+
+
+def attn_in(q, k, v, ldq: int = 0, ldk: int = 0, ldv: int = 0, tgt_pos=None, hist_pos=None,
+            bias=None) -> stca_attn_in_t:
+    return stca_attn_in_t(_ptr(q), _ptr(k), _ptr(v), ldq, ldk, ldv, _ptr(tgt_pos), _ptr(hist_pos), _ptr(bias))
+
+
+def attn_grads(dq, dk, dv, lddq: int = 0, lddk: int = 0, lddv: int = 0, dbias=None) -> stca_attn_grads_t:
+    return stca_attn_grads_t(_ptr(dq), _ptr(dk), _ptr(dv), lddq, lddk, lddv, _ptr(dbias))
+
+
+def cache(n_pages: int, page_size: int, n_kv_heads: int, d_head: int, fmt: int, k, v, k_exp=None, v_exp=None,
+          pos=None) -> stca_cache_t:
+    return stca_cache_t(n_pages, page_size, n_kv_heads, d_head, fmt, _ptr(k), _ptr(v), _ptr(k_exp), _ptr(v_exp),
+                        _ptr(pos))
+
+
+def cache_rows(n_requests: int, n_rows: int, row_off, start, table, table_ld: int) -> stca_cache_rows_t:
+    return stca_cache_rows_t(n_requests, n_rows, _ptr(row_off), _ptr(start), _ptr(table), table_ld)
+
+
+def cache_batch(n_requests: int, n_tgt: int, tgt_off, lens, max_len: int, table, table_ld: int,
+                tgt_off_host=None) -> stca_cache_batch_t:
+    """tgt_off_host: optional contiguous int32 numpy array, kept alive by the caller."""
+    return stca_cache_batch_t(n_requests, n_tgt, _ptr(tgt_off), None if tgt_off_host is None else
+                              tgt_off_host.ctypes.data, _ptr(lens), max_len, _ptr(table), table_ld)
+
+
+def stca_attn_workspace_size(a: stca_attn_t, b: stca_batch_t, with_backward: bool = False) -> int:
+    return lib().stca_attn_workspace_size(ctypes.byref(a), ctypes.byref(b), int(with_backward))
+
+
+def stca_attn_saved_size(a: stca_attn_t, b: stca_batch_t) -> int:
+    return lib().stca_attn_saved_size(ctypes.byref(a), ctypes.byref(b))
+
+
+def stca_attn_saved_layout(a: stca_attn_t, b: stca_batch_t) -> stca_attn_saved_layout_t:
+    out = stca_attn_saved_layout_t()
+    _checked("stca_attn_saved_layout", True, ctypes.byref(a), ctypes.byref(b), ctypes.byref(out))
+    return out
+
+
+def stca_attn_forward(a, b, given, out, saved, ws, ws_bytes: int, stream=None, check: bool = True) -> int:
+    return _checked("stca_attn_forward", check, ctypes.byref(a), ctypes.byref(b), ctypes.byref(given), _ptr(out),
+                    _ptr(saved), _ptr(ws), int(ws_bytes), _ptr(stream))
+
+
+def stca_attn_backward(a, b, given, saved, dout, grads, ws, ws_bytes: int, stream=None, check: bool = True) -> int:
+    return _checked("stca_attn_backward", check, ctypes.byref(a), ctypes.byref(b), ctypes.byref(given), _ptr(saved),
+                    _ptr(dout), ctypes.byref(grads), _ptr(ws), int(ws_bytes), _ptr(stream))
+
+
+def bias_edges(n_buckets: int, n_exact: int, max_distance: int):
+    """Edges [n_buckets - 1] (int32): 1 .. n_exact, then a geometric series to max_distance."""
+    import numpy as np
+    out = np.empty(max(0, n_buckets - 1), dtype=np.int32)
+    _checked("stca_bias_edges", True, n_buckets, n_exact, max_distance, _i32p(out))
+    return out
+
+
+def stca_cache_write(c, rows, dtype: int, k, v, ldk: int = 0, ldv: int = 0, pos=None, ws=None, stream=None,
+                     check: bool = True) -> int:
+    return _checked("stca_cache_write", check, ctypes.byref(c), ctypes.byref(rows), dtype, _ptr(k), _ptr(v), ldk, ldv,
+                    _ptr(pos), _ptr(ws), _ptr(stream))
+
+
+def stca_cache_read(c, rows, dtype: int, k, v, ldk: int = 0, ldv: int = 0, pos=None, ws=None, stream=None,
+                    check: bool = True) -> int:
+    return _checked("stca_cache_read", check, ctypes.byref(c), ctypes.byref(rows), dtype, _ptr(k), _ptr(v), ldk, ldv,
+                    _ptr(pos), _ptr(ws), _ptr(stream))
+
+
+def stca_cache_attn_workspace_size(a: stca_attn_t, c: stca_cache_t, b: stca_cache_batch_t) -> int:
+    return lib().stca_cache_attn_workspace_size(ctypes.byref(a), ctypes.byref(c), ctypes.byref(b))
+
+
+def stca_cache_attn(a, c, b, q, ldq: int, tgt_pos, bias, out, ws, ws_bytes: int, stream=None,
+                    check: bool = True) -> int:
+    return _checked("stca_cache_attn", check, ctypes.byref(a), ctypes.byref(c), ctypes.byref(b), _ptr(q), ldq,
+                    _ptr(tgt_pos), _ptr(bias), _ptr(out), _ptr(ws), int(ws_bytes), _ptr(stream))
 
 
 class HipEvents:
