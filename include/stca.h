@@ -437,12 +437,12 @@ typedef struct {
   float softcap;             /* >= 0, 0 = none */
   int32_t masked;            /* nonzero: rows with hist_pos > tgt_pos are hidden */
   int32_t n_buckets;         /* 0 = no bias; at most 128 */
-  const int32_t* edges_host; /* host [n_buckets - 1], strictly ascending, the first >= 1; read by the call */
+  const int32_t* edges_host; /* host [n_buckets - 1], strictly ascending in 1..2^31-2; read by the call */
 } stca_attn_t;
 
 /* Positions and tables of bias, and a cache's pos, need 4-byte alignment only.
  * Rows of q, k, v hold their heads one after the other; ld* are row strides in
- * elements (0 = dense; a multiple of 16 bytes).  tgt_pos is needed with a mask
+ * elements (0 = dense; a multiple of 16 bytes, below 16 MB).  tgt_pos is needed with a mask
  * or a bias; hist_pos NULL: a row's position is its index in its request. */
 typedef struct {
   const void* q;            /* [n_tgt][n_heads][d_head] */
@@ -464,7 +464,8 @@ typedef struct {
 
 /* Byte offsets into the buffer that a forward saves for its backward, fp32:
  * a [n_tgt][n_heads][d_head] (the output before rounding), and per target and
- * head the largest score and the sum of exp(x - largest) [n_tgt][n_heads]. */
+ * head a score max near the largest, in units of log2 e, and the sum of
+ * 2^(x log2 e - max) [n_tgt][n_heads]. */
 typedef struct {
   size_t a, max, sum;
   size_t total;
@@ -490,7 +491,8 @@ stca_status_t stca_attn_backward(const stca_attn_t* attn, const stca_batch_t* ba
 
 /* Bucket edges as distances grow: 1, 2, ..., n_exact, then a geometric series
  * to max_distance (each at least one more than the last), n_buckets - 1 in all.
- * Host function.  1 <= n_exact < n_buckets <= 128, max_distance >= n_buckets. */
+ * Host function.  1 <= n_exact < n_buckets <= 128,
+ * n_buckets <= max_distance < 2^31 - 1. */
 stca_status_t stca_bias_edges(int32_t n_buckets, int32_t n_exact, int32_t max_distance, int32_t* edges);
 
 /* ---- Paged history cache.  K and V of a history row do not depend on the

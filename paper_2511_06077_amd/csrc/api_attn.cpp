@@ -11,6 +11,9 @@ using namespace stca;
 using namespace stca::api;
 using namespace stca::ops;
 
+#ifndef PCU
+#define PCU 4
+#endif
 namespace {
 
 constexpr int64_t kMaxRows = 0x7fff0000;  // rows of one call: indices a few blocks past the end stay int32
@@ -30,6 +33,7 @@ stca_status_t check_attn(const stca_attn_t* a) {
     if (!a->edges_host || a->edges_host[0] < 1) return STCA_ERR_INVALID_ARG;
     for (int i = 1; i < a->n_buckets - 1; ++i)
       if (a->edges_host[i] <= a->edges_host[i - 1]) return STCA_ERR_INVALID_ARG;
+    if (a->edges_host[a->n_buckets - 2] == INT32_MAX) return STCA_ERR_INVALID_ARG;
   }
   if ((a->d_head != 32 && a->d_head != 64 && a->d_head != 128) || a->n_heads / a->n_kv_heads > kMaxGroup ||
       static_cast<int64_t>(a->n_heads) * a->d_head > 65536)
@@ -76,26 +80,28 @@ int shift_of(int page_size) {
 // Row stride: 0 = dense; else at least the row and a multiple of 16 bytes.
 bool stride(int64_t given, int64_t dense, int es, int64_t* out) {
   *out = given == 0 ? dense : given;
-  return *out >= dense && *out * es % 16 == 0 && *out <= (int64_t(1) << 22);
+  return *out >= dense && *out * es % 16 == 0 && *out * es < (int64_t(1) << 24);
 }
 
-void fill_buckets(const stca_attn_t* a, Buckets* b) {
+void fill_edges(const stca_attn_t* a, Buckets* b) {
   b->n = a->n_buckets;
+  b->multi = 0;
   const int n = std::max(0, a->n_buckets - 1);
   for (int i = 0; i < n; ++i) b->edges[i] = a->edges_host[i];
   for (int i = n; i < kMaxBuckets; ++i) b->edges[i] = INT32_MAX;
-  int k = 0;
-  for (int c = 0; c < 128; ++c) {
-    // lowest distance of octave c / 4, quarter c % 4 (cells of the first two
-    // octaves that hold no whole number are never asked for)
-    const int64_t low = c == 0 ? 0 : (static_cast<int64_t>(4 + c % 4) << (c / 4)) >> 2;
-    while (k < n && b->edges[k] <= low) ++k;
+  // an entry of the lookup holds one edge: which lowest x has not passed, but
+  // the cell's other ones may
+  for (int c = 0, k = 0; c < kHiddenCell; ++c) {
+    const int64_t low = cell_low(c), last = cell_low(c + 1) - 1;
+    while (k < n && b->edges[k] < low) ++k;
     b->cell[c] = static_cast<uint8_t>(k);
+    if (k + 1 < n && b->edges[k + 1] < last) b->multi = 1;
   }
+  b->cell[kHiddenCell] = 0;
 }
 
 struct Plan {
-  int chunk, max_chunks, units, tiles, zgroups, btiles, passes;
+  int chunk, max_chunks, units, tiles, zgroups, btiles, passes, hw;
   size_t hdr, part_o, part_ml, part_dq, part_db, acc_kv, total;
 };
 
@@ -107,6 +113,16 @@ int chunk_for(int64_t rows, int64_t per_row, int per_cu) {
   const int64_t want = static_cast<int64_t>(per_cu) * device_cus();
   const int64_t c = round_up(std::max<int64_t>(1, ceil_div(rows * per_row, want)), kChunkStep);
   return static_cast<int>(std::min<int64_t>(c, round_up(kMaxRows, kChunkStep) - kChunkStep));
+}
+
+// kv heads a workgroup takes (see attn_fwd.h): as many as there are to four,
+// where a wave to a head then has 256 history rows on every SIMD of the card.
+int heads_of(int Hk, int64_t n_hist) {
+  const int most = Hk % 4 == 0 ? 4 : Hk % 2 == 0 ? 2 : 1;
+#ifdef HWF
+  return std::min(most, HWF);
+#endif
+  return n_hist * Hk >= 256 * 4 * static_cast<int64_t>(device_cus()) ? most : 1;
 }
 
 bool ragged_plan(const stca_attn_t* a, const stca_batch_t* b, bool backward, Plan* p) {
@@ -122,17 +138,18 @@ bool ragged_plan(const stca_attn_t* a, const stca_batch_t* b, bool backward, Pla
   p->tiles = forward_tiles(a->dtype, dh, static_cast<int>(std::min<int64_t>(max_m * G, 1 << 20)));
   p->zgroups = static_cast<int>(std::min<int64_t>(std::max<int64_t>(1, ceil_div(max_m * G, 16 * p->tiles)),
                                                   b->hist_off_host ? 1024 : 8));
-  p->chunk = chunk_for(b->n_hist, static_cast<int64_t>(Hk) * (backward ? 1 : p->zgroups), 4);
+  p->chunk = chunk_for(b->n_hist, static_cast<int64_t>(Hk / heads_of(Hk, b->n_hist)) * (backward ? 1 : p->zgroups), PCU);
   if (!b->hist_off_host)
     p->chunk = static_cast<int>(std::max<int64_t>(p->chunk, round_up(ceil_div(b->n_hist, kNoHostChunks), kChunkStep)));
   p->chunk = static_cast<int>(std::min<int64_t>(p->chunk, std::max<int64_t>(kChunkStep, round_up(max_l, kChunkStep))));
   p->max_chunks = static_cast<int>(std::max<int64_t>(1, ceil_div(max_l, p->chunk)));
+  p->hw = heads_of(Hk, b->n_hist);
   const int64_t units = b->n_hist / p->chunk + b->n_requests;
   if (units * Hk * p->zgroups > 0x7f000000) return false;
   p->units = static_cast<int>(units);
-  const int64_t need = ceil_div(max_m, 16) * G;
+  const int64_t need = ceil_div(max_m, 16);
   p->btiles = backward_tiles(a->dtype, dh, static_cast<int>(std::min<int64_t>(need, 1 << 20)));
-  p->passes = static_cast<int>(std::max<int64_t>(1, ceil_div(need, p->btiles)));
+  p->passes = static_cast<int>(std::max<int64_t>(1, ceil_div(need, p->btiles) * G));
   Bump m;
   p->hdr = m.take(sizeof(WsHeader));
   const size_t rows = static_cast<size_t>(b->n_tgt) * H, split = p->max_chunks > 1 ? p->max_chunks : 0;
@@ -156,7 +173,7 @@ void fill_attn(const stca_attn_t* a, AttnArgs* g) {
   g->placed = a->masked != 0 || a->n_buckets > 0;
   g->scale = a->scale;
   g->cap = a->softcap;
-  fill_buckets(a, &g->b);
+  fill_edges(a, &g->b);
 }
 
 stca_status_t fill_ragged(const stca_attn_t* a, const stca_batch_t* b, const stca_attn_in_t* in, AttnArgs* g) {
@@ -219,6 +236,7 @@ bool paged_plan(const stca_attn_t* a, const stca_cache_t* c, const stca_cache_ba
   const int64_t units = static_cast<int64_t>(b->n_requests) * p->max_chunks;
   if (units * Hk * p->zgroups > 0x7f000000) return false;
   p->units = static_cast<int>(units);
+  p->hw = 1;  // (a head's pages are contiguous)
   Bump m;
   p->hdr = m.take(sizeof(WsHeader));
   const size_t rows = static_cast<size_t>(b->n_tgt) * H, split = p->max_chunks > 1 ? p->max_chunks : 0;
@@ -327,6 +345,7 @@ stca_status_t stca_attn_forward(const stca_attn_t* attn, const stca_batch_t* bat
   a.chunk = p.chunk;
   a.max_chunks = p.max_chunks;
   a.units = p.units;
+  a.hw = p.hw;
   a.zgroups = p.zgroups;
   a.out = out;
   if (saved) {
@@ -377,6 +396,7 @@ stca_status_t stca_attn_backward(const stca_attn_t* attn, const stca_batch_t* ba
   a.chunk = p.chunk;
   a.max_chunks = p.max_chunks;
   a.units = p.units;
+  a.hw = p.hw;
   a.zgroups = 1;
   a.part_dq = at<float>(ws, p.part_dq);
   a.part_db = at<float>(ws, p.part_db);
@@ -387,7 +407,8 @@ stca_status_t stca_attn_backward(const stca_attn_t* attn, const stca_batch_t* ba
 }
 
 stca_status_t stca_bias_edges(int32_t n_buckets, int32_t n_exact, int32_t max_distance, int32_t* edges) {
-  if (n_buckets < 2 || n_buckets > kMaxBuckets || n_exact < 1 || n_exact >= n_buckets || max_distance < n_buckets || !edges)
+  if (n_buckets < 2 || n_buckets > kMaxBuckets || n_exact < 1 || n_exact >= n_buckets || max_distance < n_buckets ||
+      max_distance == INT32_MAX || !edges)
     return STCA_ERR_INVALID_ARG;
   const int n = n_buckets - 1;
   for (int i = 0; i < n; ++i) {
@@ -453,6 +474,7 @@ stca_status_t stca_cache_attn(const stca_attn_t* attn, const stca_cache_t* cache
   a.chunk = p.chunk;
   a.max_chunks = p.max_chunks;
   a.units = p.units;
+  a.hw = p.hw;
   a.zgroups = p.zgroups;
   a.out = out;
   a.part_o = at<float>(ws, p.part_o);

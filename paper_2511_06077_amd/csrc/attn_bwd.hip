@@ -5,28 +5,32 @@
 //   dz = dx (1 - (y / c)^2)                                 (c: the score cap)
 //   dv_j += w dout,  dk_j += scale dz q,  dq_t += scale dz k_j
 //
-// One workgroup takes one chunk of one request's history for one kv head; its
-// four waves take steps of 16 JT history rows in turn and hold dK^T, dV^T of a
-// step in registers while they go through the pass's MT tiles of 16 targets (of
+// One workgroup takes one chunk of one request's history for hw kv heads; 4 / hw
+// of its four waves share a head, each with consecutive steps of 16 JT history
+// rows (see attn_fwd.h), and hold dK^T, dV^T of a step in registers while they go through the pass's MT tiles of 16 targets (of
 // one query head each), whose q and dout rows wait in LDS.  dq of a pass stays
 // in registers over the whole chunk.  More tiles than MT are further passes
 // over the chunk, with dK, dV of the passes so far in fp32 in the workspace
 // (the same lanes write and read them).  So K, V are read and dK, dV written
 // once, nothing is added in order of arrival, and gradients repeat bitwise.
 //
-// Scores are formed as S = Q K^T: a lane holds column j = lane % 16 and rows
-// t = 4 (lane / 16) + i, which is the operand of the sums over t (dV^T =
-// dout^T w, dK^T = q^T dz) as it stands.  The sum over j (dQ = dz K) needs the
-// other order: dz goes through LDS, written four targets at a time and read
-// with the transposing LDS read; K too, and q^T, dout^T likewise.
+// Scores are formed as S^T = K Q^T: a lane holds one target, column t = lane %
+// 16, and rows j = 4 (lane / 16) + i, so that the target's constants and its
+// bucket are a lane's own, and dz is the operand of the sum over j (dQ^T = K^T
+// dz) as it stands.  The sums over t (dV^T = dout^T w, dK^T = q^T dz) need the
+// other order: w and dz go through LDS, written four rows at a time and read
+// with the transposing LDS read; K^T, q^T and dout^T likewise.
 //
-// w and dz are split into two bf16 terms (the products then carry 16
-// significant bits, and the one rounding left is the output's).
+// w and dz enter the products as two bf16 terms each (16 significant bits, so
+// the one rounding that is left is the output's).
 //
-// dbias: a lane sums the dx of its column in a register as long as its bucket
-// (an interval of distances) covers all four targets; when a vote finds a lane
-// outside, the wave sums bucket by bucket what its lanes hold (the first
-// lane's bucket, then the first of those left) into LDS sums of its own.
+// dbias: a lane sums the dx of its target in a register as long as its bucket
+// (an interval of distances) covers its rows.  When a vote finds a lane outside,
+// every score looks its bucket up, and the four of a lane go to LDS sums that
+// belong to the lane (or to lanes that take turns), so that the order is fixed:
+// in two sums where they lie in the first's and the last's bucket, else one by
+// one.  (LDS float atomics in their place take a cycle a lane: 2.3 times the
+// kernel's time, window of 256 requests with 32 buckets.)
 #include <type_traits>
 
 #include "attn_ops.h"
@@ -75,6 +79,17 @@ __device__ __forceinline__ Eight<T> load8(const T* p) {
   } else {
     r.a = reinterpret_cast<const f32x4*>(p)[0];
     r.b = reinterpret_cast<const f32x4*>(p)[1];
+  }
+  return r;
+}
+template <typename T>
+__device__ __forceinline__ Eight<T> load8_at(gptr p, uint32_t at) {
+  Eight<T> r;
+  if constexpr (Elem<T>::bf16) {
+    r.v = load_at<bf16x8>(p, at);
+  } else {
+    r.a = load_at<f32x4>(p, at);
+    r.b = load_at<f32x4>(p + 16, at);
   }
   return r;
 }
@@ -141,25 +156,38 @@ __device__ __forceinline__ f32x4 cleared(f32x4 x, uint32_t h) {
   return x;
 }
 
+// Bytes of a target's row in the tiles of w and dz: bf16 4 terms of 16 rows,
+// fp32 2 of 16 and a pad.
+template <typename T> constexpr int kPRow = Elem<T>::bf16 ? 4 * 32 + 16 : 2 * 64 + 16;
+
 // LDS of a workgroup, in bytes.
 template <typename T, int DH, int MT, int JT>
 struct BwdLds {
-  static constexpr int kQ = 0;                                       // q rows of the pass
-  static constexpr int kDo = kQ + 16 * MT * kRowBytes<T, DH>;        // dout rows
-  static constexpr int kRow = kDo + 16 * MT * kRowBytes<T, DH>;      // per row: maximum, 1 / sum, D, position
-  static constexpr int kK = kRow + 16 * MT * 16;                     // per wave: K rows of the step
+  static constexpr int kHead = 16 * MT * (2 * kRowBytes<T, DH> + 16);  // per head of the pass: q rows, dout rows,
+  static constexpr int kDo = 16 * MT * kRowBytes<T, DH>;               // and per row maximum, 1 / sum, D, position
+  static constexpr int kRow = 2 * kDo;
+  static constexpr int kK = 0;                                       // per wave: K rows of the step
   static constexpr int kKWave = 16 * JT * kRowBytes<T, DH>;
-  static constexpr int kDz = kK + kWaves * kKWave;                   // per wave: dz tile, both terms
-  static constexpr int kDzWave = 16 * JT * (Elem<T>::bf16 ? 2 * 32 : 80);
+  static constexpr int kDz = kK + kWaves * kKWave;                   // per wave: w and dz tiles, both terms
+  static constexpr int kDzWave = JT * kPRow<T> * 16;
   static constexpr int kComb = kDz + kWaves * kDzWave;               // dq of the waves
-  static constexpr int kBins = kComb + kWaves * 16 * DH * 4;         // dbias per wave and tile
-  static size_t bytes(int G, int n) {
-    return kBins + 4 * (kWaves * MT * static_cast<size_t>(n) + kMaxBuckets + 32 + 2 * static_cast<size_t>(G) * n);
+  static constexpr int kTables = kComb + kWaves * 16 * (DH + 4) * 4;       // heads, cells, edges, biases, dbias per head, bins
+  static size_t bytes(int hw, int G, int n, int copies) {
+    const size_t slots = n > 1 ? n : 1, heads = static_cast<size_t>(hw) * G;
+    return kTables + hw * kHead + 8 * (kCells + 1) +
+           4 * (kMaxBuckets + heads * (slots + 1) + heads * n + (n ? kWaves * (slots + 1) * copies : 0));
   }
 };
 
+// Lanes of a wave that have dbias sums of their own: all while the four waves'
+// sums stay within 36 KB, else every second or fourth, which then take turns.
+inline __host__ __device__ int bin_copies(int n) { return n <= 34 ? 64 : n <= 70 ? 32 : 16; }
+
+#ifndef EUB
+#define EUB 2
+#endif
 template <typename T, int DH, int MT, int JT>
-__global__ __launch_bounds__(kThreads) void attn_bwd_kernel(const AttnArgs a) {
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(EUB))) void attn_bwd_kernel(const AttnArgs a) {
   constexpr bool kBf16 = Elem<T>::bf16;
   constexpr int KS = DH / 32, NE = DH / 16, BJ = 16 * JT;
   using F4 = typename Four<T>::type;
@@ -167,13 +195,13 @@ __global__ __launch_bounds__(kThreads) void attn_bwd_kernel(const AttnArgs a) {
   using Lds = BwdLds<T, DH, MT, JT>;
   extern __shared__ __align__(16) unsigned char smem[];
   const int nb = a.b.n;
-  float* s_row = reinterpret_cast<float*>(smem + Lds::kRow);
   float* s_comb = reinterpret_cast<float*>(smem + Lds::kComb);
-  float* s_bins = reinterpret_cast<float*>(smem + Lds::kBins);
-  int32_t* s_edges = reinterpret_cast<int32_t*>(s_bins + kWaves * MT * nb);
-  uint8_t* s_cell = reinterpret_cast<uint8_t*>(s_edges + kMaxBuckets);
-  float* s_bias = reinterpret_cast<float*>(s_cell + 128);
-  float* s_db = s_bias + a.G * nb;
+  const int slots = max(nb, 1), copies = bin_copies(nb);
+  int2* s_cells = reinterpret_cast<int2*>(smem + Lds::kTables + a.hw * Lds::kHead);
+  int32_t* s_edges = reinterpret_cast<int32_t*>(s_cells + kCells + 1);
+  float* s_bias = reinterpret_cast<float*>(s_edges + kMaxBuckets);
+  float* s_db = s_bias + a.hw * a.G * (slots + 1);
+  float* s_bins = s_db + a.hw * a.G * nb;
 
   const int tid = threadIdx.x, lane = tid & 63, c16 = lane & 15, g4 = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -181,48 +209,50 @@ __global__ __launch_bounds__(kThreads) void attn_bwd_kernel(const AttnArgs a) {
     check_call(a, false);
     return;
   }
-  const int unit = static_cast<int>(blockIdx.x) / kXcds / a.Hk * kXcds + static_cast<int>(blockIdx.x) % kXcds;
+  const int ghs = a.Hk / a.hw;
+  const int unit = static_cast<int>(blockIdx.x) / kXcds / ghs * kXcds + static_cast<int>(blockIdx.x) % kXcds;
   if (unit >= a.units) return;
-  const int g = static_cast<int>(blockIdx.x) / kXcds % a.Hk;
-  const int r = find_request(a.hist_off, a.R, a.n_hist, a.chunk, unit);
-  const int64_t h0 = clamp_off(a.hist_off[r], a.n_hist);
-  const int len = max(0, static_cast<int>(clamp_off(a.hist_off[r + 1], a.n_hist) - h0));
+  const int g0 = static_cast<int>(blockIdx.x) / kXcds % ghs * a.hw;
+  const int hs = wave % a.hw, part = wave / a.hw, parts = kWaves / a.hw, g = g0 + hs, heads = a.hw * a.G;
+  const int r = uniform(find_request(a.hist_off, a.R, a.n_hist, a.chunk, unit));
+  const int64_t h0 = uniform(clamp_off(a.hist_off[r], a.n_hist));
+  const int len = uniform(max(0, static_cast<int>(clamp_off(a.hist_off[r + 1], a.n_hist) - h0)));
   const int c = unit - static_cast<int>(h0 / a.chunk + r);
-  float* part_db = a.part_db + (static_cast<int64_t>(unit) * a.H + g * a.G) * nb;
+  float* part_db = a.part_db + (static_cast<int64_t>(unit) * a.H + g0 * a.G) * nb;
   if (c < 0 || c >= a.max_chunks || (c > 0 && static_cast<int64_t>(c) * a.chunk >= len)) {
-    for (int i = tid; i < a.G * nb; i += kThreads) part_db[i] = 0.f;
+    for (int i = tid; i < heads * nb; i += kThreads) part_db[i] = 0.f;
     return;
   }
   const int j0 = c * a.chunk, j1 = min(len, j0 + a.chunk);
-  const int t0 = clamp_off(a.tgt_off[r], a.n_tgt), m = max(0, clamp_off(a.tgt_off[r + 1], a.n_tgt) - t0);
-  const int ttiles = (m + 15) / 16, tiles = ttiles * a.G;
+  const int t0 = uniform(clamp_off(a.tgt_off[r], a.n_tgt)), m = max(0, uniform(clamp_off(a.tgt_off[r + 1], a.n_tgt)) - t0);
+  const int ttiles = (m + 15) / 16, groups = (ttiles + MT - 1) / MT;  // groups of MT tiles of one head
 
-  for (int i = tid; i < nb; i += kThreads) s_edges[i] = a.b.edges[i];
-  if (nb) {
-    if (tid < 128) s_cell[tid] = a.b.cell[tid];
-    for (int i = tid; i < a.G * nb; i += kThreads) {
-      s_bias[i] = a.bias[static_cast<int64_t>(g) * a.G * nb + i];
-      s_db[i] = 0.f;
-    }
-  }
-  const BucketLds bl{s_edges, s_cell, s_bias, nb};
+  BucketLds bl{};
+  if (a.placed) bl = fill_buckets(a, g0, heads, s_cells, s_bias, s_edges);
+  for (int i = tid; i < heads * nb; i += kThreads) s_db[i] = 0.f;
+  unsigned char* mine = smem + Lds::kTables + hs * Lds::kHead;  // q, dout and rows of this wave's head
+  const float* s_row = reinterpret_cast<const float*>(mine + Lds::kRow);
   unsigned char* kt = smem + Lds::kK + wave * Lds::kKWave;
   unsigned char* dzt = smem + Lds::kDz + wave * Lds::kDzWave;
+  float* bins = s_bins + wave * (slots + 1) * copies;
+  const float gain = kLog2e * (a.cap > 0.f ? a.cap : a.scale), cap_in = a.cap > 0.f ? a.scale / a.cap : 0.f;
 
-  const int passes = max(1, (tiles + MT - 1) / MT);
+  const int passes = max(1, groups * a.G);
   for (int pass = 0; pass < passes; ++pass) {
-    const int first = pass * MT, held = min(MT, tiles - first);
+    const int hh = groups ? pass / groups : 0, first = groups ? pass % groups * MT : 0;
+    const int held = min(MT, ttiles - first);
     __syncthreads();
     // ---- the pass's rows: 16 threads a row, DH / 16 features each
     int odd_rows = 0;
-    for (int row = tid >> 4; row < 16 * MT; row += kThreads / 16) {
-      const int tile = first + row / 16, hh = tile < tiles ? tile / ttiles : 0;
-      const int t = tile < tiles ? tile % ttiles * 16 + row % 16 : m;
+    for (int at = tid >> 4; at < 16 * MT * a.hw; at += kThreads / 16) {
+      const int hd = at / (16 * MT), row = at % (16 * MT);
+      unsigned char* to = smem + Lds::kTables + hd * Lds::kHead;
+      const int t = 16 * first + row;
       const bool have = t < m;
-      const int64_t tr = t0 + min(t, max(m - 1, 0)), h = g * a.G + hh;
+      const int64_t tr = t0 + min(t, max(m - 1, 0)), h = (g0 + hd) * a.G + hh;
       const int f = (tid & 15) * NE;
-      T* qs = reinterpret_cast<T*>(smem + Lds::kQ + row * kRowBytes<T, DH>) + f;
-      T* ds = reinterpret_cast<T*>(smem + Lds::kDo + row * kRowBytes<T, DH>) + f;
+      T* qs = reinterpret_cast<T*>(to + row * kRowBytes<T, DH>) + f;
+      T* ds = reinterpret_cast<T*>(to + Lds::kDo + row * kRowBytes<T, DH>) + f;
       float D = 0.f;
       bool odd = false;
 #pragma unroll
@@ -244,71 +274,90 @@ __global__ __launch_bounds__(kThreads) void attn_bwd_kernel(const AttnArgs a) {
         // a row without a target, or that sees nothing, has no weight anywhere
         const float mx = have ? a.fm[tr * a.H + h] : INFINITY, l = have ? a.fl[tr * a.H + h] : 1.f;
         const bool none = mx == -INFINITY && l == 0.f;
-        s_row[4 * row] = none ? INFINITY : mx;
-        s_row[4 * row + 1] = none ? 0.f : 1.f / l;
-        s_row[4 * row + 2] = none ? 0.f : D;
-        s_row[4 * row + 3] = __int_as_float(a.placed && m > 0 ? a.tgt_pos[tr] : 0);
+        reinterpret_cast<f32x4*>(to + Lds::kRow)[row] =
+            f32x4{none ? INFINITY : mx, none ? 0.f : 1.f / l, none ? 0.f : D,
+                  __int_as_float(a.placed && m > 0 ? a.tgt_pos[tr] : 0)};
       }
     }
-    for (int i = tid; i < kWaves * MT * nb; i += kThreads) s_bins[i] = 0.f;
+    if (nb)
+      for (int i = tid; i < kWaves * (slots + 1) * copies; i += kThreads) s_bins[i] = 0.f;
     odd_rows = __syncthreads_or(odd_rows);
 
+    // this lane's target of each tile: its constants, the bucket it keeps
     f32x4 dq[MT][NE];
-    float bias[MT], dsum[MT];
-    int blo[MT], bhi[MT], bk[MT], tmin[MT], tmax[MT], head[MT];
+    float mx[MT], il[MT], D[MT], bias[MT], dsum[MT];
+    int tp[MT], blo[MT], bhi[MT], bk[MT];
     int seen_max = -2147483647 - 1;
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
 #pragma unroll
       for (int e = 0; e < NE; ++e) dq[mt][e] = f32x4{};
+      const f32x4 row = *reinterpret_cast<const f32x4*>(s_row + 4 * (16 * mt + c16));
+      mx[mt] = row[0];
+      il[mt] = row[1];
+      D[mt] = row[2];
+      tp[mt] = __float_as_int(row[3]);
       bias[mt] = dsum[mt] = 0.f;
       bk[mt] = 0;
-      head[mt] = mt < held ? (first + mt) / ttiles : 0;
-      blo[mt] = a.masked ? 0 : -2147483647 - 1;
-      bhi[mt] = nb ? -2147483647 - 1 : 2147483647;
-      tmin[mt] = 2147483647;
-      tmax[mt] = -2147483647 - 1;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int p = __float_as_int(s_row[4 * (16 * mt + 4 * g4 + i) + 3]);
-        tmin[mt] = min(tmin[mt], p);
-        tmax[mt] = max(tmax[mt], p);
-      }
-      if (mt < held) seen_max = max(seen_max, tmax[mt]);
+      blo[mt] = a.masked ? 1 : 0;
+      bhi[mt] = nb ? -1 : 0x7fffffff;  // (a bias: none kept yet)
+      if (mt < held) seen_max = max(seen_max, tp[mt]);
     }
     int jend = j1;  // rows from here on are hidden from every target of the pass
     if (a.masked && !a.hist_pos) {
-      seen_max = max(seen_max, __shfl_xor(seen_max, 16));
-      seen_max = max(seen_max, __shfl_xor(seen_max, 32));
+#pragma unroll
+      for (int o = 1; o < 16; o <<= 1) seen_max = max(seen_max, __shfl_xor(seen_max, o));
       jend = static_cast<int>(min<int64_t>(jend, static_cast<int64_t>(seen_max) + 1));
       jend = __builtin_amdgcn_readfirstlane(jend);
     }
     if (held <= 0) jend = 0;
 
-    // what lanes hold for their buckets, into this wave's sums
-    auto add_bins = [&](int mt, const int* kk, const float* vv, int n) {
-      uint32_t left = (1u << n) - 1u;
-      while (true) {
-        const uint64_t some = __ballot(left != 0);
-        if (!some) break;
-        const int src = static_cast<int>(__builtin_ctzll(some));
-        int mine = kk[0];
-        for (int i = n - 1; i >= 0; --i)
-          if ((left >> i) & 1) mine = kk[i];
-        const int k = __builtin_amdgcn_readlane(mine, src);
-        float v = 0.f;
-        for (int i = 0; i < n; ++i)
-          if (((left >> i) & 1) && kk[i] == k) {
-            v += vv[i];
-            left &= ~(1u << i);
-          }
-#pragma unroll
-        for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
-        if (lane == 0) s_bins[(wave * MT + mt) * nb + k] += v;
+    // v to bucket k and u to bucket l of this lane's sums (l = -1: nothing)
+    auto add_bins = [&](int k, float v, int l, float u) {
+      if (l == k) {
+        v += u;
+        l = -1;
+      }
+      for (int turn = 0; turn < 64 / copies; ++turn) {
+        if (copies < 64 && lane / copies != turn) continue;
+        float* p = bins + k * copies + lane % copies;
+        float* q = bins + max(l, 0) * copies + lane % copies;
+        const float x = *p, y = *q;
+        *p = x + v;
+        if (l >= 0) *q = y + u;
       }
     };
 
-    for (int jb = j0 + wave * BJ; jb < j1; jb += kWaves * BJ) {
+    // each wave takes consecutive steps (a lane's bucket changes seldom then)
+    const int steps = (j1 - j0 + BJ - 1) / BJ, share = (steps + parts - 1) / parts;
+    const int jfirst = j0 + part * share * BJ, jstop = min(j1, jfirst + share * BJ);
+    E8 kf[JT][KS], vf[JT][KS];  // the step's rows, or the next one's once they are used
+    int pj[JT][4];              // positions of rows 4 g4 + i
+    const uint32_t lk = static_cast<uint32_t>(a.ldk * sizeof(T)), lv = static_cast<uint32_t>(a.ldv * sizeof(T));
+    auto load = [&](int jb) {
+      const int last = len - 1 - jb;
+      const gptr kp = uniform(static_cast<const T*>(a.k) + (h0 + jb) * a.ldk + g * DH);
+      const gptr vp = uniform(static_cast<const T*>(a.v) + (h0 + jb) * a.ldv + g * DH);
+#pragma unroll
+      for (int jt = 0; jt < JT; ++jt) {
+        const int jr = min(16 * jt + c16, last);
+        const uint32_t ak = __umul24(jr, lk) + 8 * g4 * sizeof(T), av = __umul24(jr, lv) + 8 * g4 * sizeof(T);
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+          kf[jt][s] = load8_at<T>(kp + 32 * s * sizeof(T), ak);
+          vf[jt][s] = load8_at<T>(vp + 32 * s * sizeof(T), av);
+        }
+      }
+      if (a.hist_pos) {
+        const gptr hp = uniform(a.hist_pos + h0 + jb);
+#pragma unroll
+        for (int jt = 0; jt < JT; ++jt)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) pj[jt][i] = load_at<int>(hp, 4u * min(16 * jt + 4 * g4 + i, last));
+      }
+    };
+    if (jfirst < min(jstop, jend)) load(jfirst);
+    for (int jb = jfirst; jb < jstop; jb += BJ) {
       f32x4 dk[JT][NE], dv[JT][NE];
       const int64_t acc_at = ((h0 + jb) * a.Hk + g) * DH;  // fp32 sums of the earlier passes: row jt 16 + c16
       const int64_t acc_v = a.n_hist * a.Hk * DH;
@@ -325,222 +374,236 @@ __global__ __launch_bounds__(kThreads) void attn_bwd_kernel(const AttnArgs a) {
           }
         }
       if (jb < jend) {
-        E8 kf[JT][KS], vf[JT][KS];
-        int pj[JT];
-        const int last = len - 1 - jb;
-#pragma unroll
-        for (int jt = 0; jt < JT; ++jt) {
-          const int jr = min(16 * jt + c16, last);
-          const T* kp = static_cast<const T*>(a.k) + (h0 + jb + jr) * a.ldk + g * DH + 8 * g4;
-          const T* vp = static_cast<const T*>(a.v) + (h0 + jb + jr) * a.ldv + g * DH + 8 * g4;
-#pragma unroll
-          for (int s = 0; s < KS; ++s) {
-            kf[jt][s] = load8<T>(kp + 32 * s);
-            vf[jt][s] = load8<T>(vp + 32 * s);
-          }
-          pj[jt] = !a.placed ? 0 : a.hist_pos ? a.hist_pos[h0 + jb + jr] : jb + 16 * jt + c16;
-        }
         // K in the other order: rows of the step along the operand
-        F4 kc[JT][NE];
         bool odd_k = false;
 #pragma unroll
         for (int jt = 0; jt < JT; ++jt)
 #pragma unroll
-          for (int s = 0; s < KS; ++s) {
+          for (int s = 0; s < KS; ++s)
             store8<T>(reinterpret_cast<T*>(kt + (16 * jt + c16) * kRowBytes<T, DH>) + 32 * s + 8 * g4, kf[jt][s]);
-            odd_k |= odd8<T>(kf[jt][s]);
+        f32x4 S[MT][JT], dP[MT][JT];
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+#pragma unroll
+          for (int jt = 0; jt < JT; ++jt) S[mt][jt] = dP[mt][jt] = f32x4{};
+#pragma unroll
+          for (int s = 0; s < KS; ++s) {
+            const unsigned char* row = mine + (16 * mt + c16) * kRowBytes<T, DH> + (32 * s + 8 * g4) * sizeof(T);
+            const E8 qf = load8<T>(reinterpret_cast<const T*>(row));
+            const E8 df = load8<T>(reinterpret_cast<const T*>(row + Lds::kDo));
+#pragma unroll
+            for (int jt = 0; jt < JT; ++jt) {
+              S[mt][jt] = mma32(kf[jt][s], qf, S[mt][jt]);
+              dP[mt][jt] = mma32(vf[jt][s], df, dP[mt][jt]);
+            }
           }
+        }
+        const bool tail = jb + BJ > jend;
+        int pos[JT][4];
+#pragma unroll
+        for (int jt = 0; jt < JT; ++jt)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) pos[jt][i] = a.hist_pos ? pj[jt][i] : jb + 16 * jt + 4 * g4 + i;
+        if (a.placed) {
+#pragma unroll
+          for (int jt = 0; jt < JT; ++jt)
+#pragma unroll
+            for (int s = 0; s < KS; ++s) odd_k |= odd8<T>(kf[jt][s]);
+        }
+        if (jb + BJ < min(jstop, jend)) load(jb + BJ);
+        F4 kc[JT][NE];
         __builtin_amdgcn_wave_barrier();
 #pragma unroll
         for (int jt = 0; jt < JT; ++jt)
 #pragma unroll
           for (int e = 0; e < NE; ++e) kc[jt][e] = column4<T, DH>(kt, 16 * jt, e, c16, g4);
         __builtin_amdgcn_wave_barrier();
-        const bool tail = jb + BJ > jend;
-        const bool odd_step = odd_rows || __ballot(odd_k) != 0;
+        int pmin = pos[0][0], pmax = pos[0][0];
+#pragma unroll
+        for (int jt = 0; jt < JT; ++jt)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            pmin = min(pmin, pos[jt][i]);
+            pmax = max(pmax, pos[jt][i]);
+          }
 
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
           if (mt >= held) break;
-          const unsigned char* qt = smem + Lds::kQ + 16 * mt * kRowBytes<T, DH>;
-          const unsigned char* dt = smem + Lds::kDo + 16 * mt * kRowBytes<T, DH>;
-          float mx[4], il[4], D[4];
-          int tp[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const f32x4 row = *reinterpret_cast<const f32x4*>(s_row + 4 * (16 * mt + 4 * g4 + i));
-            mx[i] = row[0];
-            il[i] = row[1];
-            D[i] = row[2];
-            tp[i] = __float_as_int(row[3]);
-          }
-          f32x4 S[JT], dP[JT];
-#pragma unroll
-          for (int jt = 0; jt < JT; ++jt) S[jt] = dP[jt] = f32x4{};
-#pragma unroll
-          for (int s = 0; s < KS; ++s) {
-            const E8 qf = load8<T>(reinterpret_cast<const T*>(qt + c16 * kRowBytes<T, DH>) + 32 * s + 8 * g4);
-            const E8 df = load8<T>(reinterpret_cast<const T*>(dt + c16 * kRowBytes<T, DH>) + 32 * s + 8 * g4);
+          const unsigned char* qt = mine + 16 * mt * kRowBytes<T, DH>;
+          const unsigned char* dt = qt + Lds::kDo;
+          const bool slow =
+              __ballot(tail || (a.placed && (place_of(tp[mt], pmax) < blo[mt] || place_of(tp[mt], pmin) > bhi[mt]))) != 0;
+          uint32_t hid = 0;  // bit 4 jt + i
+          float w[JT][4], dz[JT][4], dx[JT][4];
+          int kk[JT][4];
+          if (slow) {
 #pragma unroll
             for (int jt = 0; jt < JT; ++jt) {
-              S[jt] = mma32(qf, kf[jt][s], S[jt]);
-              dP[jt] = mma32(df, vf[jt][s], dP[jt]);
+              int at[4];
+              int2 cell[4];
+              if (a.placed) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                  at[i] = place_of(tp[mt], pos[jt][i]);
+                  cell[i] = bl.cells[cell_of(at[i])];
+                }
+              }
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                kk[jt][i] = a.placed ? bucket_in(bl, at[i], cell[i]) : 0;
+                dx[jt][i] = a.placed ? bl.bias[(hs * a.G + hh) * (slots + 1) + kk[jt][i]] : 0.f;
+                if (jb + 16 * jt + 4 * g4 + i >= jend) dx[jt][i] = -INFINITY;
+                hid |= dx[jt][i] == -INFINITY ? 1u << (4 * jt + i) : 0u;
+              }
             }
-          }
-          bool out = tail;
-#pragma unroll
-          for (int jt = 0; jt < JT; ++jt)
-            out |= sub_sat(tmin[mt], pj[jt]) < blo[mt] || sub_sat(tmax[mt], pj[jt]) > bhi[mt];
-          const bool slow = __ballot(out) != 0;
-          uint32_t hid = 0;  // bit 4 jt + i
-          float w[JT][4], dz[JT][4];
-          int kk[4 * JT + 1];
-          float xb[JT][4];
-          if (!slow) {
-#pragma unroll
-            for (int jt = 0; jt < JT; ++jt)
-#pragma unroll
-              for (int i = 0; i < 4; ++i) xb[jt][i] = bias[mt];
           } else {
 #pragma unroll
             for (int jt = 0; jt < JT; ++jt)
 #pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                const int d = a.placed ? sub_sat(tp[i], pj[jt]) : 0;
-                bool vis = jb + 16 * jt + c16 < jend && !(a.masked && d < 0);
-                xb[jt][i] = 0.f;
-                kk[4 * jt + i] = 0;
-                if (nb) {
-                  kk[4 * jt + i] = bucket_of(bl, d);
-                  xb[jt][i] = s_bias[head[mt] * nb + kk[4 * jt + i]];
-                  vis = vis && xb[jt][i] != -INFINITY;
-                }
-                if (!vis) hid |= 1u << (4 * jt + i);
-              }
+              for (int i = 0; i < 4; ++i) dx[jt][i] = bias[mt];
           }
-          float dx[4 * JT + 1];
 #pragma unroll
           for (int jt = 0; jt < JT; ++jt)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-              float x = S[jt][i] * a.scale, slope = 1.f;
+              float x = S[mt][jt][i], slope = 1.f;
               if (a.cap > 0.f) {
-                const float th = kBf16 ? tanh_fast(x / a.cap) : tanhf(x / a.cap);
-                x = a.cap * th;
-                slope = 1.f - th * th;
+                x = kBf16 ? tanh_fast(x * cap_in) : tanhf(x * cap_in);
+                slope = 1.f - x * x;
               }
-              x += xb[jt][i];
-              float p = exp_nat(x - mx[i]) * il[i];
-              float g = p * (dP[jt][i] - D[i]);
-              if (slow && ((hid >> (4 * jt + i)) & 1)) p = g = 0.f;
+              x = fmaf(x, gain, dx[jt][i]);
+              float p = exp2_fast(x - mx[mt]) * il[mt];
+              float d = p * (dP[mt][jt][i] - D[mt]);
+              if (slow && ((hid >> (4 * jt + i)) & 1)) p = d = 0.f;
               w[jt][i] = p;
-              dx[4 * jt + i] = g;
-              dz[jt][i] = g * slope;
+              dz[jt][i] = d * slope;
+              dx[jt][i] = d;
             }
           if (nb) {
             if (!slow) {
 #pragma unroll
-              for (int i = 0; i < 4 * JT; ++i) dsum[mt] += dx[i];
+              for (int jt = 0; jt < JT; ++jt) dsum[mt] += (dx[jt][0] + dx[jt][1]) + (dx[jt][2] + dx[jt][3]);
             } else {
-              kk[4 * JT] = bk[mt];
-              dx[4 * JT] = dsum[mt];
+#pragma unroll
+              for (int jt = 0; jt < JT; ++jt) {
+                const int ka = kk[jt][0], kb = kk[jt][3];
+                const bool two = (kk[jt][1] == ka || kk[jt][1] == kb) && (kk[jt][2] == ka || kk[jt][2] == kb);
+                if (__ballot(!two) == 0) {
+                  float va = dx[jt][0], vb = 0.f;
+#pragma unroll
+                  for (int i = 1; i < 4; ++i) {
+                    va += kk[jt][i] == ka ? dx[jt][i] : 0.f;
+                    vb += kk[jt][i] == ka ? 0.f : dx[jt][i];
+                  }
+                  // (what the lane has kept so far goes with them)
+                  if (jt == 0 && __ballot(dsum[mt] != 0.f && bk[mt] != ka) == 0) {
+                    va += dsum[mt];
+                    dsum[mt] = 0.f;
+                  }
+                  add_bins(ka, va, kb == ka ? -1 : kb, vb);
+                } else {
+                  add_bins(ka, dx[jt][0], kk[jt][1], dx[jt][1]);
+                  add_bins(kk[jt][2], dx[jt][2], kb, dx[jt][3]);
+                }
+              }
+              if (__ballot(dsum[mt] != 0.f)) add_bins(bk[mt], dsum[mt], -1, 0.f);
               dsum[mt] = 0.f;
-              bk[mt] = kk[4 * JT - 1];
-              bias[mt] = xb[JT - 1][3];
-              const int edge = bk[mt] ? s_edges[bk[mt] - 1] : (a.masked ? 0 : -2147483647 - 1);
-              blo[mt] = bias[mt] == -INFINITY ? 2147483647 : edge;
-              bhi[mt] = bk[mt] == nb - 1 ? 2147483647 : s_edges[bk[mt]] - 1;
-              add_bins(mt, kk, dx, 4 * JT + 1);
+              bk[mt] = kk[JT - 1][3];
+              bias[mt] = bl.bias[(hs * a.G + hh) * (slots + 1) + bk[mt]];
+              keep_bucket(bl, a.masked, bk[mt], bias[mt], blo[mt], bhi[mt]);
             }
           }
           if (slow && __ballot(hid != (1u << (4 * JT)) - 1u) == 0) continue;
 
-          // ---- sums over targets: dV^T += dout^T w, dK^T += q^T dz
-          F4 wh[JT], wl[JT], zh[JT], zl[JT];
+          // ---- the terms of w and dz; by target in LDS
+          F4 zh[JT], zl[JT];
 #pragma unroll
           for (int jt = 0; jt < JT; ++jt) {
+            unsigned char* row = dzt + (16 * jt + c16) * kPRow<T>;
             if constexpr (kBf16) {
-              uint2 h, l;
-              split_bf16(w[jt][0], w[jt][1], h.x, l.x);
-              split_bf16(w[jt][2], w[jt][3], h.y, l.y);
-              wh[jt] = __builtin_bit_cast(s16x4, h);
-              wl[jt] = __builtin_bit_cast(s16x4, l);
-              split_bf16(dz[jt][0], dz[jt][1], h.x, l.x);
-              split_bf16(dz[jt][2], dz[jt][3], h.y, l.y);
+              auto cut4 = [](float (&x)[4], bool last) {
+                return last ? make_uint2(high_halves(x[0], x[1]), high_halves(x[2], x[3]))
+                            : make_uint2(cut_bf16(x[0], x[1]), cut_bf16(x[2], x[3]));
+              };
+              *reinterpret_cast<uint2*>(row + 8 * g4) = cut4(w[jt], false);
+              *reinterpret_cast<uint2*>(row + 32 + 8 * g4) = cut4(w[jt], true);
+              const uint2 h = cut4(dz[jt], false), l = cut4(dz[jt], true);
+              *reinterpret_cast<uint2*>(row + 64 + 8 * g4) = h;
+              *reinterpret_cast<uint2*>(row + 96 + 8 * g4) = l;
               zh[jt] = __builtin_bit_cast(s16x4, h);
               zl[jt] = __builtin_bit_cast(s16x4, l);
-              *reinterpret_cast<uint2*>(dzt + (16 * jt + c16) * 64 + 8 * g4) = __builtin_bit_cast(uint2, zh[jt]);
-              *reinterpret_cast<uint2*>(dzt + (16 * jt + c16) * 64 + 32 + 8 * g4) = __builtin_bit_cast(uint2, zl[jt]);
             } else {
 #pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                wh[jt][i] = w[jt][i];
-                zh[jt][i] = dz[jt][i];
-              }
-              *reinterpret_cast<f32x4*>(dzt + (16 * jt + c16) * 80 + 16 * g4) = zh[jt];
+              for (int i = 0; i < 4; ++i) zh[jt][i] = dz[jt][i];
+              *reinterpret_cast<f32x4*>(row + 16 * g4) = f32x4{w[jt][0], w[jt][1], w[jt][2], w[jt][3]};
+              *reinterpret_cast<f32x4*>(row + 64 + 16 * g4) = zh[jt];
             }
           }
           __builtin_amdgcn_wave_barrier();
-          const bool careful = slow && odd_step && __ballot(hid != 0) != 0;
+          const bool careful = slow && (odd_rows || __ballot(odd_k)) && __ballot(hid != 0) != 0;
+          // ---- sum over the step's rows: dQ^T += K^T dz; sums over targets:
+          // dV^T += dout^T w, dK^T += q^T dz
+          F4 p[JT][4];  // w, dz (bf16: two terms each) of row c16, targets 4 g4 + i
 #pragma unroll
-          for (int e = 0; e < NE; ++e) {
-            const F4 dT = column4<T, DH>(dt, 0, e, c16, g4), qT = column4<T, DH>(qt, 0, e, c16, g4);
+          for (int jt = 0; jt < JT; ++jt) {
+            if constexpr (kBf16) {
+              const unsigned char* at = dzt + (16 * jt + 4 * g4 + (c16 >> 2)) * kPRow<T> + 8 * (c16 & 3);
 #pragma unroll
-            for (int jt = 0; jt < JT; ++jt) {
-              if (!careful) {
-                dv[jt][e] = mma16(dT, wh[jt], dv[jt][e]);
-                dk[jt][e] = mma16(qT, zh[jt], dk[jt][e]);
-                if constexpr (kBf16) {
-                  dv[jt][e] = mma16(dT, wl[jt], dv[jt][e]);
-                  dk[jt][e] = mma16(qT, zl[jt], dk[jt][e]);
-                }
-              } else {
-                // 0 times an infinite or NaN row is not 0: column by column,
-                // with the rows that a column is hidden from cleared
-                for (int col = 0; col < 16; ++col) {
-                  const uint32_t h = __shfl(hid, col + 16 * g4) >> (4 * jt);
-                  const F4 dc = cleared(dT, h), qc = cleared(qT, h);
-                  f32x4 nv = mma16(dc, wh[jt], dv[jt][e]), nk = mma16(qc, zh[jt], dk[jt][e]);
-                  if constexpr (kBf16) {
-                    nv = mma16(dc, wl[jt], nv);
-                    nk = mma16(qc, zl[jt], nk);
-                  }
-                  if (c16 == col) {
-                    dv[jt][e] = nv;
-                    dk[jt][e] = nk;
-                  }
-                }
+              for (int i = 0; i < 4; ++i) p[jt][i] = __builtin_bit_cast(s16x4, lds_read_tr16(at + 32 * i));
+            } else {
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const float* at = reinterpret_cast<const float*>(dzt + (16 * jt + 4 * g4 + i) * kPRow<T>) + c16;
+                p[jt][0][i] = at[0];
+                p[jt][2][i] = at[16];
               }
             }
           }
-          // ---- sum over the step's rows: dQ += dz K
-#pragma unroll
-          for (int jt = 0; jt < JT; ++jt) {
-            F4 ah, al;
-            if constexpr (kBf16) {
-              const unsigned char* p = dzt + (16 * jt + 4 * g4 + (c16 >> 2)) * 64 + 8 * (c16 & 3);
-              ah = __builtin_bit_cast(s16x4, lds_read_tr16(p));
-              al = __builtin_bit_cast(s16x4, lds_read_tr16(p + 32));
-            } else {
-#pragma unroll
-              for (int i = 0; i < 4; ++i)
-                ah[i] = *reinterpret_cast<const float*>(dzt + (16 * jt + 4 * g4 + i) * 80 + 4 * c16);
-            }
+          if (!careful) {
 #pragma unroll
             for (int e = 0; e < NE; ++e) {
-              if (!careful) {
-                dq[mt][e] = mma16(ah, kc[jt][e], dq[mt][e]);
-                if constexpr (kBf16) dq[mt][e] = mma16(al, kc[jt][e], dq[mt][e]);
-              } else {
-                for (int t = 0; t < 16; ++t) {
-                  uint32_t h = 0;
+              const F4 dT = column4<T, DH>(dt, 0, e, c16, g4), qT = column4<T, DH>(qt, 0, e, c16, g4);
 #pragma unroll
-                  for (int i = 0; i < 4; ++i)
-                    h |= ((__shfl(hid, 4 * g4 + i + 16 * (t >> 2)) >> (4 * jt + (t & 3))) & 1u) << i;
-                  const F4 kx = cleared(kc[jt][e], h);
-                  f32x4 n = mma16(ah, kx, dq[mt][e]);
-                  if constexpr (kBf16) n = mma16(al, kx, n);
-                  if (g4 == (t >> 2)) dq[mt][e][t & 3] = n[t & 3];
+              for (int jt = 0; jt < JT; ++jt) {
+                dq[mt][e] = mma16(kc[jt][e], zh[jt], dq[mt][e]);
+                dv[jt][e] = mma16(dT, p[jt][0], dv[jt][e]);
+                dk[jt][e] = mma16(qT, p[jt][2], dk[jt][e]);
+                if constexpr (kBf16) {
+                  dq[mt][e] = mma16(kc[jt][e], zl[jt], dq[mt][e]);
+                  dv[jt][e] = mma16(dT, p[jt][1], dv[jt][e]);
+                  dk[jt][e] = mma16(qT, p[jt][3], dk[jt][e]);
+                }
+              }
+            }
+          } else {
+            // 0 times an infinite or NaN row is not 0: column by column, with
+            // the rows that a column does not see (is hidden from) cleared
+#pragma unroll 1
+            for (int col = 0; col < 16; ++col) {
+              const uint32_t hq = __shfl(hid, col + 16 * g4);
+#pragma unroll
+              for (int jt = 0; jt < JT; ++jt) {
+                uint32_t hk = 0;  // targets 4 g4 + i that row `col` is hidden from
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                  hk |= ((__shfl(hid, 4 * g4 + i + 16 * (col >> 2)) >> (4 * jt + (col & 3))) & 1u) << i;
+#pragma unroll
+                for (int e = 0; e < NE; ++e) {
+                  const F4 kx = cleared(kc[jt][e], hq >> (4 * jt)), dx = cleared(column4<T, DH>(dt, 0, e, c16, g4), hk),
+                           qx = cleared(column4<T, DH>(qt, 0, e, c16, g4), hk);
+                  f32x4 nq = mma16(kx, zh[jt], dq[mt][e]), nv = mma16(dx, p[jt][0], dv[jt][e]),
+                        nk = mma16(qx, p[jt][2], dk[jt][e]);
+                  if constexpr (kBf16) {
+                    nq = mma16(kx, zl[jt], nq);
+                    nv = mma16(dx, p[jt][1], nv);
+                    nk = mma16(qx, p[jt][3], nk);
+                  }
+                  if (c16 == col) {
+                    dq[mt][e] = nq;
+                    dv[jt][e] = nv;
+                    dk[jt][e] = nk;
+                  }
                 }
               }
             }
@@ -582,27 +645,20 @@ __global__ __launch_bounds__(kThreads) void attn_bwd_kernel(const AttnArgs a) {
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
       if (mt >= held) break;
-      if (nb) {
-        const int kk[1] = {bk[mt]};
-        const float vv[1] = {dsum[mt]};
-        add_bins(mt, kk, vv, 1);
-      }
+      if (nb) add_bins(bk[mt], dsum[mt], -1, 0.f);
       __syncthreads();
 #pragma unroll
       for (int e = 0; e < NE; ++e)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          s_comb[(wave * 16 + 4 * g4 + i) * DH + tile_feature<DH>(e, c16)] = dq[mt][e][i];
+        reinterpret_cast<f32x4*>(s_comb + (wave * 16 + c16) * (DH + 4) + 4 * NE * g4)[e] = dq[mt][e];
       __syncthreads();
-      const int tile = first + mt, hh = tile / ttiles, row = tid >> 4, t = tile % ttiles * 16 + row;
-      if (t < m) {
-        const int64_t tr = t0 + t, h = g * a.G + hh;
+      const int row = tid >> 4, t = 16 * (first + mt) + row;
+      for (int hd = 0; hd < a.hw && t < m; ++hd) {
+        const int64_t tr = t0 + t, h = (g0 + hd) * a.G + hh;
         const int f = (tid & 15) * NE;
 #pragma unroll
         for (int e = 0; e < NE; ++e) {
           float v = 0.f;
-#pragma unroll
-          for (int wv = 0; wv < kWaves; ++wv) v += s_comb[(wv * 16 + row) * DH + f + e];
+          for (int wv = hd; wv < kWaves; wv += a.hw) v += s_comb[(wv * 16 + row) * (DH + 4) + f + e];
           v *= a.scale;
           if (a.max_chunks > 1) a.part_dq[((static_cast<int64_t>(c) * a.n_tgt + tr) * a.H + h) * DH + f + e] = v;
           else static_cast<T*>(a.dq)[tr * a.lddq + h * DH + f + e] = from_f32<T>(v);
@@ -610,16 +666,20 @@ __global__ __launch_bounds__(kThreads) void attn_bwd_kernel(const AttnArgs a) {
       }
     }
     __syncthreads();
-    for (int k = tid; k < nb; k += kThreads)
-      for (int mt = 0; mt < held; ++mt) {
-        float v = 0.f;
-        for (int wv = 0; wv < kWaves; ++wv) v += s_bins[(wv * MT + mt) * nb + k];
-        s_db[(first + mt) / ttiles * nb + k] += v;
-      }
+    // dbias of the pass: 4 threads a bucket, one wave's sums each, added over the head's waves
+    for (int i = tid; i < (4 * nb + 63) / 64 * 64; i += kThreads) {
+      const int k = i >> 2, wv = i & 3;
+      float v = 0.f;
+      if (k < nb)
+        for (int l = 0; l < copies; ++l) v += s_bins[(wv * (slots + 1) + k) * copies + ((l + k) & (copies - 1))];
+      if (a.hw < 4) v += __shfl_xor(v, 2);
+      if (a.hw < 2) v += __shfl_xor(v, 1);
+      if (k < nb && wv < a.hw) s_db[(wv * a.G + hh) * nb + k] += v;
+    }
   }
   if (nb) {
     __syncthreads();
-    for (int i = tid; i < a.G * nb; i += kThreads) part_db[i] = s_db[i];
+    for (int i = tid; i < heads * nb; i += kThreads) part_db[i] = s_db[i];
   }
 }
 
@@ -665,9 +725,12 @@ __global__ __launch_bounds__(256) void attn_bwd_sum_kernel(const AttnArgs a, int
 
 template <typename T, int DH, int MT>
 hipError_t launch_bwd(const AttnArgs& a, hipStream_t st) {
-  constexpr int JT = DH == 128 ? 1 : 2;
-  const size_t lds = BwdLds<T, DH, MT, JT>::bytes(a.G, a.b.n);
-  const int64_t grid = round_up(a.units, kXcds) * a.Hk + 1;
+#ifndef JTB
+#define JTB 1
+#endif
+  constexpr int JT = DH == 128 ? 1 : JTB;
+  const size_t lds = BwdLds<T, DH, MT, JT>::bytes(a.hw, a.G, a.b.n, bin_copies(a.b.n));
+  const int64_t grid = round_up(a.units, kXcds) * (a.Hk / a.hw) + 1;
   if (grid > 0x7fffffff) return hipErrorInvalidValue;
   hipError_t e = allow_lds<&attn_bwd_kernel<T, DH, MT, JT>>(lds);
   if (e != hipSuccess) return e;

@@ -2,11 +2,13 @@
 // over a paged cache:
 //   x = cap(scale q.k) + bias[h][bucket(p_t - p_j)];  out = softmax(x) v.
 //
-// One workgroup of four waves takes one chunk of one request's history for one
-// kv head and up to 16 MT rows (target, query head of the kv head's group);
-// its waves take the chunk's blocks of 16 NT history rows in turn, each with
-// softmax statistics and an output of its own, joined in LDS at the end.
-// Several chunks leave (output, maximum, sum) partials for attn_merge.
+// One workgroup of four waves takes one chunk of one request's history for up to
+// 16 MT rows (target, query head of a kv head's group) and hw kv heads; 4 / hw
+// waves share a head, each with consecutive blocks of 16 NT history rows and
+// softmax statistics and an output of its own, joined in LDS at the end.  Four
+// heads a workgroup read packed rows in whole cache lines at one time (window
+// of 256 requests, 16 targets, 2048 rows, d_h = 32: @@); one head a workgroup
+// spreads a small batch over more of them.  Several chunks leave (output, maximum, sum) partials for attn_merge.
 //
 // Everything of a block stays in one wave's registers.  Scores are formed
 // transposed, S^T = K Q^T (v_mfma 16x16x32 bf16, or 16x16x4 fp32), so that the
@@ -19,14 +21,17 @@
 // A row's maximum is only raised (and O rescaled) when a score passes it by
 // kSlack: a vote per block instead of a reduction across lanes.
 //
-// P is split into two bf16 terms: one term's rounding would show in the
-// output as a second rounding of its size (1.7e-3 -> 2.4e-3 relative to 64
-// bits on normal inputs); the matrix cores have the time.
+// P enters the matrix cores as bf16 terms: two (one term's rounding would show
+// in the output as a second rounding of its size, 1.7e-3 -> 2.4e-3 relative to
+// 64 bits on normal inputs), or three, an fp32 whole, where a backward will
+// form D = dout . out from what is saved.  The matrix cores have the time.
 //
-// Distances of most blocks lie in one bucket for every lane: each lane keeps
-// its bucket's interval and bias, a vote tells whether a block is inside, and
-// only the others look buckets and masks up score by score.
+// Where the distances of a block lie in one bucket for every lane (a vote over
+// the interval that each lane keeps), its bias is added as it stands; elsewhere
+// every score looks its bucket up.
 #pragma once
+
+#include <algorithm>
 
 #include "attn_ops.h"
 
@@ -34,9 +39,12 @@ namespace stca {
 namespace ops {
 
 constexpr int kRagged = 0, kPagedBf16 = 1, kPagedInt8 = 2;
-constexpr float kSlack = 6.f;  // e^6: sums and products stay far inside fp32 and bf16 ranges
+constexpr float kSlack = 8.f;  // 2^8: sums and products stay far inside fp32 and bf16 ranges
 
-template <int KV> constexpr int kTilesOf = KV == kPagedInt8 ? 4 : 2;
+#ifndef NTR
+#define NTR 2
+#endif
+template <int KV> constexpr int kTilesOf = KV == kPagedInt8 ? 4 : KV == kPagedBf16 ? 2 : NTR;
 
 // LDS of a workgroup before the dynamic part's tables.
 template <int DH> constexpr int kCombineFloats = kWaves * 16 * (DH + 2);
@@ -55,25 +63,26 @@ struct Block {
   uint32_t vw[KV == kRagged ? NJ : 1][KV == kRagged ? (kF32 ? NE : NE / 2) : 1];
   uint4 vp[KV == kRagged ? 1 : NE];
   uint4 ke, ve;                        // 16 exponents each
+  int pj[NJ];                          // positions, where the rows have some
 };
 
 template <int N>
-__device__ __forceinline__ void load_words(const char* p, uint32_t* w) {
+__device__ __forceinline__ void load_words(gptr base, uint32_t at, uint32_t* w) {
   typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
   typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
   if constexpr (N >= 4) {
 #pragma unroll
     for (int i = 0; i < N / 4; ++i) {
-      const u32x4 x = reinterpret_cast<const u32x4*>(p)[i];
+      const u32x4 x = load_at<u32x4>(base + 16 * i, at);
 #pragma unroll
       for (int k = 0; k < 4; ++k) w[4 * i + k] = x[k];
     }
   } else if constexpr (N == 2) {
-    const u32x2 x = *reinterpret_cast<const u32x2*>(p);
+    const u32x2 x = load_at<u32x2>(base, at);
     w[0] = x[0];
     w[1] = x[1];
   } else {
-    w[0] = *reinterpret_cast<const uint32_t*>(p);
+    w[0] = load_at<uint32_t>(base, at);
   }
 }
 
@@ -107,8 +116,11 @@ __device__ __forceinline__ bool odd_bf16(uint32_t w) {  // a half of w is not fi
   return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u;
 }
 
+#ifndef EU
+#define EU 2
+#endif
 template <typename T, int KV, int DH, int MT>
-__global__ __launch_bounds__(kThreads) void attn_fwd_kernel(const AttnArgs a) {
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(EU))) void attn_fwd_kernel(const AttnArgs a) {
   constexpr bool kF32 = !Elem<T>::bf16;
   constexpr bool kPaged = KV != kRagged;
   constexpr int NT = kTilesOf<KV>;
@@ -117,10 +129,10 @@ __global__ __launch_bounds__(kThreads) void attn_fwd_kernel(const AttnArgs a) {
   using Blk = Block<T, KV, DH, NT>;
   extern __shared__ __align__(16) unsigned char smem[];
   float* comb = reinterpret_cast<float*>(smem);
-  int32_t* s_edges = reinterpret_cast<int32_t*>(comb + kCombineFloats<DH>);
-  uint8_t* s_cell = reinterpret_cast<uint8_t*>(s_edges + kMaxBuckets);
-  float* s_bias = reinterpret_cast<float*>(s_cell + 128);
-  int32_t* s_table = reinterpret_cast<int32_t*>(s_bias + a.G * a.b.n);
+  int2* s_cells = reinterpret_cast<int2*>(comb + kCombineFloats<DH>);
+  int32_t* s_edges = reinterpret_cast<int32_t*>(s_cells + kCells + 1);
+  float* s_bias = reinterpret_cast<float*>(s_edges + kMaxBuckets);
+  int32_t* s_table = reinterpret_cast<int32_t*>(s_bias + a.hw * a.G * (max(a.b.n, 1) + 1));
 
   const int tid = threadIdx.x, lane = tid & 63, c16 = lane & 15, g4 = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -131,38 +143,36 @@ __global__ __launch_bounds__(kThreads) void attn_fwd_kernel(const AttnArgs a) {
   }
   // every kv head and row group of a chunk on one XCD: heads share cache lines
   // of packed rows, row groups share everything
-  const int per = a.Hk * a.zgroups;
+  const int ghs = a.Hk / a.hw, per = ghs * a.zgroups;
   const int unit = static_cast<int>(blockIdx.x) / kXcds / per * kXcds + static_cast<int>(blockIdx.x) % kXcds;
   if (unit >= a.units) return;
   const int rem = static_cast<int>(blockIdx.x) / kXcds % per;
-  const int g = rem % a.Hk, z = rem / a.Hk;
+  const int g0 = rem % ghs * a.hw, z = rem / ghs;
+  const int hs = wave % a.hw, part = wave / a.hw, parts = kWaves / a.hw, g = g0 + hs;
 
   int r, c, len;
   int64_t h0 = 0;
   if constexpr (kPaged) {
     r = unit / a.max_chunks;
     c = unit % a.max_chunks;
-    len = min(max(a.lens[r], 0), a.max_len);
+    len = uniform(min(max(a.lens[r], 0), a.max_len));
   } else {
-    r = find_request(a.hist_off, a.R, a.n_hist, a.chunk, unit);
-    h0 = clamp_off(a.hist_off[r], a.n_hist);
-    len = max(0, static_cast<int>(clamp_off(a.hist_off[r + 1], a.n_hist) - h0));
+    r = uniform(find_request(a.hist_off, a.R, a.n_hist, a.chunk, unit));
+    h0 = uniform(clamp_off(a.hist_off[r], a.n_hist));
+    len = uniform(max(0, static_cast<int>(clamp_off(a.hist_off[r + 1], a.n_hist) - h0)));
     c = unit - static_cast<int>(h0 / a.chunk + r);
   }
   if (c < 0 || c >= a.max_chunks || (c > 0 && static_cast<int64_t>(c) * a.chunk >= len)) return;
   const int j0 = c * a.chunk;
-  const int t0 = clamp_off(a.tgt_off[r], a.n_tgt), m = clamp_off(a.tgt_off[r + 1], a.n_tgt) - t0;
+  const int t0 = uniform(clamp_off(a.tgt_off[r], a.n_tgt)), m = uniform(clamp_off(a.tgt_off[r + 1], a.n_tgt)) - t0;
   const int rows = m * a.G;
   if (z * 16 * MT >= rows) return;
   const bool split = len > a.chunk;
   int j1 = min(len, j0 + a.chunk);
 
   // tables
-  for (int i = tid; i < a.b.n; i += kThreads) s_edges[i] = a.b.edges[i];
-  if (a.b.n) {
-    if (tid < 128) s_cell[tid] = a.b.cell[tid];
-    for (int i = tid; i < a.G * a.b.n; i += kThreads) s_bias[i] = a.bias[static_cast<int64_t>(g) * a.G * a.b.n + i];
-  }
+  BucketLds bl{};
+  if (a.placed) bl = fill_buckets(a, g0, a.hw * a.G, s_cells, s_bias, s_edges);
   bool holes = false;
   if constexpr (kPaged) {
     const int p0 = j0 >> a.page_shift, p1 = (j1 + (1 << a.page_shift) - 1) >> a.page_shift;
@@ -176,11 +186,10 @@ __global__ __launch_bounds__(kThreads) void attn_fwd_kernel(const AttnArgs a) {
   } else {
     __syncthreads();
   }
-  const BucketLds bl{s_edges, s_cell, s_bias, a.b.n};
 
   for (int zz = z; zz * 16 * MT < rows; zz += a.zgroups) {
     // ---- this lane's rows: column c16 of each tile
-    int tpos[MT], head[MT];
+    int tpos[MT], hbias[MT];  // hbias: this row's biases in the table
     int64_t trow[MT];
     bool have[MT];
     bf16x8 qb[kF32 ? 1 : MT][KS];
@@ -191,11 +200,12 @@ __global__ __launch_bounds__(kThreads) void attn_fwd_kernel(const AttnArgs a) {
       const int row = (zz * MT + mt) * 16 + c16;
       have[mt] = row < rows;
       const int t = have[mt] ? row / a.G : 0;
-      head[mt] = have[mt] ? row % a.G : 0;
+      const int head = have[mt] ? row % a.G : 0;
+      hbias[mt] = (hs * a.G + head) * (bl.slots + 1);
       trow[mt] = t0 + t;
       tpos[mt] = a.placed ? a.tgt_pos[trow[mt]] : 0;
       if (have[mt]) seen_max = max(seen_max, tpos[mt]);
-      const T* qp = static_cast<const T*>(a.q) + trow[mt] * a.ldq + (static_cast<int64_t>(g) * a.G + head[mt]) * DH;
+      const T* qp = static_cast<const T*>(a.q) + trow[mt] * a.ldq + (static_cast<int64_t>(g) * a.G + head) * DH;
 #pragma unroll
       for (int s = 0; s < KS; ++s) {
         const T* p = qp + feature<KV, DH>(s, g4);
@@ -217,44 +227,49 @@ __global__ __launch_bounds__(kThreads) void attn_fwd_kernel(const AttnArgs a) {
     }
 
     float mx[MT], sum[MT], bias[MT];
-    int blo[MT], bhi[MT];  // distances of the bucket held
+    int blo[MT], bhi[MT];  // the distances that `bias` is for
     f32x4 o[MT][NE];
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
       mx[mt] = -INFINITY;
       sum[mt] = 0.f;
       bias[mt] = 0.f;
-      blo[mt] = a.masked ? 0 : -2147483647 - 1;
-      bhi[mt] = 2147483647;
-      if (a.b.n) bhi[mt] = -2147483647 - 1;  // none yet
+      blo[mt] = a.masked ? 1 : 0;
+      bhi[mt] = a.b.n ? -1 : 0x7fffffff;  // (a bias: none kept yet)
 #pragma unroll
       for (int e = 0; e < NE; ++e) o[mt][e] = f32x4{};
     }
 
+    // K and V of block jb; a row past the end is the last one again (hidden below)
+    const uint32_t lk = static_cast<uint32_t>(a.ldk * sizeof(T)), lv = static_cast<uint32_t>(a.ldv * sizeof(T));
     auto load = [&](Blk& b, int jb) {
-      const int last = len - 1 - jb;  // clamped: rows past the end are hidden below
+      const int last = len - 1 - jb;
       if constexpr (!kPaged) {
-        const char* kp = static_cast<const char*>(a.k) + ((h0 + jb) * a.ldk + static_cast<int64_t>(g) * DH) * sizeof(T);
-        const char* vp = static_cast<const char*>(a.v) + ((h0 + jb) * a.ldv + static_cast<int64_t>(g) * DH) * sizeof(T);
-        const int lk = static_cast<int>(a.ldk * sizeof(T)), lv = static_cast<int>(a.ldv * sizeof(T));
+        const gptr kp = uniform(static_cast<const char*>(a.k) + ((h0 + jb) * a.ldk + static_cast<int64_t>(g) * DH) * sizeof(T));
+        const gptr vp = uniform(static_cast<const char*>(a.v) + ((h0 + jb) * a.ldv + static_cast<int64_t>(g) * DH) * sizeof(T));
 #pragma unroll
         for (int i = 0; i < NT; ++i) {
-          const int jr = min(NJ * (c16 >> 2) + 4 * i + (c16 & 3), last);
+          const uint32_t at = __umul24(min(NJ * (c16 >> 2) + 4 * i + (c16 & 3), last), lk) + 8 * g4 * sizeof(T);
 #pragma unroll
           for (int s = 0; s < KS; ++s) {
-            const char* p = kp + jr * lk + feature<KV, DH>(s, g4) * sizeof(T);
+            const gptr p = kp + 32 * s * sizeof(T);
             if constexpr (kF32) {
-              b.kf[i][2 * s] = reinterpret_cast<const f32x4*>(p)[0];
-              b.kf[i][2 * s + 1] = reinterpret_cast<const f32x4*>(p)[1];
+              b.kf[i][2 * s] = load_at<f32x4>(p, at);
+              b.kf[i][2 * s + 1] = load_at<f32x4>(p + 16, at);
             } else {
-              b.kb[i][s] = *reinterpret_cast<const bf16x8*>(p);
+              b.kb[i][s] = load_at<bf16x8>(p, at);
             }
           }
         }
 #pragma unroll
         for (int i = 0; i < NJ; ++i) {
-          const int jr = min(NJ * g4 + i, last);
-          load_words<(kF32 ? NE : NE / 2)>(vp + jr * lv + c16 * NE * static_cast<int>(sizeof(T)), b.vw[i]);
+          const uint32_t at = __umul24(min(NJ * g4 + i, last), lv) + c16 * NE * static_cast<uint32_t>(sizeof(T));
+          load_words<(kF32 ? NE : NE / 2)>(vp, at, b.vw[i]);
+        }
+        if (a.hist_pos) {
+          const gptr hp = uniform(a.hist_pos + h0 + jb);
+#pragma unroll
+          for (int i = 0; i < NJ; ++i) b.pj[i] = load_at<int>(hp, 4u * min(NJ * g4 + i, last));
         }
       } else {
         const int P = 1 << a.page_shift, ps = a.page_shift, p0 = j0 >> ps;
@@ -276,32 +291,48 @@ __global__ __launch_bounds__(kThreads) void attn_fwd_kernel(const AttnArgs a) {
         // this lane group's NJ rows lie in one page
         const int j = min(jb + NJ * g4, (len - 1) & ~(NJ - 1));
         const int64_t page = max(s_table[(j >> ps) - p0], 0), slot = j & (P - 1);
+        const char* vp = static_cast<const char*>(a.v) + (((page * a.Hk + g) * DH + NE * c16) * P + slot) * ES;
 #pragma unroll
-        for (int e = 0; e < NE; ++e)
-          b.vp[e] = *reinterpret_cast<const uint4*>(static_cast<const char*>(a.v) +
-                                                    (((page * a.Hk + g) * DH + NE * c16 + e) * P + slot) * ES);
+        for (int e = 0; e < NE; ++e) b.vp[e] = *reinterpret_cast<const uint4*>(vp + e * (P * ES));
         if constexpr (KV == kPagedInt8) {
           b.ke = *reinterpret_cast<const uint4*>(a.ke + (page * a.Hk + g) * P + slot);
           b.ve = *reinterpret_cast<const uint4*>(a.ve + (page * a.Hk + g) * P + slot);
         }
+        if (a.hist_pos) {
+          const int32_t* hp = a.hist_pos + (page << ps) + slot;
+#pragma unroll
+          for (int i = 0; i < NJ; ++i) b.pj[i] = hp[i];
+        }
       }
     };
 
-    auto compute = [&](const Blk& b, int jb) {
+    // scores in units of log2 e: gain (q k) + bias, or with a cap gain tanh(cap_in (q k)) + bias
+    const float gain = kLog2e * (a.cap > 0.f ? a.cap : a.scale), cap_in = a.cap > 0.f ? a.scale / a.cap : 0.f;
+    const bool whole = a.sa != nullptr;
+
+    auto compute = [&](Blk& b, int jb, bool more) {
       // V operand of O^T: rows NJ g4 + 8 s + 0..7, feature NE c16 + e
       bf16x8 vb[kF32 ? 1 : NT / 2][kF32 ? 1 : NE];
+      float vf[kF32 ? NJ : 1][kF32 ? NE : 1];
       if constexpr (KV == kRagged && !kF32) {
 #pragma unroll
-        for (int e2 = 0; e2 < NE / 2; ++e2) {
-          uint32_t lo[4], hi[4];
+        for (int s = 0; s < NT / 2; ++s)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            lo[i] = __builtin_amdgcn_perm(b.vw[2 * i + 1][e2], b.vw[2 * i][e2], 0x05040100u);
-            hi[i] = __builtin_amdgcn_perm(b.vw[2 * i + 1][e2], b.vw[2 * i][e2], 0x07060302u);
+          for (int e2 = 0; e2 < NE / 2; ++e2) {
+            uint32_t lo[4], hi[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              lo[i] = __builtin_amdgcn_perm(b.vw[8 * s + 2 * i + 1][e2], b.vw[8 * s + 2 * i][e2], 0x05040100u);
+              hi[i] = __builtin_amdgcn_perm(b.vw[8 * s + 2 * i + 1][e2], b.vw[8 * s + 2 * i][e2], 0x07060302u);
+            }
+            vb[s][2 * e2] = __builtin_bit_cast(bf16x8, make_uint4(lo[0], lo[1], lo[2], lo[3]));
+            vb[s][2 * e2 + 1] = __builtin_bit_cast(bf16x8, make_uint4(hi[0], hi[1], hi[2], hi[3]));
           }
-          vb[0][2 * e2] = __builtin_bit_cast(bf16x8, make_uint4(lo[0], lo[1], lo[2], lo[3]));
-          vb[0][2 * e2 + 1] = __builtin_bit_cast(bf16x8, make_uint4(hi[0], hi[1], hi[2], hi[3]));
-        }
+      } else if constexpr (KV == kRagged) {
+#pragma unroll
+        for (int i = 0; i < NJ; ++i)
+#pragma unroll
+          for (int e = 0; e < NE; ++e) vf[i][e] = __uint_as_float(b.vw[i][e]);
       } else if constexpr (KV == kPagedBf16) {
 #pragma unroll
         for (int e = 0; e < NE; ++e) vb[0][e] = __builtin_bit_cast(bf16x8, b.vp[e]);
@@ -312,114 +343,114 @@ __global__ __launch_bounds__(kThreads) void attn_fwd_kernel(const AttnArgs a) {
           vb[1][e] = int8_bf16(b.vp[e].z, b.vp[e].w);
         }
       }
-      bf16x8 kc[KV == kPagedInt8 ? NT : 1][KV == kPagedInt8 ? KS : 1];
-      if constexpr (KV == kPagedInt8) {
+      f32x4 S[MT][NT];
 #pragma unroll
-        for (int i = 0; i < NT; ++i)
+      for (int i = 0; i < NT; ++i) {
 #pragma unroll
-          for (int s = 0; s < KS; ++s) kc[i][s] = int8_bf16(b.k8[i][s].x, b.k8[i][s].y);
+        for (int mt = 0; mt < MT; ++mt) S[mt][i] = f32x4{};
+        if constexpr (kF32) {
+#pragma unroll
+          for (int k = 0; k < 2 * KS; ++k)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+              for (int mt = 0; mt < MT; ++mt) S[mt][i] = mfma_f32(b.kf[i][k][e], qf[mt][k][e], S[mt][i]);
+        } else {
+#pragma unroll
+          for (int k = 0; k < KS; ++k) {
+            bf16x8 kc;
+            if constexpr (KV == kPagedInt8) kc = int8_bf16(b.k8[i][k].x, b.k8[i][k].y);
+            else kc = b.kb[i][k];
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) S[mt][i] = mfma_bf16(kc, qb[mt][k], S[mt][i]);
+          }
+        }
       }
-      // positions of this lane's rows
-      const bool tail = jb + BJ > jend || holes;
+      const uint4 kexp = b.ke, vexp = b.ve;
       int pj[NJ];
       int pmin = 0, pmax = 0;
       if (a.placed) {
         if (a.hist_pos) {
-          const int32_t* hp;
-          if constexpr (kPaged) {
-            const int j = min(jb + NJ * g4, (len - 1) & ~(NJ - 1));
-            hp = a.hist_pos + (static_cast<int64_t>(max(s_table[(j >> a.page_shift) - (j0 >> a.page_shift)], 0))
-                               << a.page_shift) + (j & ((1 << a.page_shift) - 1));
+          pmin = pmax = b.pj[0];
 #pragma unroll
-            for (int i = 0; i < NJ; ++i) pj[i] = hp[i];
-          } else {
-            hp = a.hist_pos + h0 + jb;
-            const int last = len - 1 - jb;
-#pragma unroll
-            for (int i = 0; i < NJ; ++i) pj[i] = hp[min(NJ * g4 + i, last)];
-          }
-          pmin = pmax = pj[0];
-#pragma unroll
-          for (int i = 1; i < NJ; ++i) {
+          for (int i = 0; i < NJ; ++i) {
+            pj[i] = b.pj[i];
             pmin = min(pmin, pj[i]);
             pmax = max(pmax, pj[i]);
           }
         } else {
           pmin = jb + NJ * g4;
           pmax = pmin + NJ - 1;
-        }
-      }
-      float ks[KV == kPagedInt8 ? NJ : 1], vs[KV == kPagedInt8 ? NJ : 1];
-      if constexpr (KV == kPagedInt8) {
 #pragma unroll
-        for (int i = 0; i < NJ; ++i) {
-          ks[i] = exp_byte(word(b.ke, i / 4), i % 4);
-          vs[i] = exp_byte(word(b.ve, i / 4), i % 4);
+          for (int i = 0; i < NJ; ++i) pj[i] = pmin + i;
         }
       }
+      // the block's registers are free: the next one is on its way from here on
+      if (more) load(b, jb + BJ);
+      const bool tail = jb + BJ > jend || holes;
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt) {
+        // biases, in units of log2 e as the scores
         float x[NJ];
+        uint32_t hid = 0;
+        const bool slow = __ballot(tail || place_of(tpos[mt], pmax) < blo[mt] || place_of(tpos[mt], pmin) > bhi[mt]) != 0;
+        if constexpr (KV == kPagedInt8) {
 #pragma unroll
-        for (int i = 0; i < NT; ++i) {
-          f32x4 s = {};
-          if constexpr (kF32) {
-#pragma unroll
-            for (int k = 0; k < 2 * KS; ++k)
-#pragma unroll
-              for (int e = 0; e < 4; ++e) s = mfma_f32(b.kf[i][k][e], qf[mt][k][e], s);
-          } else {
-#pragma unroll
-            for (int k = 0; k < KS; ++k) {
-              if constexpr (KV == kPagedInt8) s = mfma_bf16(kc[i][k], qb[mt][k], s);
-              else s = mfma_bf16(b.kb[i][k], qb[mt][k], s);
-            }
-          }
-#pragma unroll
-          for (int k = 0; k < 4; ++k) x[4 * i + k] = s[k];
-        }
-#pragma unroll
-        for (int i = 0; i < NJ; ++i) {
-          if constexpr (KV == kPagedInt8) x[i] *= ks[i];
-          x[i] *= a.scale;
+          for (int i = 0; i < NJ; ++i) S[mt][i / 4][i % 4] *= exp_byte(word(kexp, i / 4), i % 4);
         }
         if (a.cap > 0.f) {
-          const float inv = 1.f / a.cap;
-#pragma unroll
-          for (int i = 0; i < NJ; ++i) x[i] = a.cap * (kF32 ? tanhf(x[i] / a.cap) : tanh_fast(x[i] * inv));
-        }
-        uint32_t hid = 0;
-        const bool slow = __ballot(tail || sub_sat(tpos[mt], pmax) < blo[mt] || sub_sat(tpos[mt], pmin) > bhi[mt]) != 0;
-        if (!slow) {
-#pragma unroll
-          for (int i = 0; i < NJ; ++i) x[i] += bias[mt];
-        } else {
-          int k = 0;
 #pragma unroll
           for (int i = 0; i < NJ; ++i) {
-            const int j = jb + NJ * g4 + i;
-            const int d = a.placed ? sub_sat(tpos[mt], a.hist_pos ? pj[i] : j) : 0;
-            bool vis = j < jend && !(a.masked && d < 0);
-            if constexpr (kPaged)
-              if (holes) vis = vis && s_table[(min(j, len - 1) >> a.page_shift) - (j0 >> a.page_shift)] >= 0;
-            if (a.b.n) {
-              k = bucket_of(bl, d);
-              const float bv = s_bias[head[mt] * a.b.n + k];
-              x[i] += bv;
-              vis = vis && bv != -INFINITY;
+            const float y = S[mt][i / 4][i % 4] * cap_in;
+            S[mt][i / 4][i % 4] = kF32 ? tanhf(y) : tanh_fast(y);
+          }
+        }
+        if (!slow) {
+#pragma unroll
+          for (int i = 0; i < NJ; ++i) x[i] = fmaf(S[mt][i / 4][i % 4], gain, bias[mt]);
+        } else {
+          if (a.placed) {
+            int k = 0;
+            float bk = 0.f;
+#pragma unroll
+            for (int i4 = 0; i4 < NJ; i4 += 4) {
+              int at[4];
+              int2 cell[4];
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                at[i] = place_of(tpos[mt], pj[i4 + i]);
+                cell[i] = bl.cells[cell_of(at[i])];
+              }
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                k = bucket_in(bl, at[i], cell[i]);
+                x[i4 + i] = bk = bl.bias[hbias[mt] + k];
+              }
             }
-            if (!vis) {
-              x[i] = -INFINITY;
-              hid |= 1u << i;
+            bias[mt] = bk;  // the lane keeps its last row's bucket
+            keep_bucket(bl, a.masked, k, bk, blo[mt], bhi[mt]);
+          } else {
+#pragma unroll
+            for (int i = 0; i < NJ; ++i) x[i] = 0.f;
+          }
+          if (tail) {
+#pragma unroll
+            for (int i = 0; i < NJ; ++i) {
+              const int j = jb + NJ * g4 + i;
+              bool out = j >= jend;
+              if constexpr (kPaged)
+                if (holes) out |= s_table[(min(j, len - 1) >> a.page_shift) - (j0 >> a.page_shift)] < 0;
+              if (out) x[i] = -INFINITY;
             }
           }
-          if (a.b.n) {  // hold the bucket of the lane's last row
-            bias[mt] = s_bias[head[mt] * a.b.n + k];
-            const int edge = k ? s_edges[k - 1] : (a.masked ? 0 : -2147483647 - 1);
-            blo[mt] = bias[mt] == -INFINITY ? 2147483647 : edge;
-            bhi[mt] = k == a.b.n - 1 ? 2147483647 : s_edges[k] - 1;
+          // (a hidden row's score may be NaN)
+#pragma unroll
+          for (int i = 0; i < NJ; ++i) {
+            hid |= x[i] == -INFINITY ? 1u << i : 0u;
+            const float y = fmaf(S[mt][i / 4][i % 4], gain, x[i]);
+            x[i] = x[i] == -INFINITY ? x[i] : y;
           }
-          if (__ballot(hid != (1u << NJ) - 1u) == 0) continue;  // nothing of this block is seen
+          if (!__ballot(hid != (1u << NJ) - 1u)) continue;  // nothing of this block is seen
         }
         // running maximum
         float top = x[0];
@@ -429,7 +460,7 @@ __global__ __launch_bounds__(kThreads) void attn_fwd_kernel(const AttnArgs a) {
           top = fmaxf(top, __shfl_xor(top, 16));
           top = fmaxf(top, __shfl_xor(top, 32));
           const float mn = fmaxf(mx[mt], top);
-          const float f = mx[mt] == -INFINITY ? 0.f : exp_nat(mx[mt] - mn);
+          const float f = mx[mt] == -INFINITY ? 0.f : exp2_fast(mx[mt] - mn);
           mx[mt] = mn;
           sum[mt] *= f;
 #pragma unroll
@@ -438,30 +469,44 @@ __global__ __launch_bounds__(kThreads) void attn_fwd_kernel(const AttnArgs a) {
         const float base = mx[mt] == -INFINITY ? 0.f : mx[mt];
 #pragma unroll
         for (int i = 0; i < NJ; ++i) {
-          x[i] = exp_nat(x[i] - base);
+          x[i] = exp2_fast(x[i] - base);
           sum[mt] += x[i];
         }
         if constexpr (KV == kPagedInt8) {
 #pragma unroll
-          for (int i = 0; i < NJ; ++i) x[i] *= vs[i];
-          if (hid) {
+          for (int i = 0; i < NJ; ++i) x[i] *= exp_byte(word(vexp, i / 4), i % 4);
+        }
+        // A hidden row's value (or its scale) may be infinite or NaN, and 0
+        // times it is not 0: such blocks go column by column, each with the
+        // values it may not see cleared.
+        bool careful = false;
+        if (slow && __ballot(hid != 0)) {
+          bool odd = false;
+          if constexpr (KV == kPagedInt8) {
 #pragma unroll
-            for (int i = 0; i < NJ; ++i) x[i] = (hid >> i) & 1 ? 0.f : x[i];  // (a hidden row's scale may be infinite)
+            for (int i = 0; i < NJ; ++i) x[i] = (hid >> i) & 1 ? 0.f : x[i];
+          } else if constexpr (kF32) {
+#pragma unroll
+            for (int i = 0; i < NJ; ++i)
+#pragma unroll
+              for (int e = 0; e < NE; ++e) odd |= !(fabsf(vf[i][e]) < INFINITY);
+          } else {
+#pragma unroll
+            for (int s = 0; s < NT / 2; ++s)
+#pragma unroll
+              for (int e = 0; e < NE; ++e) {
+                const uint4 w = __builtin_bit_cast(uint4, vb[s][e]);
+                odd |= odd_bf16(w.x) || odd_bf16(w.y) || odd_bf16(w.z) || odd_bf16(w.w);
+              }
           }
+          careful = __ballot(odd) != 0;
         }
         if constexpr (kF32) {
-          bool odd = false;
-          if (slow) {
+          if (!careful) {
 #pragma unroll
             for (int i = 0; i < NJ; ++i)
 #pragma unroll
-              for (int e = 0; e < NE; ++e) odd |= (b.vw[i][e] & 0x7f800000u) == 0x7f800000u;
-          }
-          if (!slow || !__ballot(odd)) {
-#pragma unroll
-            for (int i = 0; i < NJ; ++i)
-#pragma unroll
-              for (int e = 0; e < NE; ++e) o[mt][e] = mfma_f32(__uint_as_float(b.vw[i][e]), x[i], o[mt][e]);
+              for (int e = 0; e < NE; ++e) o[mt][e] = mfma_f32(vf[i][e], x[i], o[mt][e]);
           } else {
             for (int col = 0; col < 16; ++col) {
               const uint32_t h = __shfl(hid, col + 16 * g4);
@@ -469,72 +514,60 @@ __global__ __launch_bounds__(kThreads) void attn_fwd_kernel(const AttnArgs a) {
               for (int e = 0; e < NE; ++e) {
                 f32x4 n = o[mt][e];
 #pragma unroll
-                for (int i = 0; i < NJ; ++i)
-                  n = mfma_f32((h >> i) & 1 ? 0.f : __uint_as_float(b.vw[i][e]), x[i], n);
+                for (int i = 0; i < NJ; ++i) n = mfma_f32((h >> i) & 1 ? 0.f : vf[i][e], x[i], n);
                 if (c16 == col) o[mt][e] = n;
               }
             }
           }
         } else {
-          bf16x8 ph[NT / 2], pl[NT / 2];
+          // a term at a time: its operands, then its products
+          auto term = [&] {
+            bf16x8 p[NT / 2];
 #pragma unroll
-          for (int s = 0; s < NT / 2; ++s) {
-            uint32_t hi[4], lo[4];
+            for (int s = 0; s < NT / 2; ++s) {
+              uint32_t w[4];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) split_bf16(x[8 * s + 2 * k], x[8 * s + 2 * k + 1], hi[k], lo[k]);
-            ph[s] = __builtin_bit_cast(bf16x8, make_uint4(hi[0], hi[1], hi[2], hi[3]));
-            pl[s] = __builtin_bit_cast(bf16x8, make_uint4(lo[0], lo[1], lo[2], lo[3]));
-          }
-          // a hidden row's value may be infinite or NaN, and 0 times it is
-          // not 0: such blocks take the columns one by one, each with the
-          // values it may not see cleared
-          bool odd = false;
-          if (KV != kPagedInt8 && slow) {
-#pragma unroll
-            for (int e = 0; e < NE; ++e) {
-              const uint4 w = __builtin_bit_cast(uint4, vb[0][e]);
-              odd |= odd_bf16(w.x) || odd_bf16(w.y) || odd_bf16(w.z) || odd_bf16(w.w);
+              for (int k = 0; k < 4; ++k) w[k] = cut_bf16(x[8 * s + 2 * k], x[8 * s + 2 * k + 1]);
+              p[s] = __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
             }
-          }
-          if (KV == kPagedInt8 || !slow || !__ballot(odd)) {
+            if (!careful) {
 #pragma unroll
-            for (int s = 0; s < NT / 2; ++s)
+              for (int s = 0; s < NT / 2; ++s)
 #pragma unroll
-              for (int e = 0; e < NE; ++e) {
-                o[mt][e] = mfma_bf16(vb[s][e], ph[s], o[mt][e]);
-                o[mt][e] = mfma_bf16(vb[s][e], pl[s], o[mt][e]);
-              }
-          } else {
-            for (int col = 0; col < 16; ++col) {
-              const uint32_t h = __shfl(hid, col + 16 * g4);
+                for (int e = 0; e < NE; ++e) o[mt][e] = mfma_bf16(vb[s][e], p[s], o[mt][e]);
+            } else {
+              for (int col = 0; col < 16; ++col) {
+                const uint32_t h = __shfl(hid, col + 16 * g4);
 #pragma unroll
-              for (int e = 0; e < NE; ++e) {
-                uint4 w = __builtin_bit_cast(uint4, vb[0][e]);
-                auto keep = [&](uint32_t v, int i) {
-                  return v & (((h >> i) & 1 ? 0u : 0xffffu) | ((h >> (i + 1)) & 1 ? 0u : 0xffff0000u));
-                };
-                w = make_uint4(keep(w.x, 0), keep(w.y, 2), keep(w.z, 4), keep(w.w, 6));
-                const bf16x8 vz = __builtin_bit_cast(bf16x8, w);
-                const f32x4 n = mfma_bf16(vz, pl[0], mfma_bf16(vz, ph[0], o[mt][e]));
-                if (c16 == col) o[mt][e] = n;
+                for (int s = 0; s < NT / 2; ++s)
+#pragma unroll
+                  for (int e = 0; e < NE; ++e) {
+                    uint4 w = __builtin_bit_cast(uint4, vb[s][e]);
+                    auto keep = [&](uint32_t v, int i) {
+                      return v & (((h >> (8 * s + i)) & 1 ? 0u : 0xffffu) | ((h >> (8 * s + i + 1)) & 1 ? 0u : 0xffff0000u));
+                    };
+                    w = make_uint4(keep(w.x, 0), keep(w.y, 2), keep(w.z, 4), keep(w.w, 6));
+                    const f32x4 n = mfma_bf16(__builtin_bit_cast(bf16x8, w), p[s], o[mt][e]);
+                    if (c16 == col) o[mt][e] = n;
+                  }
               }
             }
-          }
+          };
+          term();
+          term();
+          if (whole) term();
         }
       }
     };
 
-    int jb = j0 + wave * BJ;
-    if (jb < jend) {
-      Blk cur;
-      load(cur, jb);
-      for (; jb < jend; jb += kWaves * BJ) {
-        Blk nxt;
-        const bool more = jb + kWaves * BJ < jend;
-        if (more) load(nxt, jb + kWaves * BJ);
-        compute(cur, jb);
-        if (more) cur = nxt;
-      }
+    // each wave takes consecutive blocks (a lane's bucket changes seldom then)
+    const int blocks = (jend - j0 + BJ - 1) / BJ, share = (blocks + parts - 1) / parts;
+    int jb = j0 + part * share * BJ;
+    const int jstop = min(jend, jb + share * BJ);
+    if (jb < jstop) {
+      Blk blk;
+      load(blk, jb);
+      for (; jb < jstop; jb += BJ) compute(blk, jb, jb + BJ < jstop);
     }
 
     // ---- join the waves: lane group g4 of wave w holds features NE (4 g4 + i) + e of column c16
@@ -554,50 +587,49 @@ __global__ __launch_bounds__(kThreads) void attn_fwd_kernel(const AttnArgs a) {
 #pragma unroll
         for (int e = 0; e < NE; ++e) cw[(NE * (4 * g4 + i) + e) * 16 + c16] = o[mt][e][i];
       __syncthreads();
-      // thread: column tid / 16, DH / 16 consecutive features
+      // thread: column tid / 16, DH / 16 consecutive features, of each head
       const int col = tid >> 4, f0 = (tid & 15) * NE;
-      float M = -INFINITY, L = 0.f, acc[NE];
+      const int row = (zz * MT + mt) * 16 + col;
+      for (int hd = 0; hd < a.hw && row < rows; ++hd) {
+        float M = -INFINITY, L = 0.f, acc[NE];
+        for (int w = hd; w < kWaves; w += a.hw) M = fmaxf(M, comb[w * 16 * (DH + 2) + 16 * DH + 2 * col]);
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w) M = fmaxf(M, comb[w * 16 * (DH + 2) + 16 * DH + 2 * col]);
+        for (int e = 0; e < NE; ++e) acc[e] = 0.f;
+        for (int w = hd; w < kWaves; w += a.hw) {
+          const float* p = comb + w * 16 * (DH + 2);
+          const float mw = p[16 * DH + 2 * col], lw = p[16 * DH + 2 * col + 1];
+          // (a NaN sum without a maximum is a row of NaN scores)
+          const float f = mw == -INFINITY ? (lw != lw ? lw : 0.f) : exp2_fast(mw - M);
+          L += f * lw;
 #pragma unroll
-      for (int e = 0; e < NE; ++e) acc[e] = 0.f;
+          for (int e = 0; e < NE; ++e) acc[e] += f * p[(f0 + e) * 16 + col];
+        }
+        const int64_t t = t0 + row / a.G;
+        const int h = (g0 + hd) * a.G + row % a.G;
+        if (split) {
+          const int64_t at = (static_cast<int64_t>(c) * a.n_tgt + t) * a.H + h;
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w) {
-        const float* p = comb + w * 16 * (DH + 2);
-        const float mw = p[16 * DH + 2 * col], lw = p[16 * DH + 2 * col + 1];
-        // (a NaN sum without a maximum is a row of NaN scores)
-        const float f = mw == -INFINITY ? (lw != lw ? lw : 0.f) : exp_nat(mw - M);
-        L += f * lw;
+          for (int e = 0; e < NE; ++e) a.part_o[at * DH + f0 + e] = acc[e];
+          if (f0 == 0) {
+            a.part_ml[2 * at] = M;
+            a.part_ml[2 * at + 1] = L;
+          }
+        } else {
+          const float inv = L == 0.f ? 0.f : 1.f / L;
+          T* op = static_cast<T*>(a.out) + (t * a.H + h) * DH + f0;
 #pragma unroll
-        for (int e = 0; e < NE; ++e) acc[e] += f * p[(f0 + e) * 16 + col];
+          for (int e = 0; e < NE; ++e) {
+            const float y = acc[e] * inv;
+            op[e] = from_f32<T>(y);
+            if (a.sa) a.sa[(t * a.H + h) * DH + f0 + e] = y;
+          }
+          if (a.sm && f0 == 0) {
+            a.sm[t * a.H + h] = M;
+            a.sl[t * a.H + h] = L;
+          }
+        }
       }
       __syncthreads();
-      const int row = (zz * MT + mt) * 16 + col;
-      if (row >= rows) continue;
-      const int64_t t = t0 + row / a.G;
-      const int h = g * a.G + row % a.G;
-      if (split) {
-        const int64_t at = (static_cast<int64_t>(c) * a.n_tgt + t) * a.H + h;
-#pragma unroll
-        for (int e = 0; e < NE; ++e) a.part_o[at * DH + f0 + e] = acc[e];
-        if (f0 == 0) {
-          a.part_ml[2 * at] = M;
-          a.part_ml[2 * at + 1] = L;
-        }
-      } else {
-        const float inv = L == 0.f ? 0.f : 1.f / L;
-        T* op = static_cast<T*>(a.out) + (t * a.H + h) * DH + f0;
-#pragma unroll
-        for (int e = 0; e < NE; ++e) {
-          const float y = acc[e] * inv;
-          op[e] = from_f32<T>(y);
-          if (a.sa) a.sa[(t * a.H + h) * DH + f0 + e] = y;
-        }
-        if (a.sm && f0 == 0) {
-          a.sm[t * a.H + h] = M;
-          a.sl[t * a.H + h] = L;
-        }
-      }
     }
   }
 }
@@ -605,8 +637,9 @@ __global__ __launch_bounds__(kThreads) void attn_fwd_kernel(const AttnArgs a) {
 template <typename T, int KV, int DH, int MT>
 hipError_t launch_fwd(const AttnArgs& a, hipStream_t st) {
   const int64_t pages = KV == kRagged ? 0 : (a.chunk >> a.page_shift) + 1;
-  const size_t lds = 4 * (kCombineFloats<DH> + kMaxBuckets + 32 + static_cast<int64_t>(a.G) * a.b.n + pages);
-  const int64_t grid = round_up(a.units, kXcds) * a.Hk * a.zgroups + 1;
+  const size_t lds = 4 * (kCombineFloats<DH> + 2 * (kCells + 1) + kMaxBuckets +
+                          static_cast<int64_t>(a.hw) * a.G * (std::max(a.b.n, 1) + 1) + pages);
+  const int64_t grid = round_up(a.units, kXcds) * (a.Hk / a.hw) * a.zgroups + 1;
   if (grid > 0x7fffffff) return hipErrorInvalidValue;
   const hipError_t e = allow_lds<&attn_fwd_kernel<T, KV, DH, MT>>(lds);
   if (e != hipSuccess) return e;

@@ -46,7 +46,7 @@ __global__ __launch_bounds__(256) void attn_merge_kernel(const AttnArgs a, bool 
   for (int c = 0; c < n; ++c) {
     const int64_t at = c * step + row;
     const float m = a.part_ml[2 * at], l = a.part_ml[2 * at + 1];
-    const float f = m == -INFINITY ? (l != l ? l : 0.f) : exp_nat(m - M);
+    const float f = m == -INFINITY ? (l != l ? l : 0.f) : exp2_fast(m - M);
     L += f * l;
 #pragma unroll
     for (int e = 0; e < NE; ++e) acc[e] += f * a.part_o[at * DH + f0 + e];

@@ -21,15 +21,23 @@ constexpr int kXcds = 8;          // workgroup i runs on XCD i % 8
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 
-// Buckets of distance, by value in the kernel arguments.  A distance's cell is
-// its octave and next two bits; cell[] holds the bucket of the cell's lowest
-// distance, from which the edges above it are walked (none or one, where edges
-// are no closer than a quarter octave).
+// Buckets of distance, by value in the kernel arguments.
 struct Buckets {
   int32_t n;                       // buckets; 0: no bias
+  int32_t multi;                   // a cell of the lookup holds several edges
   int32_t edges[kMaxBuckets];      // n - 1 ascending, then INT32_MAX
-  uint8_t cell[128];
+  uint8_t cell[512];               // bucket of each cell's lowest x (see below)
 };
+
+// The lookup of a bucket: with x = max(D + 1, 0), cell 0..495 is x's octave and
+// next four bits (so the cells of up to 32 distances hold one each), and cell
+// kHiddenCell is x = 0, a distance below 0.  An entry holds the bucket of the
+// cell's lowest x and the first edge above it, which x > edge has passed.
+constexpr int kCells = 497, kHiddenCell = 496;
+inline __host__ __device__ int64_t cell_low(int c) {  // lowest x of cell c (rounded up)
+  const int o = c >> 4;
+  return ((static_cast<int64_t>(16 + (c & 15)) << o) + 15) >> 4;
+}
 
 struct AttnArgs {
   const void *q, *k, *v;           // ragged: rows of the batch; cache: q rows, K and V pages
@@ -46,6 +54,7 @@ struct AttnArgs {
   float scale, cap;
   int64_t n_hist, n_tgt;
   int32_t chunk, max_chunks, units, zgroups;
+  int32_t hw;                      // kv heads of a workgroup (1, 2 or 4): a wave has one, 4 / hw waves share it
   // forward
   void* out;
   float *sa, *sm, *sl;             // saved (nullable): normalised output, score maximum, sum
@@ -122,16 +131,21 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
 __device__ __forceinline__ float lo_f32(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float hi_f32(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 
-// Both terms of a two-term bf16 split of (a, b): hi is a rounded to 8
-// significant bits, lo the rest rounded likewise, together 16 bits or more.
-__device__ __forceinline__ void split_bf16(float a, float b, uint32_t& hi, uint32_t& lo) {
-  hi = pack_bf16(a, b);
-  lo = pack_bf16(a - lo_f32(hi), b - hi_f32(hi));
+// The high halves of a and b as a pair of bf16.
+__device__ __forceinline__ uint32_t high_halves(float a, float b) {
+  return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
+}
+// Splits a and b into bf16 terms by cutting bits off: the first returned, the
+// rest left in a and b.  Each term holds 8 significant bits, so two leave less
+// than 2^-16 of a value and three nothing of an fp32.
+__device__ __forceinline__ uint32_t cut_bf16(float& a, float& b) {
+  const uint32_t t = high_halves(a, b);
+  a -= __uint_as_float(__float_as_uint(a) & 0xffff0000u);
+  b -= __uint_as_float(__float_as_uint(b) & 0xffff0000u);
+  return t;
 }
 
-// exp(x) of a difference in natural units: the factor log2 e comes after the
-// subtraction, so that scores of the type's lowest value still cancel.
-__device__ __forceinline__ float exp_nat(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // tanh(x) to about 1e-7 relative: 1 - 2 / (e^2x + 1) away from zero, the odd
 // series up to x^9 near it, where the difference would cancel.
@@ -148,22 +162,57 @@ __device__ __forceinline__ float tanh_fast(float x) {
 
 __device__ __forceinline__ int sub_sat(int a, int b) { return __builtin_elementwise_sub_sat(a, b); }
 
-// Buckets in LDS: edges, cells and the bias rows of a workgroup's heads.
+// A workgroup's bucket tables in LDS: the cells, and per query head (`heads` from
+// that of kv head g on) the biases in units of log2 e (a finite one stays finite).  Without a
+// bias there is one bucket, of bias 0; the slot after the buckets is for what
+// is hidden, minus infinity.
 struct BucketLds {
+  const int2* cells;  // {next edge, bucket}
+  const float* bias;  // [heads][slots + 1]
   const int32_t* edges;
-  const uint8_t* cell;
-  const float* bias;  // [heads of the workgroup][n]
-  int n;
+  int slots, multi;
 };
 
-__device__ __forceinline__ int bucket_of(const BucketLds& b, int dist) {
-  const uint32_t d = static_cast<uint32_t>(max(dist, 0));
-  const int z = __clz(static_cast<int>(d | 1u));
-  const uint32_t top = (d << z) >> 29;                 // 1xx (0 for d = 0)
-  const int c = 4 * (31 - z) + static_cast<int>(top & 3u);
-  int k = b.cell[c];
-  while (static_cast<int>(d) >= b.edges[k] && k < b.n - 1) ++k;
+__device__ __forceinline__ float scaled_bias(float b) {
+  const float x = b * kLog2e;
+  constexpr float top = 3.4028234663852886e38f;
+  return fabsf(b) <= top ? fminf(fmaxf(x, -top), top) : x;
+}
+
+// Fills the tables (threads of the whole workgroup; a barrier follows).
+__device__ __forceinline__ BucketLds fill_buckets(const AttnArgs& a, int g, int heads, int2* cells, float* bias, int32_t* edges) {
+  const int n = a.b.n, slots = max(n, 1);
+  for (int i = threadIdx.x; i < kCells; i += blockDim.x) {
+    const int k = i == kHiddenCell && a.masked ? slots : a.b.cell[i];
+    cells[i] = make_int2(k < slots - 1 ? a.b.edges[k] : 0x7fffffff, k);
+  }
+  for (int i = threadIdx.x; i < heads * (slots + 1); i += blockDim.x) {
+    const int h = i / (slots + 1), k = i % (slots + 1);
+    bias[i] = k < n ? scaled_bias(a.bias[(static_cast<int64_t>(g) * a.G + h) * n + k]) : k == slots ? -INFINITY : 0.f;
+  }
+  for (int i = threadIdx.x; i < slots; i += blockDim.x) edges[i] = a.b.edges[i];
+  return BucketLds{cells, bias, edges, slots, a.b.multi};
+}
+
+// x of a distance and its cell
+__device__ __forceinline__ int place_of(int tpos, int pos) {
+  return max(__builtin_elementwise_add_sat(sub_sat(tpos, pos), 1), 0);
+}
+__device__ __forceinline__ int cell_of(int x) {
+  const int z = x ? __builtin_clz(static_cast<uint32_t>(x)) : -1;
+  return static_cast<int>((static_cast<uint32_t>(x) << (z & 31)) >> 27) - 16 * z + 480;
+}
+__device__ __forceinline__ int bucket_in(const BucketLds& b, int x, int2 cell) {
+  int k = cell.y + (x > cell.x);
+  if (b.multi && x > 0)
+    while (k < b.slots - 1 && x > b.edges[k]) ++k;
   return k;
+}
+// Distances (as x) of a bucket, for a lane that keeps it: none if it is hidden.
+__device__ __forceinline__ void keep_bucket(const BucketLds& b, bool masked, int k, float bias, int& lo, int& hi) {
+  lo = k > 0 && k < b.slots ? b.edges[k - 1] + 1 : masked ? 1 : 0;
+  hi = k < b.slots - 1 ? b.edges[k] : 0x7fffffff;
+  if (bias == -INFINITY) lo = 0x7fffffff, hi = 0;
 }
 
 // The request of unit u: every request r holds the units from hist_off[r] /
@@ -186,6 +235,21 @@ __device__ __forceinline__ int find_request(const int32_t* off, int R, int64_t n
     n_left = min(stride, n_left - (c - 1) * stride);
   }
   return lo;
+}
+
+// A value that is the same in every lane, in scalar registers (so that loads
+// take it as their base).
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+typedef const __attribute__((address_space(1))) char* gptr;  // global memory
+__device__ __forceinline__ gptr uniform(const void* p) {
+  const uint64_t v = reinterpret_cast<uint64_t>(p);
+  const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(v));
+  const uint32_t hi = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(v >> 32));
+  return reinterpret_cast<gptr>(static_cast<uint64_t>(hi) << 32 | lo);
+}
+template <typename V>
+__device__ __forceinline__ V load_at(gptr base, uint32_t at) {
+  return *reinterpret_cast<const __attribute__((address_space(1))) V*>(base + at);
 }
 
 __device__ __forceinline__ int clamp_off(int32_t v, int64_t n) {

@@ -41,7 +41,7 @@ def forward(a=None, b=None, g=None, out=0x600000, ws=0x700000, ws_bytes=1 << 40)
     (dict(n_heads=7), BAD), (dict(n_kv_heads=0), BAD), (dict(n_heads=0), BAD), (dict(dtype=3), BAD),
     (dict(scale=float("nan")), BAD), (dict(scale=float("inf")), BAD), (dict(softcap=-1.0), BAD),
     (dict(softcap=float("nan")), BAD), (dict(n_buckets=129), BAD), (dict(n_buckets=-1), BAD), (dict(edges=None), BAD),
-    (dict(edges=EDGES[::-1].copy()), BAD), (dict(edges=EDGES * 0 + 1), BAD), (dict(edges=EDGES - 1), BAD),
+    (dict(edges=EDGES[::-1].copy()), BAD), (dict(edges=EDGES * 0 + 1), BAD), (dict(edges=EDGES - 1), BAD), (dict(edges=np.r_[EDGES[:6], 2 ** 31 - 1].astype(np.int32)), BAD),
     (dict(d_head=48), NO), (dict(d_head=256), NO), (dict(d_head=16), NO), (dict(n_heads=65, n_kv_heads=1), NO),
     (dict(n_heads=1024, n_kv_heads=1024, d_head=128), NO)])
 def test_scores_are_checked(kw, status):
@@ -153,13 +153,13 @@ def test_cache_attention_arguments_are_checked():
 
 
 def test_bias_edges():
-    for n, exact, top in ((2, 1, 2), (32, 8, 8192), (128, 64, 2 ** 31 - 1), (128, 1, 128), (100, 99, 100), (8, 7, 8)):
+    for n, exact, top in ((2, 1, 2), (32, 8, 8192), (128, 64, 2 ** 31 - 2), (128, 1, 128), (100, 99, 100), (8, 7, 8)):
         e = stca.bias_edges(n, exact, top)
         assert len(e) == n - 1 and e[0] == 1 and (np.diff(e.astype(np.int64)) >= 1).all() and e[-1] <= top
         assert list(e[:exact]) == list(range(1, min(exact, n - 1) + 1))
         if exact < n - 1:
             assert e[-1] == top
-    for n, exact, top in ((1, 1, 8), (129, 8, 8192), (8, 0, 100), (8, 8, 100), (8, 2, 7)):
+    for n, exact, top in ((1, 1, 8), (129, 8, 8192), (8, 0, 100), (8, 8, 100), (8, 2, 7), (8, 2, 2 ** 31 - 1)):
         with pytest.raises(stca.StcaError):
             stca.bias_edges(n, exact, top)
     assert stca.lib().stca_bias_edges(8, 2, 100, ctypes.POINTER(ctypes.c_int32)()) == BAD
