@@ -11,13 +11,17 @@ using namespace stca;
 using namespace stca::api;
 using namespace stca::ops;
 
+#ifndef PCP
+#define PCP 4
+#endif
 #ifndef PCU
-#define PCU 4
+#define PCU 8
 #endif
 namespace {
 
 constexpr int64_t kMaxRows = 0x7fff0000;  // rows of one call: indices a few blocks past the end stay int32
 constexpr int kNoHostChunks = 16;         // chunks per request where the host knows no lengths
+constexpr int kMostChunks = 512;           // of a request, in a backward of several passes
 constexpr int kMaxPagesOfChunk = 1024;    // a chunk's pages are listed in LDS
 
 bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
@@ -102,26 +106,43 @@ void fill_edges(const stca_attn_t* a, Buckets* b) {
 
 struct Plan {
   int chunk, max_chunks, units, tiles, zgroups, btiles, passes, hw;
-  size_t hdr, part_o, part_ml, part_dq, part_db, acc_kv, total;
+  size_t hdr, part_o, part_ml, part_dq, part_db, acc_kv, rows, total;
 };
 
-// Chunk length that gives about `per_cu` workgroups per CU (whole histories
-// where that is enough): a workgroup costs its start, the join of its waves
-// and a partial to merge, and the last ones to run leave CUs idle, the less
-// the more there are.
-int chunk_for(int64_t rows, int64_t per_row, int per_cu) {
+// Chunk length that gives about `per_cu` workgroups per CU, each of which is to
+// have `rows` history rows times `per_row` workgroups to itself: a workgroup
+// costs its start, the join of its waves and a partial to merge, and the last
+// ones to run leave CUs idle, the less the more there are (window of 256
+// requests, 16 targets, 2048 rows, d_h = 32: 4 a CU 145 us forward, 354
+// backward, 8 134 and 320, 16 142 and 336).
+int chunk_for(int64_t rows, int64_t per_row, int per_cu, int step) {
   const int64_t want = static_cast<int64_t>(per_cu) * device_cus();
-  const int64_t c = round_up(std::max<int64_t>(1, ceil_div(rows * per_row, want)), kChunkStep);
-  return static_cast<int>(std::min<int64_t>(c, round_up(kMaxRows, kChunkStep) - kChunkStep));
+  const int64_t c = round_up(std::max<int64_t>(1, ceil_div(rows * per_row, want)), step);
+  return static_cast<int>(std::min<int64_t>(c, kMaxRows / step * step));
 }
 
-// kv heads a workgroup takes (see attn_fwd.h): as many as there are to four,
-// where a wave to a head then has 256 history rows on every SIMD of the card.
-int heads_of(int Hk, int64_t n_hist) {
-  const int most = Hk % 4 == 0 ? 4 : Hk % 2 == 0 ? 2 : 1;
-#ifdef HWF
-  return std::min(most, HWF);
+#ifndef HWF
+#define HWF 4
 #endif
+#ifndef CMINF
+#define CMINF 128
+#endif
+#ifndef CMINB
+#define CMINB 64
+#endif
+#ifndef HWB
+#define HWB 2
+#endif
+#ifndef PCB
+#define PCB 8
+#endif
+// kv heads a workgroup takes (see attn_fwd.h): as many as there are to four (two
+// in the backward, one where it holds several tiles: its rows of every head
+// wait in LDS), where a wave to a head then has 256 history rows on every SIMD
+// of the card.
+int heads_of(int Hk, int64_t n_hist, bool backward, int tiles) {
+  int most = Hk % 4 == 0 ? 4 : Hk % 2 == 0 ? 2 : 1;
+  most = std::min(most, backward ? (tiles > 1 ? 1 : HWB) : HWF);
   return n_hist * Hk >= 256 * 4 * static_cast<int64_t>(device_cus()) ? most : 1;
 }
 
@@ -138,18 +159,26 @@ bool ragged_plan(const stca_attn_t* a, const stca_batch_t* b, bool backward, Pla
   p->tiles = forward_tiles(a->dtype, dh, static_cast<int>(std::min<int64_t>(max_m * G, 1 << 20)));
   p->zgroups = static_cast<int>(std::min<int64_t>(std::max<int64_t>(1, ceil_div(max_m * G, 16 * p->tiles)),
                                                   b->hist_off_host ? 1024 : 8));
-  p->chunk = chunk_for(b->n_hist, static_cast<int64_t>(Hk / heads_of(Hk, b->n_hist)) * (backward ? 1 : p->zgroups), PCU);
-  if (!b->hist_off_host)
-    p->chunk = static_cast<int>(std::max<int64_t>(p->chunk, round_up(ceil_div(b->n_hist, kNoHostChunks), kChunkStep)));
-  p->chunk = static_cast<int>(std::min<int64_t>(p->chunk, std::max<int64_t>(kChunkStep, round_up(max_l, kChunkStep))));
-  p->max_chunks = static_cast<int>(std::max<int64_t>(1, ceil_div(max_l, p->chunk)));
-  p->hw = heads_of(Hk, b->n_hist);
-  const int64_t units = b->n_hist / p->chunk + b->n_requests;
-  if (units * Hk * p->zgroups > 0x7f000000) return false;
-  p->units = static_cast<int>(units);
   const int64_t need = ceil_div(max_m, 16);
   p->btiles = backward_tiles(a->dtype, dh, static_cast<int>(std::min<int64_t>(need, 1 << 20)));
   p->passes = static_cast<int>(std::max<int64_t>(1, ceil_div(need, p->btiles) * G));
+  p->hw = backward && p->passes > 1 ? 1 : heads_of(Hk, b->n_hist, backward, p->btiles);
+  const int parts = 4 / p->hw;
+  if (backward && p->passes > 1) {
+    // one step a wave, unless that makes more chunks than dq's partials are worth
+    p->chunk = static_cast<int>(std::max<int64_t>(16 * parts, round_up(ceil_div(max_l, kMostChunks), 16 * parts)));
+  } else {
+    p->chunk = chunk_for(b->n_hist, static_cast<int64_t>(Hk / p->hw) * (backward ? 1 : p->zgroups), backward ? PCB : PCU,
+                         16 * parts);
+    p->chunk = std::max(p->chunk, (backward ? CMINB : CMINF) * parts);
+  }
+  if (!b->hist_off_host)
+    p->chunk = static_cast<int>(std::max<int64_t>(p->chunk, round_up(ceil_div(b->n_hist, kNoHostChunks), 64)));
+  p->chunk = static_cast<int>(std::min<int64_t>(p->chunk, std::max<int64_t>(64, round_up(max_l, 64))));
+  p->max_chunks = static_cast<int>(std::max<int64_t>(1, ceil_div(max_l, p->chunk)));
+  const int64_t units = b->n_hist / p->chunk + b->n_requests;
+  if (units * Hk * p->zgroups > 0x7f000000) return false;
+  p->units = static_cast<int>(units);
   Bump m;
   p->hdr = m.take(sizeof(WsHeader));
   const size_t rows = static_cast<size_t>(b->n_tgt) * H, split = p->max_chunks > 1 ? p->max_chunks : 0;
@@ -157,9 +186,10 @@ bool ragged_plan(const stca_attn_t* a, const stca_batch_t* b, bool backward, Pla
     p->part_o = m.take(4 * split * rows * dh);
     p->part_ml = m.take(8 * split * rows);
   } else {
+    p->rows = m.take(16 * rows);
     p->part_dq = m.take(4 * split * rows * dh);
     p->part_db = m.take(4 * static_cast<size_t>(p->units) * H * a->n_buckets);
-    p->acc_kv = m.take(p->passes > 1 ? 8 * static_cast<size_t>(b->n_hist) * Hk * dh : 0);
+    p->acc_kv = m.take(p->passes > 1 && p->chunk > 16 * parts ? 8 * static_cast<size_t>(b->n_hist) * Hk * dh : 0);
   }
   p->total = m.off;
   return true;
@@ -229,9 +259,9 @@ bool paged_plan(const stca_attn_t* a, const stca_cache_t* c, const stca_cache_ba
   p->tiles = forward_tiles(STCA_BF16, dh, static_cast<int>(std::min<int64_t>(max_m * G, 1 << 20)));
   p->zgroups = static_cast<int>(std::min<int64_t>(std::max<int64_t>(1, ceil_div(max_m * G, 16 * p->tiles)),
                                                   b->tgt_off_host ? 1024 : 8));
-  p->chunk = chunk_for(static_cast<int64_t>(b->n_requests) * b->max_len, static_cast<int64_t>(Hk) * p->zgroups, 4);
+  p->chunk = chunk_for(static_cast<int64_t>(b->n_requests) * b->max_len, static_cast<int64_t>(Hk) * p->zgroups, PCP, kPageStep);
   p->chunk = std::min(p->chunk, kMaxPagesOfChunk * c->page_size);
-  p->chunk = static_cast<int>(std::min<int64_t>(p->chunk, std::max<int64_t>(kChunkStep, round_up(b->max_len, kChunkStep))));
+  p->chunk = static_cast<int>(std::min<int64_t>(p->chunk, std::max<int64_t>(kPageStep, round_up(b->max_len, kPageStep))));
   p->max_chunks = static_cast<int>(std::max<int64_t>(1, ceil_div(b->max_len, p->chunk)));
   const int64_t units = static_cast<int64_t>(b->n_requests) * p->max_chunks;
   if (units * Hk * p->zgroups > 0x7f000000) return false;
@@ -401,6 +431,7 @@ stca_status_t stca_attn_backward(const stca_attn_t* attn, const stca_batch_t* ba
   a.part_dq = at<float>(ws, p.part_dq);
   a.part_db = at<float>(ws, p.part_db);
   a.acc_kv = at<float>(ws, p.acc_kv);
+  a.rows = at<float>(ws, p.rows);
   a.hdr = at<WsHeader>(ws, p.hdr);
   HIPCHK(attn_backward(a, attn->dtype, attn->d_head, p.btiles, stream));
   return STCA_OK;

@@ -10,8 +10,10 @@
 // rows (see attn_fwd.h), and hold dK^T, dV^T of a step in registers while they go through the pass's MT tiles of 16 targets (of
 // one query head each), whose q and dout rows wait in LDS.  dq of a pass stays
 // in registers over the whole chunk.  More tiles than MT are further passes
-// over the chunk, with dK, dV of the passes so far in fp32 in the workspace
-// (the same lanes write and read them).  So K, V are read and dK, dV written
+// over the chunk; a chunk is then one step a wave, whose K, V, dK and dV stay in
+// registers from pass to pass (or, where that would make too many chunks, dK
+// and dV of the passes so far wait in fp32 in the workspace, written and read by
+// the same lanes).  So K, V are read and dK, dV written
 // once, nothing is added in order of arrival, and gradients repeat bitwise.
 //
 // Scores are formed as S^T = K Q^T: a lane holds one target, column t = lane %
@@ -144,6 +146,15 @@ __device__ __forceinline__ typename Four<T>::type column4(const unsigned char* t
   }
 }
 
+template <typename T>
+__device__ __forceinline__ bool odd16(const uint4& w) {  // a value of 16 bytes is not finite
+  const uint32_t v[4] = {w.x, w.y, w.z, w.w};
+  bool odd = false;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) odd |= (v[i] & 0x7f800000u) == 0x7f800000u || (Elem<T>::bf16 && (v[i] & 0x7f80u) == 0x7f80u);
+  return odd;
+}
+
 // Elements of x whose bit in h is set are cleared.
 __device__ __forceinline__ s16x4 cleared(s16x4 x, uint32_t h) {
 #pragma unroll
@@ -175,7 +186,7 @@ struct BwdLds {
   static size_t bytes(int hw, int G, int n, int copies) {
     const size_t slots = n > 1 ? n : 1, heads = static_cast<size_t>(hw) * G;
     return kTables + hw * kHead + 8 * (kCells + 1) +
-           4 * (kMaxBuckets + heads * (slots + 1) + heads * n + (n ? kWaves * (slots + 1) * copies : 0));
+           4 * (kMaxBuckets + (heads * (slots + 1) + heads * n + 3) / 4 * 4 + (n ? kWaves * (slots + 1) * copies : 0));
   }
 };
 
@@ -183,11 +194,15 @@ struct BwdLds {
 // sums stay within 36 KB, else every second or fourth, which then take turns.
 inline __host__ __device__ int bin_copies(int n) { return n <= 34 ? 64 : n <= 70 ? 32 : 16; }
 
-#ifndef EUB
-#define EUB 2
+#ifndef EUB64
+#define EUB64 2
 #endif
+// Waves a SIMD is to hold: what the registers allow without spills.
+template <typename T, int DH, int MT>
+constexpr int kBwdWaves = DH == 128 ? 1 : DH == 64 && (MT > 1 || !Elem<T>::bf16) ? EUB64 : 2;
+
 template <typename T, int DH, int MT, int JT>
-__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(EUB))) void attn_bwd_kernel(const AttnArgs a) {
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kBwdWaves<T, DH, MT>))) void attn_bwd_kernel(const AttnArgs a) {
   constexpr bool kBf16 = Elem<T>::bf16;
   constexpr int KS = DH / 32, NE = DH / 16, BJ = 16 * JT;
   using F4 = typename Four<T>::type;
@@ -201,14 +216,10 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(EUB)))
   int32_t* s_edges = reinterpret_cast<int32_t*>(s_cells + kCells + 1);
   float* s_bias = reinterpret_cast<float*>(s_edges + kMaxBuckets);
   float* s_db = s_bias + a.hw * a.G * (slots + 1);
-  float* s_bins = s_db + a.hw * a.G * nb;
+  float* s_bins = s_db + (a.hw * a.G * nb + a.hw * a.G * (slots + 1) + 3) / 4 * 4 - a.hw * a.G * (slots + 1);
 
   const int tid = threadIdx.x, lane = tid & 63, c16 = lane & 15, g4 = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  if (blockIdx.x == gridDim.x - 1) {
-    check_call(a, false);
-    return;
-  }
   const int ghs = a.Hk / a.hw;
   const int unit = static_cast<int>(blockIdx.x) / kXcds / ghs * kXcds + static_cast<int>(blockIdx.x) % kXcds;
   if (unit >= a.units) return;
@@ -238,49 +249,82 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(EUB)))
   const float gain = kLog2e * (a.cap > 0.f ? a.cap : a.scale), cap_in = a.cap > 0.f ? a.scale / a.cap : 0.f;
 
   const int passes = max(1, groups * a.G);
+  const bool single = a.chunk <= BJ * parts;  // one step a wave
+  f32x4 dk[JT][NE], dv[JT][NE];
+  E8 kf[JT][KS], vf[JT][KS];  // the step's rows, or the next one's once they are used
+  int pj[JT][4];              // positions of rows 4 g4 + i
+  const uint32_t lk = static_cast<uint32_t>(a.ldk * sizeof(T)), lv = static_cast<uint32_t>(a.ldv * sizeof(T));
+  auto load = [&](int jb) {
+    const int last = len - 1 - jb;
+    const gptr kp = uniform(static_cast<const T*>(a.k) + (h0 + jb) * a.ldk + g * DH);
+    const gptr vp = uniform(static_cast<const T*>(a.v) + (h0 + jb) * a.ldv + g * DH);
+#pragma unroll
+    for (int jt = 0; jt < JT; ++jt) {
+      const int jr = min(16 * jt + c16, last);
+      const uint32_t ak = __umul24(jr, lk) + 8 * g4 * sizeof(T), av = __umul24(jr, lv) + 8 * g4 * sizeof(T);
+#pragma unroll
+      for (int s = 0; s < KS; ++s) {
+        kf[jt][s] = load8_at<T>(kp + 32 * s * sizeof(T), ak);
+        vf[jt][s] = load8_at<T>(vp + 32 * s * sizeof(T), av);
+      }
+    }
+    if (a.hist_pos) {
+      const gptr hp = uniform(a.hist_pos + h0 + jb);
+#pragma unroll
+      for (int jt = 0; jt < JT; ++jt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) pj[jt][i] = load_at<int>(hp, 4u * min(16 * jt + 4 * g4 + i, last));
+    }
+  };
+  // a pass's rows on their way to LDS, 16 bytes of q and of dout a thread
+  constexpr int kPieces = DH * static_cast<int>(sizeof(T)) / 16;
+  constexpr int kHeadsMost = MT == 1 ? kWaves : 1;  // (several heads a workgroup: one tile, see the host)
+  constexpr int kFetch = (16 * MT * kHeadsMost * kPieces + kThreads - 1) / kThreads;
+  uint4 fq[kFetch], fd[kFetch];
+  f32x4 frow;
+  auto fetch = [&](int pass) {
+    const int hh = groups ? pass / groups : 0, first = groups ? pass % groups * MT : 0;
+#pragma unroll
+    for (int n = 0; n < kFetch; ++n) {
+      const int i = tid + n * kThreads, piece = i % kPieces, at = i / kPieces, hd = at / (16 * MT);
+      const int t = 16 * first + at % (16 * MT);
+      fq[n] = fd[n] = uint4{};
+      if (hd < a.hw && t < m) {
+        const int64_t h = (g0 + hd) * a.G + hh;
+        fq[n] = reinterpret_cast<const uint4*>(static_cast<const T*>(a.q) + (t0 + t) * a.ldq + h * DH)[piece];
+        fd[n] = reinterpret_cast<const uint4*>(static_cast<const T*>(a.dout) + ((t0 + t) * static_cast<int64_t>(a.H) + h) * DH)[piece];
+      }
+    }
+    const int hd = tid / (16 * MT), t = 16 * first + tid % (16 * MT);
+    frow = f32x4{INFINITY, 0.f, 0.f, 0.f};  // (a row without a target has no weight anywhere)
+    if (hd < a.hw && m > 0) {
+      const f32x4 x = reinterpret_cast<const f32x4*>(a.rows)[(t0 + min(t, m - 1)) * static_cast<int64_t>(a.H) +
+                                                             (g0 + hd) * a.G + hh];
+      frow = t < m ? x : f32x4{INFINITY, 0.f, 0.f, x[3]};
+    }
+  };
+  fetch(0);
   for (int pass = 0; pass < passes; ++pass) {
     const int hh = groups ? pass / groups : 0, first = groups ? pass % groups * MT : 0;
     const int held = min(MT, ttiles - first);
     __syncthreads();
-    // ---- the pass's rows: 16 threads a row, DH / 16 features each
     int odd_rows = 0;
-    for (int at = tid >> 4; at < 16 * MT * a.hw; at += kThreads / 16) {
-      const int hd = at / (16 * MT), row = at % (16 * MT);
-      unsigned char* to = smem + Lds::kTables + hd * Lds::kHead;
-      const int t = 16 * first + row;
-      const bool have = t < m;
-      const int64_t tr = t0 + min(t, max(m - 1, 0)), h = (g0 + hd) * a.G + hh;
-      const int f = (tid & 15) * NE;
-      T* qs = reinterpret_cast<T*>(to + row * kRowBytes<T, DH>) + f;
-      T* ds = reinterpret_cast<T*>(to + Lds::kDo + row * kRowBytes<T, DH>) + f;
-      float D = 0.f;
-      bool odd = false;
 #pragma unroll
-      for (int e = 0; e < NE; ++e) {
-        T qv = 0, dv = 0;
-        if (have) {
-          qv = static_cast<const T*>(a.q)[tr * a.ldq + h * DH + f + e];
-          dv = static_cast<const T*>(a.dout)[(tr * a.H + h) * DH + f + e];
-          D += to_f32(dv) * a.fa[(tr * a.H + h) * DH + f + e];
-          odd |= !(fabsf(to_f32(qv)) < INFINITY) || !(fabsf(to_f32(dv)) < INFINITY);
-        }
-        qs[e] = qv;
-        ds[e] = dv;
-      }
-#pragma unroll
-      for (int o = 1; o < 16; o <<= 1) D += __shfl_xor(D, o);
-      odd_rows |= odd;
-      if ((tid & 15) == 0) {
-        // a row without a target, or that sees nothing, has no weight anywhere
-        const float mx = have ? a.fm[tr * a.H + h] : INFINITY, l = have ? a.fl[tr * a.H + h] : 1.f;
-        const bool none = mx == -INFINITY && l == 0.f;
-        reinterpret_cast<f32x4*>(to + Lds::kRow)[row] =
-            f32x4{none ? INFINITY : mx, none ? 0.f : 1.f / l, none ? 0.f : D,
-                  __int_as_float(a.placed && m > 0 ? a.tgt_pos[tr] : 0)};
+    for (int n = 0; n < kFetch; ++n) {
+      const int i = tid + n * kThreads, piece = i % kPieces, at = i / kPieces, hd = at / (16 * MT), row = at % (16 * MT);
+      if (hd < a.hw) {
+        unsigned char* to = smem + Lds::kTables + hd * Lds::kHead + row * kRowBytes<T, DH> + 16 * piece;
+        *reinterpret_cast<uint4*>(to) = fq[n];
+        *reinterpret_cast<uint4*>(to + Lds::kDo) = fd[n];
+        if (a.placed) odd_rows |= odd16<T>(fq[n]) || odd16<T>(fd[n]);
       }
     }
+    if (tid < 16 * MT * a.hw)
+      reinterpret_cast<f32x4*>(smem + Lds::kTables + tid / (16 * MT) * Lds::kHead + Lds::kRow)[tid % (16 * MT)] = frow;
+    if (pass + 1 < passes) fetch(pass + 1);
     if (nb)
-      for (int i = tid; i < kWaves * (slots + 1) * copies; i += kThreads) s_bins[i] = 0.f;
+      for (int i = 4 * tid; i < kWaves * (slots + 1) * copies; i += 4 * kThreads)
+        *reinterpret_cast<f32x4*>(s_bins + i) = f32x4{};
     odd_rows = __syncthreads_or(odd_rows);
 
     // this lane's target of each tile: its constants, the bucket it keeps
@@ -331,48 +375,24 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(EUB)))
     // each wave takes consecutive steps (a lane's bucket changes seldom then)
     const int steps = (j1 - j0 + BJ - 1) / BJ, share = (steps + parts - 1) / parts;
     const int jfirst = j0 + part * share * BJ, jstop = min(j1, jfirst + share * BJ);
-    E8 kf[JT][KS], vf[JT][KS];  // the step's rows, or the next one's once they are used
-    int pj[JT][4];              // positions of rows 4 g4 + i
-    const uint32_t lk = static_cast<uint32_t>(a.ldk * sizeof(T)), lv = static_cast<uint32_t>(a.ldv * sizeof(T));
-    auto load = [&](int jb) {
-      const int last = len - 1 - jb;
-      const gptr kp = uniform(static_cast<const T*>(a.k) + (h0 + jb) * a.ldk + g * DH);
-      const gptr vp = uniform(static_cast<const T*>(a.v) + (h0 + jb) * a.ldv + g * DH);
-#pragma unroll
-      for (int jt = 0; jt < JT; ++jt) {
-        const int jr = min(16 * jt + c16, last);
-        const uint32_t ak = __umul24(jr, lk) + 8 * g4 * sizeof(T), av = __umul24(jr, lv) + 8 * g4 * sizeof(T);
-#pragma unroll
-        for (int s = 0; s < KS; ++s) {
-          kf[jt][s] = load8_at<T>(kp + 32 * s * sizeof(T), ak);
-          vf[jt][s] = load8_at<T>(vp + 32 * s * sizeof(T), av);
-        }
-      }
-      if (a.hist_pos) {
-        const gptr hp = uniform(a.hist_pos + h0 + jb);
+    if (jfirst < min(jstop, single ? j1 : jend) && (pass == 0 || !single)) load(jfirst);
+    for (int jb = jfirst; jb < jstop; jb += BJ) {
+      const int64_t acc_at = ((h0 + jb) * a.Hk + g) * DH;  // fp32 sums of the earlier passes: row jt 16 + c16
+      const int64_t acc_v = a.n_hist * a.Hk * DH;
+      if (pass == 0 || !single) {
 #pragma unroll
         for (int jt = 0; jt < JT; ++jt)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) pj[jt][i] = load_at<int>(hp, 4u * min(16 * jt + 4 * g4 + i, last));
-      }
-    };
-    if (jfirst < min(jstop, jend)) load(jfirst);
-    for (int jb = jfirst; jb < jstop; jb += BJ) {
-      f32x4 dk[JT][NE], dv[JT][NE];
-      const int64_t acc_at = ((h0 + jb) * a.Hk + g) * DH;  // fp32 sums of the earlier passes: row jt 16 + c16
-      const int64_t acc_v = a.n_hist * a.Hk * DH;
-#pragma unroll
-      for (int jt = 0; jt < JT; ++jt)
-#pragma unroll
-        for (int e = 0; e < NE; ++e) {
-          dk[jt][e] = dv[jt][e] = f32x4{};
-          const int j = 16 * jt + c16;
-          if (pass > 0 && jb + j < j1) {
-            const float* p = a.acc_kv + acc_at + static_cast<int64_t>(j) * a.Hk * DH + 4 * (NE * g4 + e);
-            dk[jt][e] = *reinterpret_cast<const f32x4*>(p);
-            dv[jt][e] = *reinterpret_cast<const f32x4*>(p + acc_v);
+          for (int e = 0; e < NE; ++e) {
+            dk[jt][e] = dv[jt][e] = f32x4{};
+            const int j = 16 * jt + c16;
+            if (pass > 0 && jb + j < j1) {
+              const float* p = a.acc_kv + acc_at + static_cast<int64_t>(j) * a.Hk * DH + 4 * (NE * g4 + e);
+              dk[jt][e] = *reinterpret_cast<const f32x4*>(p);
+              dv[jt][e] = *reinterpret_cast<const f32x4*>(p + acc_v);
+            }
           }
-        }
+      }
       if (jb < jend) {
         // K in the other order: rows of the step along the operand
         bool odd_k = false;
@@ -410,7 +430,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(EUB)))
 #pragma unroll
             for (int s = 0; s < KS; ++s) odd_k |= odd8<T>(kf[jt][s]);
         }
-        if (jb + BJ < min(jstop, jend)) load(jb + BJ);
+        if (!single && jb + BJ < min(jstop, jend)) load(jb + BJ);
         F4 kc[JT][NE];
         __builtin_amdgcn_wave_barrier();
 #pragma unroll
@@ -617,6 +637,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(EUB)))
         const int j = 16 * jt + c16;
         if (jb + j >= j1) continue;
         if (pass + 1 < passes) {
+          if (single) continue;
           float* p = a.acc_kv + acc_at + static_cast<int64_t>(j) * a.Hk * DH + 4 * NE * g4;
 #pragma unroll
           for (int e = 0; e < NE; ++e) {
@@ -683,6 +704,33 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(EUB)))
   }
 }
 
+// Per target and head what every chunk's workgroups need: the forward's maximum,
+// 1 / its sum, D = dout . out and the position.  A row that sees nothing has an
+// infinite maximum, and so no weight anywhere.
+template <typename T, int DH>
+__global__ __launch_bounds__(256) void attn_bwd_rows_kernel(const AttnArgs a) {
+  constexpr int NE = DH / 16;
+  if (blockIdx.x == gridDim.x - 1) {
+    check_call(a, false);
+    return;
+  }
+  const int64_t row = static_cast<int64_t>(blockIdx.x) * 16 + (threadIdx.x >> 4);
+  if (row >= a.n_tgt * a.H) return;
+  const int f = (threadIdx.x & 15) * NE;
+  float D = 0.f;
+#pragma unroll
+  for (int e = 0; e < NE; ++e)
+    D += to_f32(static_cast<const T*>(a.dout)[row * DH + f + e]) * a.fa[row * DH + f + e];
+#pragma unroll
+  for (int o = 1; o < 16; o <<= 1) D += __shfl_xor(D, o);
+  if (f == 0) {
+    const float mx = a.fm[row], l = a.fl[row];
+    const bool none = mx == -INFINITY && l == 0.f;
+    reinterpret_cast<f32x4*>(a.rows)[row] = f32x4{none ? INFINITY : mx, none ? 0.f : 1.f / l, none ? 0.f : D,
+                                                  __int_as_float(a.placed ? a.tgt_pos[row / a.H] : 0)};
+  }
+}
+
 // The chunks' dq (one row per 16 lanes) and the units' dbias (one bucket per
 // thread column, 16 unit strides), each summed in a fixed order.
 template <typename T, int DH>
@@ -730,9 +778,12 @@ hipError_t launch_bwd(const AttnArgs& a, hipStream_t st) {
 #endif
   constexpr int JT = DH == 128 ? 1 : JTB;
   const size_t lds = BwdLds<T, DH, MT, JT>::bytes(a.hw, a.G, a.b.n, bin_copies(a.b.n));
-  const int64_t grid = round_up(a.units, kXcds) * (a.Hk / a.hw) + 1;
-  if (grid > 0x7fffffff) return hipErrorInvalidValue;
+  const int64_t grid = round_up(a.units, kXcds) * (a.Hk / a.hw), rows = ceil_div(a.n_tgt * a.H, 16) + 1;
+  if (grid > 0x7fffffff || rows > 0x7fffffff) return hipErrorInvalidValue;
   hipError_t e = allow_lds<&attn_bwd_kernel<T, DH, MT, JT>>(lds);
+  if (e != hipSuccess) return e;
+  attn_bwd_rows_kernel<T, DH><<<static_cast<unsigned>(rows), 256, 0, st>>>(a);
+  e = hipGetLastError();
   if (e != hipSuccess) return e;
   attn_bwd_kernel<T, DH, MT, JT><<<static_cast<unsigned>(grid), kThreads, lds, st>>>(a);
   e = hipGetLastError();
@@ -765,7 +816,16 @@ hipError_t backward_t(const AttnArgs& a, int dh, int tiles, hipStream_t st) {
 // Row tiles a wave holds: the fewest that take a request's tiles in one pass,
 // up to what registers (dq, DH / 16 x 4 a tile) and LDS allow.
 int backward_tiles(int dtype, int dh, int need) {
-  const int most = dtype == STCA_BF16 ? (dh == 128 ? 2 : 4) : (dh == 128 ? 1 : 2);
+#ifndef BT64
+#define BT64 1
+#endif
+#ifndef BT32
+#define BT32 4
+#endif
+#ifndef BT128
+#define BT128 1
+#endif
+  const int most = dtype == STCA_BF16 ? (dh == 128 ? BT128 : dh == 64 ? BT64 : BT32) : (dh == 128 ? 1 : 2);
   return need >= 3 && most == 4 ? 4 : need >= 2 && most >= 2 ? 2 : 1;
 }
 

@@ -116,11 +116,19 @@ __device__ __forceinline__ bool odd_bf16(uint32_t w) {  // a half of w is not fi
   return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u;
 }
 
-#ifndef EU
-#define EU 2
+// Waves a SIMD is to hold: what the registers of a block, its output and its
+// rows allow without spills.
+#ifndef EU64
+#define EU64 2
 #endif
+#ifndef EU128
+#define EU128 1
+#endif
+template <typename T, int DH, int MT>
+constexpr int kFwdWaves = DH == 128 ? EU128 : DH == 64 && MT > 1 ? EU64 : 2;
+
 template <typename T, int KV, int DH, int MT>
-__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(EU))) void attn_fwd_kernel(const AttnArgs a) {
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kFwdWaves<T, DH, MT>))) void attn_fwd_kernel(const AttnArgs a) {
   constexpr bool kF32 = !Elem<T>::bf16;
   constexpr bool kPaged = KV != kRagged;
   constexpr int NT = kTilesOf<KV>;

@@ -15,7 +15,7 @@ constexpr int kMaxBuckets = 128;
 constexpr int kMaxGroup = 64;     // query heads per kv head
 constexpr int kWaves = 4;         // waves per workgroup of the attention kernels
 constexpr int kThreads = 64 * kWaves;
-constexpr int kChunkStep = 256;   // chunk lengths are multiples of this: a chunk starts on a page
+constexpr int kPageStep = 256;    // a cache's chunk lengths are multiples of this: a chunk starts on a page
 constexpr int kXcds = 8;          // workgroup i runs on XCD i % 8
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
@@ -65,6 +65,7 @@ struct AttnArgs {
   void *dq, *dk, *dv;
   int64_t lddq, lddk, lddv;
   float *dbias, *part_dq, *part_db, *acc_kv;
+  float* rows;                     // per target and head: maximum, 1 / sum, D, position (attn_bwd.hip)
   WsHeader* hdr;
   Buckets b;
 };
@@ -261,28 +262,35 @@ __device__ __forceinline__ void set_status(WsHeader* hdr, int bad) {
   hdr->range = 0;
 }
 
+// Entries [i0, i1) of request r's row of a table of pages, for a share of the
+// threads: nonzero if one is outside the pages.
+__device__ __forceinline__ int check_pages(const int32_t* table, int64_t row, int i0, int i1, int step, int n_pages) {
+  int bad = 0;
+#pragma unroll 4
+  for (int i = i0; i < i1; i += step) {
+    const int p = table[row + i];
+    bad |= p < 0 || p >= n_pages;
+  }
+  return bad;
+}
+
 // The whole of a call's device offsets, lengths and pages as its status: one
-// workgroup of its own, the only writer of the status word.
+// workgroup of its own, the only writer of the status word.  As many threads a
+// request as there are (a wave a request took 0.3 us for each of them).
 __device__ __forceinline__ void check_call(const AttnArgs& a, bool paged) {
   int bad = 0;
-  for (int r = threadIdx.x; r < a.R; r += blockDim.x) {
+  const int per = max(1, static_cast<int>(blockDim.x) / a.R), sub = threadIdx.x % per;
+  for (int r = threadIdx.x / per; r < a.R; r += blockDim.x / per) {
     bad |= a.tgt_off[r + 1] < a.tgt_off[r] || (r == 0 && a.tgt_off[0] != 0) ||
            (r == a.R - 1 && a.tgt_off[a.R] != a.n_tgt);
     if (paged) {
-      bad |= a.lens[r] < 0 || a.lens[r] > a.max_len;
+      const int len = a.lens[r];
+      bad |= len < 0 || len > a.max_len;
+      const int n = (min(max(len, 0), a.max_len) + (1 << a.page_shift) - 1) >> a.page_shift;
+      bad |= check_pages(a.table, static_cast<int64_t>(r) * a.table_ld, sub, n, per, a.n_pages);
     } else {
       bad |= a.hist_off[r + 1] < a.hist_off[r] || (r == 0 && a.hist_off[0] != 0) ||
              (r == a.R - 1 && a.hist_off[a.R] != a.n_hist);
-    }
-  }
-  if (paged) {
-    const int lane = threadIdx.x & 63, waves = blockDim.x >> 6;
-    for (int r = threadIdx.x >> 6; r < a.R; r += waves) {
-      const int n = (min(max(a.lens[r], 0), a.max_len) + (1 << a.page_shift) - 1) >> a.page_shift;
-      for (int i = lane; i < n; i += 64) {
-        const int p = a.table[static_cast<int64_t>(r) * a.table_ld + i];
-        bad |= p < 0 || p >= a.n_pages;
-      }
     }
   }
   bad = __syncthreads_or(bad);

@@ -61,24 +61,22 @@ __device__ __forceinline__ int page_of(const CacheArgs& a, int r, int pos) {
 }
 
 __device__ void check_rows(const CacheArgs& a) {
+  if (!a.hdr) return;
   int bad = 0;
-  for (int r = threadIdx.x >> 6; r < a.R; r += blockDim.x >> 6) {
+  const int per = max(1, static_cast<int>(blockDim.x) / a.R), sub = threadIdx.x % per;
+  for (int r = threadIdx.x / per; r < a.R; r += blockDim.x / per) {
     const int o0 = a.row_off[r], o1 = a.row_off[r + 1];
     const int64_t start = a.start[r], end = start + o1 - o0;
-    bad |= o1 < o0 || start < 0 || (r == 0 && o0 != 0) || (r == a.R - 1 && o1 != a.n_rows) || end > 0x7fffffff - kSlots;
-    if (bad || o1 == o0) continue;
-    const int i1 = static_cast<int>((end - 1) >> a.page_shift);
-    if (i1 >= a.table_ld) {
-      bad = 1;
-      continue;
-    }
-    for (int i = static_cast<int>(start >> a.page_shift) + (threadIdx.x & 63); i <= i1; i += 64) {
-      const int p = a.table[static_cast<int64_t>(r) * a.table_ld + i];
-      bad |= p < 0 || p >= a.n_pages;
-    }
+    const bool odd = o1 < o0 || start < 0 || (r == 0 && o0 != 0) || (r == a.R - 1 && o1 != a.n_rows) ||
+                     end > 0x7fffffff - kSlots;
+    bad |= odd;
+    if (odd || o1 == o0) continue;
+    const int i0 = static_cast<int>(start >> a.page_shift), i1 = static_cast<int>((end - 1) >> a.page_shift) + 1;
+    bad |= i1 > a.table_ld;
+    bad |= check_pages(a.table, static_cast<int64_t>(r) * a.table_ld, i0 + sub, min(i1, a.table_ld), per, a.n_pages);
   }
   bad = __syncthreads_or(bad);
-  if (threadIdx.x == 0 && a.hdr) set_status(a.hdr, bad);
+  if (threadIdx.x == 0) set_status(a.hdr, bad);
 }
 
 template <typename T, int N>
