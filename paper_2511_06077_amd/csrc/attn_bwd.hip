@@ -205,6 +205,7 @@ template <typename T, int DH, int MT, int JT>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kBwdWaves<T, DH, MT>))) void attn_bwd_kernel(const AttnArgs a) {
   constexpr bool kBf16 = Elem<T>::bf16;
   constexpr int KS = DH / 32, NE = DH / 16, BJ = 16 * JT;
+  static_assert(JT == 1, "a lane's rows are one run of four");
   using F4 = typename Four<T>::type;
   using E8 = Eight<T>;
   using Lds = BwdLds<T, DH, MT, JT>;
@@ -238,8 +239,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kBwdWa
   const int t0 = uniform(clamp_off(a.tgt_off[r], a.n_tgt)), m = max(0, uniform(clamp_off(a.tgt_off[r + 1], a.n_tgt)) - t0);
   const int ttiles = (m + 15) / 16, groups = (ttiles + MT - 1) / MT;  // groups of MT tiles of one head
 
-  BucketLds bl{};
-  if (a.placed) bl = fill_buckets(a, g0, heads, s_cells, s_bias, s_edges);
+  const BucketLds bl{s_cells, s_bias, s_edges, slots, a.b.multi};  // (pointers that are known to be LDS)
+  if (a.placed) fill_buckets(a, g0, heads, s_cells, s_bias, s_edges);
   for (int i = tid; i < heads * nb; i += kThreads) s_db[i] = 0.f;
   unsigned char* mine = smem + Lds::kTables + hs * Lds::kHead;  // q, dout and rows of this wave's head
   const float* s_row = reinterpret_cast<const float*>(mine + Lds::kRow);
@@ -456,32 +457,44 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kBwdWa
               __ballot(tail || (a.placed && (place_of(tp[mt], pmax) < blo[mt] || place_of(tp[mt], pmin) > bhi[mt]))) != 0;
           uint32_t hid = 0;  // bit 4 jt + i
           float w[JT][4], dz[JT][4], dx[JT][4];
-          int kk[JT][4];
+          // (JT = 1) a lane's rows in two buckets at most, or each in its own
+          int kk[4];
+          TwoBuckets two{0, 0, 0};
+          bool each = false;
           if (slow) {
+            const float* hb = bl.bias + (hs * a.G + hh) * (slots + 1);
+            if (a.placed) {
+              each = __ballot(!two_buckets(bl, place_of(tp[mt], pmax), place_of(tp[mt], pmin), two)) != 0;
+              if (!each) {
+                const float near = hb[two.near], far = hb[two.far];
 #pragma unroll
-            for (int jt = 0; jt < JT; ++jt) {
-              int at[4];
-              int2 cell[4];
-              if (a.placed) {
+                for (int i = 0; i < 4; ++i) dx[0][i] = sub_sat(tp[mt], pos[0][i]) >= two.edge ? far : near;
+              } else {
+                int at[4];
+                int2 cell[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                  at[i] = place_of(tp[mt], pos[jt][i]);
+                  at[i] = place_of(tp[mt], pos[0][i]);
                   cell[i] = bl.cells[cell_of(at[i])];
                 }
-              }
 #pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                kk[jt][i] = a.placed ? bucket_in(bl, at[i], cell[i]) : 0;
-                dx[jt][i] = a.placed ? bl.bias[(hs * a.G + hh) * (slots + 1) + kk[jt][i]] : 0.f;
-                if (jb + 16 * jt + 4 * g4 + i >= jend) dx[jt][i] = -INFINITY;
-                hid |= dx[jt][i] == -INFINITY ? 1u << (4 * jt + i) : 0u;
+                for (int i = 0; i < 4; ++i) {
+                  kk[i] = bucket_in(bl, at[i], cell[i]);
+                  dx[0][i] = hb[kk[i]];
+                }
               }
+            } else {
+#pragma unroll
+              for (int i = 0; i < 4; ++i) dx[0][i] = 0.f;
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              if (tail && jb + 4 * g4 + i >= jend) dx[0][i] = -INFINITY;
+              hid |= dx[0][i] == -INFINITY ? 1u << i : 0u;
             }
           } else {
 #pragma unroll
-            for (int jt = 0; jt < JT; ++jt)
-#pragma unroll
-              for (int i = 0; i < 4; ++i) dx[jt][i] = bias[mt];
+            for (int i = 0; i < 4; ++i) dx[0][i] = bias[mt];
           }
 #pragma unroll
           for (int jt = 0; jt < JT; ++jt)
@@ -502,34 +515,29 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kBwdWa
             }
           if (nb) {
             if (!slow) {
-#pragma unroll
-              for (int jt = 0; jt < JT; ++jt) dsum[mt] += (dx[jt][0] + dx[jt][1]) + (dx[jt][2] + dx[jt][3]);
+              dsum[mt] += (dx[0][0] + dx[0][1]) + (dx[0][2] + dx[0][3]);
             } else {
+              // what the lane has kept so far goes along where it can
+              if (!each) {
+                float near = 0.f, far = 0.f;
 #pragma unroll
-              for (int jt = 0; jt < JT; ++jt) {
-                const int ka = kk[jt][0], kb = kk[jt][3];
-                const bool two = (kk[jt][1] == ka || kk[jt][1] == kb) && (kk[jt][2] == ka || kk[jt][2] == kb);
-                if (__ballot(!two) == 0) {
-                  float va = dx[jt][0], vb = 0.f;
-#pragma unroll
-                  for (int i = 1; i < 4; ++i) {
-                    va += kk[jt][i] == ka ? dx[jt][i] : 0.f;
-                    vb += kk[jt][i] == ka ? 0.f : dx[jt][i];
-                  }
-                  // (what the lane has kept so far goes with them)
-                  if (jt == 0 && __ballot(dsum[mt] != 0.f && bk[mt] != ka) == 0) {
-                    va += dsum[mt];
-                    dsum[mt] = 0.f;
-                  }
-                  add_bins(ka, va, kb == ka ? -1 : kb, vb);
-                } else {
-                  add_bins(ka, dx[jt][0], kk[jt][1], dx[jt][1]);
-                  add_bins(kk[jt][2], dx[jt][2], kb, dx[jt][3]);
+                for (int i = 0; i < 4; ++i) {
+                  const bool is_far = sub_sat(tp[mt], pos[0][i]) >= two.edge;
+                  far += is_far ? dx[0][i] : 0.f;
+                  near += is_far ? 0.f : dx[0][i];
                 }
+                if (__ballot(dsum[mt] != 0.f && bk[mt] != two.far) == 0) {
+                  far += dsum[mt];
+                  dsum[mt] = 0.f;
+                }
+                add_bins(two.far, far, two.near == two.far ? -1 : two.near, near);
+              } else {
+                add_bins(kk[0], dx[0][0], kk[1], dx[0][1]);
+                add_bins(kk[2], dx[0][2], kk[3], dx[0][3]);
               }
               if (__ballot(dsum[mt] != 0.f)) add_bins(bk[mt], dsum[mt], -1, 0.f);
               dsum[mt] = 0.f;
-              bk[mt] = kk[JT - 1][3];
+              bk[mt] = each ? kk[3] : two.near;
               bias[mt] = bl.bias[(hs * a.G + hh) * (slots + 1) + bk[mt]];
               keep_bucket(bl, a.masked, bk[mt], bias[mt], blo[mt], bhi[mt]);
             }

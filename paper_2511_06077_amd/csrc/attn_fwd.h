@@ -179,8 +179,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kFwdWa
   int j1 = min(len, j0 + a.chunk);
 
   // tables
-  BucketLds bl{};
-  if (a.placed) bl = fill_buckets(a, g0, a.hw * a.G, s_cells, s_bias, s_edges);
+  // (pointers that are known to be LDS: set whether used or not)
+  const BucketLds bl{s_cells, s_bias, s_edges, max(a.b.n, 1), a.b.multi};
+  if (a.placed) fill_buckets(a, g0, a.hw * a.G, s_cells, s_bias, s_edges);
   bool holes = false;
   if constexpr (kPaged) {
     const int p0 = j0 >> a.page_shift, p1 = (j1 + (1 << a.page_shift) - 1) >> a.page_shift;
@@ -396,47 +397,60 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kFwdWa
       // the block's registers are free: the next one is on its way from here on
       if (more) load(b, jb + BJ);
       const bool tail = jb + BJ > jend || holes;
+      // a score's factor before the cap, or its whole gain; an 8-bit row's step in it
+      float row_gain[KV == kPagedInt8 ? NJ : 1];
+      if constexpr (KV == kPagedInt8) {
+#pragma unroll
+        for (int i = 0; i < NJ; ++i) row_gain[i] = exp_byte(word(kexp, i / 4), i % 4) * (a.cap > 0.f ? cap_in : gain);
+      } else {
+        row_gain[0] = a.cap > 0.f ? cap_in : gain;
+      }
+      auto gain_of = [&](int i) { return a.cap > 0.f ? gain : row_gain[KV == kPagedInt8 ? i : 0]; };
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt) {
         // biases, in units of log2 e as the scores
         float x[NJ];
         uint32_t hid = 0;
         const bool slow = __ballot(tail || place_of(tpos[mt], pmax) < blo[mt] || place_of(tpos[mt], pmin) > bhi[mt]) != 0;
-        if constexpr (KV == kPagedInt8) {
-#pragma unroll
-          for (int i = 0; i < NJ; ++i) S[mt][i / 4][i % 4] *= exp_byte(word(kexp, i / 4), i % 4);
-        }
         if (a.cap > 0.f) {
 #pragma unroll
           for (int i = 0; i < NJ; ++i) {
-            const float y = S[mt][i / 4][i % 4] * cap_in;
+            const float y = S[mt][i / 4][i % 4] * row_gain[KV == kPagedInt8 ? i : 0];
             S[mt][i / 4][i % 4] = kF32 ? tanhf(y) : tanh_fast(y);
           }
         }
         if (!slow) {
 #pragma unroll
-          for (int i = 0; i < NJ; ++i) x[i] = fmaf(S[mt][i / 4][i % 4], gain, bias[mt]);
+          for (int i = 0; i < NJ; ++i) x[i] = fmaf(S[mt][i / 4][i % 4], gain_of(i), bias[mt]);
         } else {
           if (a.placed) {
-            int k = 0;
-            float bk = 0.f;
+            TwoBuckets two;
+            int k;
+            if (__ballot(!two_buckets(bl, place_of(tpos[mt], pmax), place_of(tpos[mt], pmin), two)) == 0) {
+              const float near = bl.bias[hbias[mt] + two.near], far = bl.bias[hbias[mt] + two.far];
 #pragma unroll
-            for (int i4 = 0; i4 < NJ; i4 += 4) {
-              int at[4];
-              int2 cell[4];
+              for (int i = 0; i < NJ; ++i) x[i] = sub_sat(tpos[mt], pj[i]) >= two.edge ? far : near;
+              k = two.near;
+              bias[mt] = near;
+            } else {
 #pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                at[i] = place_of(tpos[mt], pj[i4 + i]);
-                cell[i] = bl.cells[cell_of(at[i])];
-              }
+              for (int i4 = 0; i4 < NJ; i4 += 4) {
+                int at[4];
+                int2 cell[4];
 #pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                k = bucket_in(bl, at[i], cell[i]);
-                x[i4 + i] = bk = bl.bias[hbias[mt] + k];
+                for (int i = 0; i < 4; ++i) {
+                  at[i] = place_of(tpos[mt], pj[i4 + i]);
+                  cell[i] = bl.cells[cell_of(at[i])];
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                  k = bucket_in(bl, at[i], cell[i]);
+                  x[i4 + i] = bias[mt] = bl.bias[hbias[mt] + k];
+                }
               }
             }
-            bias[mt] = bk;  // the lane keeps its last row's bucket
-            keep_bucket(bl, a.masked, k, bk, blo[mt], bhi[mt]);
+            // the lane keeps one of its buckets: its nearest rows', or its last row's
+            keep_bucket(bl, a.masked, k, bias[mt], blo[mt], bhi[mt]);
           } else {
 #pragma unroll
             for (int i = 0; i < NJ; ++i) x[i] = 0.f;
@@ -455,7 +469,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kFwdWa
 #pragma unroll
           for (int i = 0; i < NJ; ++i) {
             hid |= x[i] == -INFINITY ? 1u << i : 0u;
-            const float y = fmaf(S[mt][i / 4][i % 4], gain, x[i]);
+            const float y = fmaf(S[mt][i / 4][i % 4], gain_of(i), x[i]);
             x[i] = x[i] == -INFINITY ? x[i] : y;
           }
           if (!__ballot(hid != (1u << NJ) - 1u)) continue;  // nothing of this block is seen

@@ -181,7 +181,7 @@ __device__ __forceinline__ float scaled_bias(float b) {
 }
 
 // Fills the tables (threads of the whole workgroup; a barrier follows).
-__device__ __forceinline__ BucketLds fill_buckets(const AttnArgs& a, int g, int heads, int2* cells, float* bias, int32_t* edges) {
+__device__ __forceinline__ void fill_buckets(const AttnArgs& a, int g, int heads, int2* cells, float* bias, int32_t* edges) {
   const int n = a.b.n, slots = max(n, 1);
   for (int i = threadIdx.x; i < kCells; i += blockDim.x) {
     const int k = i == kHiddenCell && a.masked ? slots : a.b.cell[i];
@@ -192,7 +192,6 @@ __device__ __forceinline__ BucketLds fill_buckets(const AttnArgs& a, int g, int 
     bias[i] = k < n ? scaled_bias(a.bias[(static_cast<int64_t>(g) * a.G + h) * n + k]) : k == slots ? -INFINITY : 0.f;
   }
   for (int i = threadIdx.x; i < slots; i += blockDim.x) edges[i] = a.b.edges[i];
-  return BucketLds{cells, bias, edges, slots, a.b.multi};
 }
 
 // x of a distance and its cell
@@ -208,6 +207,20 @@ __device__ __forceinline__ int bucket_in(const BucketLds& b, int x, int2 cell) {
   if (b.multi && x > 0)
     while (k < b.slots - 1 && x > b.edges[k]) ++k;
   return k;
+}
+// A lane's rows may lie in two neighbouring buckets at most: `far` for distances
+// from `edge` on, else `near`.  Tells whether they do, from their least and
+// greatest x; one look-up each instead of one a row.
+struct TwoBuckets {
+  int near, far, edge;
+};
+__device__ __forceinline__ bool two_buckets(const BucketLds& b, int xmin, int xmax, TwoBuckets& t) {
+  const int2 cn = b.cells[cell_of(xmin)], cf = b.cells[cell_of(xmax)];
+  t.near = bucket_in(b, xmin, cn);
+  t.far = bucket_in(b, xmax, cf);
+  t.edge = t.far == t.near + 1 && t.near < b.slots ? b.edges[t.near] : -2147483647 - 1;
+  // (hidden rows have the bucket after the last: all of them or none)
+  return t.far == t.near || (t.far == t.near + 1 && t.far < b.slots);
 }
 // Distances (as x) of a bucket, for a lane that keeps it: none if it is hidden.
 __device__ __forceinline__ void keep_bucket(const BucketLds& b, bool masked, int k, float bias, int& lo, int& hi) {
