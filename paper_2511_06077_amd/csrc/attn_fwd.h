@@ -41,10 +41,9 @@ namespace ops {
 constexpr int kRagged = 0, kPagedBf16 = 1, kPagedInt8 = 2;
 constexpr float kSlack = 8.f;  // 2^8: sums and products stay far inside fp32 and bf16 ranges
 
-#ifndef NTR
-#define NTR 2
+#ifndef EU8
+#define EU8 2
 #endif
-template <int KV> constexpr int kTilesOf = KV == kPagedInt8 ? 4 : KV == kPagedBf16 ? 2 : NTR;
 
 // LDS of a workgroup before the dynamic part's tables.
 template <int DH> constexpr int kCombineFloats = kWaves * 16 * (DH + 2);
@@ -61,8 +60,8 @@ struct Block {
   uint2 k8[KV == kPagedInt8 ? NT : 1][KV == kPagedInt8 ? KS : 1];
   // V as loaded
   uint32_t vw[KV == kRagged ? NJ : 1][KV == kRagged ? (kF32 ? NE : NE / 2) : 1];
-  uint4 vp[KV == kRagged ? 1 : NE];
-  uint4 ke, ve;                        // 16 exponents each
+  uint32_t vp[KV == kRagged ? 1 : NE][NJ / (KV == kPagedInt8 ? 4 : 2)];
+  uint32_t ke[NJ / 4], ve[NJ / 4];     // exponents
   int pj[NJ];                          // positions, where the rows have some
 };
 
@@ -83,6 +82,22 @@ __device__ __forceinline__ void load_words(gptr base, uint32_t at, uint32_t* w) 
     w[1] = x[1];
   } else {
     w[0] = load_at<uint32_t>(base, at);
+  }
+}
+
+// N words (2 or 4, aligned to all of them).
+template <int N>
+__device__ __forceinline__ void copy_words(const void* p, uint32_t* w) {
+  if constexpr (N == 4) {
+    const uint4 x = *static_cast<const uint4*>(p);
+    w[0] = x.x;
+    w[1] = x.y;
+    w[2] = x.z;
+    w[3] = x.w;
+  } else {
+    const uint2 x = *static_cast<const uint2*>(p);
+    w[0] = x.x;
+    w[1] = x.y;
   }
 }
 
@@ -107,10 +122,31 @@ __device__ __forceinline__ bf16x8 int8_bf16(uint32_t a, uint32_t b) {
   }
   return __builtin_bit_cast(bf16x8, make_uint4(r[0], r[1], r[2], r[3]));
 }
-__device__ __forceinline__ float exp_byte(uint32_t w, int k) {  // 2^(byte - 127); 255: infinity
-  return __uint_as_float(((w >> (8 * k)) & 0xffu) << 23);
+// 2^(byte k - 127), byte 255 infinity, in one instruction (the compiler takes a
+// shift and a mask).
+template <int K>
+__device__ __forceinline__ float exp_byte(uint32_t w) {
+  uint32_t r;
+  const uint32_t n = 23;
+  if constexpr (K == 0)
+    asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_0" : "=v"(r) : "v"(n), "v"(w));
+  else if constexpr (K == 1)
+    asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_1" : "=v"(r) : "v"(n), "v"(w));
+  else if constexpr (K == 2)
+    asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_2" : "=v"(r) : "v"(n), "v"(w));
+  else
+    asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_3" : "=v"(r) : "v"(n), "v"(w));
+  return __uint_as_float(r);
 }
-__device__ __forceinline__ uint32_t word(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
+__device__ __forceinline__ void exp_bytes(const uint32_t (&w)[2], float (&f)[8]) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    f[4 * i] = exp_byte<0>(w[i]);
+    f[4 * i + 1] = exp_byte<1>(w[i]);
+    f[4 * i + 2] = exp_byte<2>(w[i]);
+    f[4 * i + 3] = exp_byte<3>(w[i]);
+  }
+}
 
 __device__ __forceinline__ bool odd_bf16(uint32_t w) {  // a half of w is not finite
   return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u;
@@ -124,14 +160,14 @@ __device__ __forceinline__ bool odd_bf16(uint32_t w) {  // a half of w is not fi
 #ifndef EU128
 #define EU128 1
 #endif
-template <typename T, int DH, int MT>
-constexpr int kFwdWaves = DH == 128 ? EU128 : DH == 64 && MT > 1 ? EU64 : 2;
+template <typename T, int KV, int DH, int MT>
+constexpr int kFwdWaves = KV == kPagedInt8 ? EU8 : DH == 128 ? EU128 : DH == 64 && MT > 1 ? EU64 : 2;
 
 template <typename T, int KV, int DH, int MT>
-__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kFwdWaves<T, DH, MT>))) void attn_fwd_kernel(const AttnArgs a) {
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kFwdWaves<T, KV, DH, MT>))) void attn_fwd_kernel(const AttnArgs a) {
   constexpr bool kF32 = !Elem<T>::bf16;
   constexpr bool kPaged = KV != kRagged;
-  constexpr int NT = kTilesOf<KV>;
+  constexpr int NT = 2;
   constexpr int BJ = 16 * NT;
   constexpr int KS = DH / 32, NE = DH / 16, NJ = 4 * NT;
   using Blk = Block<T, KV, DH, NT>;
@@ -281,34 +317,37 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kFwdWa
           for (int i = 0; i < NJ; ++i) b.pj[i] = load_at<int>(hp, 4u * min(NJ * g4 + i, last));
         }
       } else {
+        // The NJ rows of a lane's V operand lie in one page, and so do those of
+        // its K operand's tiles.  Past the end: the last run's, which exists.
         const int P = 1 << a.page_shift, ps = a.page_shift, p0 = j0 >> ps;
-        constexpr int ES = KV == kPagedInt8 ? 1 : 2;
+        constexpr uint32_t ES = KV == kPagedInt8 ? 1 : 2;
+        auto run = [&](int i) { return min(jb + NJ * i, (len - 1) & ~(NJ - 1)); };
+        auto page_at = [&](int j) { return static_cast<uint32_t>(max(s_table[(j >> ps) - p0], 0)); };
+        const uint32_t head_rows = static_cast<uint32_t>(a.Hk) << ps;  // rows of a page, all heads
+        const int jk = run(c16 >> 2), jv = run(g4);
+        const char* kp = static_cast<const char*>(a.k) + (static_cast<int64_t>(g) << ps) * (DH * ES) +
+                         static_cast<uint64_t>(page_at(jk)) * (head_rows * (DH * ES)) +
+                         ((jk & (P - 1)) + (c16 & 3)) * (DH * ES);
 #pragma unroll
-        for (int i = 0; i < NT; ++i) {
-          const int j = jb + min(NJ * (c16 >> 2) + 4 * i + (c16 & 3), last);
-          const int64_t page = max(s_table[(j >> ps) - p0], 0);
-          const char* p = static_cast<const char*>(a.k) + ((page * a.Hk + g) * P + (j & (P - 1))) * (DH * ES);
+        for (int i = 0; i < NT; ++i)
 #pragma unroll
           for (int s = 0; s < KS; ++s) {
-            if constexpr (KV == kPagedInt8) {
-              b.k8[i][s] = *reinterpret_cast<const uint2*>(p + feature<KV, DH>(s, g4));
-            } else {
-              b.kb[i][s] = *reinterpret_cast<const bf16x8*>(p + 2 * feature<KV, DH>(s, g4));
-            }
+            const char* p = kp + 4 * i * DH * ES + feature<KV, DH>(s, g4) * ES;
+            if constexpr (KV == kPagedInt8) b.k8[i][s] = *reinterpret_cast<const uint2*>(p);
+            else b.kb[i][s] = *reinterpret_cast<const bf16x8*>(p);
           }
-        }
-        // this lane group's NJ rows lie in one page
-        const int j = min(jb + NJ * g4, (len - 1) & ~(NJ - 1));
-        const int64_t page = max(s_table[(j >> ps) - p0], 0), slot = j & (P - 1);
-        const char* vp = static_cast<const char*>(a.v) + (((page * a.Hk + g) * DH + NE * c16) * P + slot) * ES;
+        const uint32_t pv = page_at(jv), slot = jv & (P - 1);
+        const char* vp = static_cast<const char*>(a.v) + (static_cast<int64_t>(g) << ps) * (DH * ES) +
+                         static_cast<uint64_t>(pv) * (head_rows * (DH * ES)) + (((NE * c16) << ps) + slot) * ES;
 #pragma unroll
-        for (int e = 0; e < NE; ++e) b.vp[e] = *reinterpret_cast<const uint4*>(vp + e * (P * ES));
+        for (int e = 0; e < NE; ++e) copy_words<NJ * ES / 4>(vp + ((e * ES) << ps), b.vp[e]);
         if constexpr (KV == kPagedInt8) {
-          b.ke = *reinterpret_cast<const uint4*>(a.ke + (page * a.Hk + g) * P + slot);
-          b.ve = *reinterpret_cast<const uint4*>(a.ve + (page * a.Hk + g) * P + slot);
+          const uint64_t at = (static_cast<uint64_t>(g) << ps) + static_cast<uint64_t>(pv) * head_rows + slot;
+          copy_words<NJ / 4>(a.ke + at, b.ke);
+          copy_words<NJ / 4>(a.ve + at, b.ve);
         }
         if (a.hist_pos) {
-          const int32_t* hp = a.hist_pos + (page << ps) + slot;
+          const int32_t* hp = a.hist_pos + (static_cast<int64_t>(pv) << ps) + slot;
 #pragma unroll
           for (int i = 0; i < NJ; ++i) b.pj[i] = hp[i];
         }
@@ -344,12 +383,13 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kFwdWa
           for (int e = 0; e < NE; ++e) vf[i][e] = __uint_as_float(b.vw[i][e]);
       } else if constexpr (KV == kPagedBf16) {
 #pragma unroll
-        for (int e = 0; e < NE; ++e) vb[0][e] = __builtin_bit_cast(bf16x8, b.vp[e]);
+        for (int e = 0; e < NE; ++e)
+          vb[0][e] = __builtin_bit_cast(bf16x8, make_uint4(b.vp[e][0], b.vp[e][1], b.vp[e][2], b.vp[e][3]));
       } else if constexpr (KV == kPagedInt8) {
 #pragma unroll
         for (int e = 0; e < NE; ++e) {
-          vb[0][e] = int8_bf16(b.vp[e].x, b.vp[e].y);
-          vb[1][e] = int8_bf16(b.vp[e].z, b.vp[e].w);
+#pragma unroll
+          for (int s = 0; s < NT / 2; ++s) vb[s][e] = int8_bf16(b.vp[e][2 * s], b.vp[e][2 * s + 1]);
         }
       }
       f32x4 S[MT][NT];
@@ -375,7 +415,12 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kFwdWa
           }
         }
       }
-      const uint4 kexp = b.ke, vexp = b.ve;
+      uint32_t kexp[NJ / 4], vexp[NJ / 4];
+#pragma unroll
+      for (int i = 0; i < NJ / 4; ++i) {
+        kexp[i] = b.ke[i];
+        vexp[i] = b.ve[i];
+      }
       int pj[NJ];
       int pmin = 0, pmax = 0;
       if (a.placed) {
@@ -399,9 +444,12 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kFwdWa
       const bool tail = jb + BJ > jend || holes;
       // a score's factor before the cap, or its whole gain; an 8-bit row's step in it
       float row_gain[KV == kPagedInt8 ? NJ : 1];
+      float vstep[KV == kPagedInt8 ? NJ : 1];
       if constexpr (KV == kPagedInt8) {
+        exp_bytes(kexp, row_gain);
+        exp_bytes(vexp, vstep);
 #pragma unroll
-        for (int i = 0; i < NJ; ++i) row_gain[i] = exp_byte(word(kexp, i / 4), i % 4) * (a.cap > 0.f ? cap_in : gain);
+        for (int i = 0; i < NJ; ++i) row_gain[i] *= a.cap > 0.f ? cap_in : gain;
       } else {
         row_gain[0] = a.cap > 0.f ? cap_in : gain;
       }
@@ -496,7 +544,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kFwdWa
         }
         if constexpr (KV == kPagedInt8) {
 #pragma unroll
-          for (int i = 0; i < NJ; ++i) x[i] *= exp_byte(word(vexp, i / 4), i % 4);
+          for (int i = 0; i < NJ; ++i) x[i] *= vstep[i];
         }
         // A hidden row's value (or its scale) may be infinite or NaN, and 0
         // times it is not 0: such blocks go column by column, each with the
