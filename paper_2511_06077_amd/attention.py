@@ -19,6 +19,7 @@ A forward replaces what the plan's backward reads.
 """
 from __future__ import annotations
 
+import contextlib
 import math
 from typing import Optional
 
@@ -33,6 +34,15 @@ def _torch():
     return torch
 
 
+def _on(device):
+    """Makes `device` current for a launch; nothing to do where it is."""
+    cuda = _torch().cuda
+    return _HERE if cuda.current_device() == device.index else cuda.device(device)
+
+
+_HERE = contextlib.nullcontext()
+
+
 def _dtype_code(dtype):
     torch = _torch()
     if dtype == torch.bfloat16:
@@ -45,9 +55,10 @@ def _dtype_code(dtype):
 def _rows(name, t, heads, d_head, dtype, device, n=None):
     """(tensor, row stride) of rows [n][heads][d_head] (or [n][heads * d_head])
     whose heads lie one after the other; rows may be strided."""
-    torch = _torch()
-    if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.device != device:
+    if not hasattr(t, "data_ptr") or t.dtype != dtype or t.device != device:
         raise ValueError(f"{name}: a {dtype} tensor on {device} is needed")
+    if t.is_contiguous() and t.shape == (t.shape[0] if n is None else n, heads, d_head):
+        return t, 0
     dense = t.numel() == 0  # (no strides to speak of)
     if t.dim() == 3:
         ok = t.shape[1:] == (heads, d_head) and (dense or t.stride(2) == 1 and (heads == 1 or t.stride(1) == d_head))
@@ -64,8 +75,7 @@ def _rows(name, t, heads, d_head, dtype, device, n=None):
 
 
 def _flat(name, t, dtype, shape, device):
-    torch = _torch()
-    if (not isinstance(t, torch.Tensor) or t.dtype != dtype or t.device != device or tuple(t.shape) != tuple(shape)
+    if (not hasattr(t, "data_ptr") or t.dtype != dtype or t.device != device or t.shape != shape
             or not t.is_contiguous()):
         raise ValueError(f"{name}: a contiguous {dtype} tensor {tuple(shape)} on {device} is needed")
     return t
@@ -115,7 +125,7 @@ class _Scores:
         return _torch().empty(nbytes, dtype=_torch().uint8, device=self.device)
 
     def stream(self):
-        return _torch().cuda.current_stream(self.device).cuda_stream
+        return _torch().cuda.current_stream(self.device.index).cuda_stream
 
     def device_status(self) -> int:
         return stca.stca_device_status(self.ws, self.stream())
@@ -161,7 +171,7 @@ class CrossAttention(_Scores):
         """out [n_tgt][n_heads][d_head]"""
         torch = _torch()
         given = self._in(q, k, v, tgt_pos, hist_pos, bias)
-        with torch.cuda.device(self.device):
+        with _on(self.device):
             out = torch.empty((self.n_tgt, self.n_heads, self.d_head), dtype=self.dtype, device=self.device)
             stca.stca_attn_forward(self.attn, self.batch, given, out, self.saved, self.ws, self.ws_bytes,
                                    self.stream() if stream is None else stream)
@@ -175,7 +185,7 @@ class CrossAttention(_Scores):
             raise ValueError("backward: the plan was made without backward=True")
         given = self._in(q, k, v, tgt_pos, hist_pos, bias)
         _flat("dout", dout, self.dtype, (self.n_tgt, self.n_heads, self.d_head), self.device)
-        with torch.cuda.device(self.device):
+        with _on(self.device):
             t = dict(dtype=self.dtype, device=self.device)
             dq = torch.empty((self.n_tgt, self.n_heads, self.d_head), **t)
             dk = torch.empty((self.n_hist, self.n_kv_heads, self.d_head), **t)
@@ -228,7 +238,7 @@ class HistoryCache:
         return stca.cache_rows(R, n_rows, row_off, start, table, table.shape[1])
 
     def stream(self):
-        return _torch().cuda.current_stream(self.device).cuda_stream
+        return _torch().cuda.current_stream(self.device.index).cuda_stream
 
     def device_status(self) -> int:
         """Of the last write or read."""
@@ -246,7 +256,7 @@ class HistoryCache:
         if pos is not None:
             _flat("pos", pos, torch.int32, (n,), self.device)
         rows = self._rows(row_off, start, table, n)
-        with torch.cuda.device(self.device):
+        with _on(self.device):
             stca.stca_cache_write(self.cache, rows, _dtype_code(k.dtype), k, v, ldk, ldv, pos, self.ws,
                                   self.stream() if stream is None else stream)
 
@@ -255,7 +265,7 @@ class HistoryCache:
         torch = _torch()
         dtype = dtype or torch.bfloat16
         rows = self._rows(row_off, start, table, n_rows)
-        with torch.cuda.device(self.device):
+        with _on(self.device):
             k, v = (torch.empty((n_rows, self.n_kv_heads, self.d_head), dtype=dtype, device=self.device)
                     for _ in range(2))
             pos = None if self.pos is None else torch.empty(n_rows, dtype=torch.int32, device=self.device)
@@ -276,14 +286,11 @@ class CacheAttention(_Scores):
         self._scores(n_heads, cache.n_kv_heads, cache.d_head, torch.bfloat16, scale, softcap, edges, masked)
         self.toff_h, self.toff = _offsets(tgt_off, self.device)
         self.n_requests, self.n_tgt = len(self.toff_h) - 1, int(self.toff_h[-1])
-        self.ws = self._workspace(stca.stca_cache_attn_workspace_size(self.attn, cache.cache, self._batch(None, None)),
+        # (sizes do not depend on where lens and table lie: each call's own are set below)
+        self.batch = stca.cache_batch(self.n_requests, self.n_tgt, self.toff, self.toff, self.max_len, self.toff,
+                                      -(-self.max_len // cache.page_size), self.toff_h)
+        self.ws = self._workspace(stca.stca_cache_attn_workspace_size(self.attn, cache.cache, self.batch),
                                   "stca_cache_attn_workspace_size")
-
-    def _batch(self, lens, table):
-        # (sizes do not depend on where lens and table lie)
-        ld = -(-self.max_len // self.cache.page_size) if table is None else table.shape[1]
-        return stca.cache_batch(self.n_requests, self.n_tgt, self.toff, self.toff if lens is None else lens,
-                                self.max_len, self.toff if table is None else table, ld, self.toff_h)
 
     def forward(self, q, lens, table, tgt_pos=None, bias=None, stream: Optional[int] = None):
         """out [n_tgt][n_heads][d_head] over the first lens[r] rows of each request."""
@@ -294,8 +301,10 @@ class CacheAttention(_Scores):
             raise ValueError(f"table: [{self.n_requests}][pages of {self.max_len} rows] is needed")
         _flat("table", table, torch.int32, table.shape, self.device)
         self._given(tgt_pos, bias, self.n_tgt)
-        with torch.cuda.device(self.device):
+        with _on(self.device):
             out = torch.empty((self.n_tgt, self.n_heads, self.d_head), dtype=self.dtype, device=self.device)
-            stca.stca_cache_attn(self.attn, self.cache.cache, self._batch(lens, table), q, ldq, tgt_pos, bias, out,
+            b = self.batch
+            b.lens, b.table, b.table_ld = lens.data_ptr(), table.data_ptr(), table.shape[1]
+            stca.stca_cache_attn(self.attn, self.cache.cache, b, q, ldq, tgt_pos, bias, out,
                                  self.ws, self.ws_bytes, self.stream() if stream is None else stream)
         return out

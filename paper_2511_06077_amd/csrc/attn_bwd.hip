@@ -194,12 +194,9 @@ struct BwdLds {
 // sums stay within 36 KB, else every second or fourth, which then take turns.
 inline __host__ __device__ int bin_copies(int n) { return n <= 34 ? 64 : n <= 70 ? 32 : 16; }
 
-#ifndef EUB64
-#define EUB64 2
-#endif
 // Waves a SIMD is to hold: what the registers allow without spills.
 template <typename T, int DH, int MT>
-constexpr int kBwdWaves = DH == 128 ? 1 : DH == 64 && (MT > 1 || !Elem<T>::bf16) ? EUB64 : 2;
+constexpr int kBwdWaves = DH == 128 ? 1 : 2;
 
 template <typename T, int DH, int MT, int JT>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kBwdWaves<T, DH, MT>))) void attn_bwd_kernel(const AttnArgs a) {
@@ -502,7 +499,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kBwdWa
             for (int i = 0; i < 4; ++i) {
               float x = S[mt][jt][i], slope = 1.f;
               if (a.cap > 0.f) {
-                x = kBf16 ? tanh_fast(x * cap_in) : tanhf(x * cap_in);
+                x = kBf16 ? tanh_fast(x * cap_in, a.cap > kPlainCap) : tanhf(x * cap_in);
                 slope = 1.f - x * x;
               }
               x = fmaf(x, gain, dx[jt][i]);
@@ -781,10 +778,7 @@ __global__ __launch_bounds__(256) void attn_bwd_sum_kernel(const AttnArgs a, int
 
 template <typename T, int DH, int MT>
 hipError_t launch_bwd(const AttnArgs& a, hipStream_t st) {
-#ifndef JTB
-#define JTB 1
-#endif
-  constexpr int JT = DH == 128 ? 1 : JTB;
+  constexpr int JT = 1;
   const size_t lds = BwdLds<T, DH, MT, JT>::bytes(a.hw, a.G, a.b.n, bin_copies(a.b.n));
   const int64_t grid = round_up(a.units, kXcds) * (a.Hk / a.hw), rows = ceil_div(a.n_tgt * a.H, 16) + 1;
   if (grid > 0x7fffffff || rows > 0x7fffffff) return hipErrorInvalidValue;
@@ -824,16 +818,7 @@ hipError_t backward_t(const AttnArgs& a, int dh, int tiles, hipStream_t st) {
 // Row tiles a wave holds: the fewest that take a request's tiles in one pass,
 // up to what registers (dq, DH / 16 x 4 a tile) and LDS allow.
 int backward_tiles(int dtype, int dh, int need) {
-#ifndef BT64
-#define BT64 1
-#endif
-#ifndef BT32
-#define BT32 4
-#endif
-#ifndef BT128
-#define BT128 1
-#endif
-  const int most = dtype == STCA_BF16 ? (dh == 128 ? BT128 : dh == 64 ? BT64 : BT32) : (dh == 128 ? 1 : 2);
+  const int most = dtype == STCA_BF16 ? (dh == 32 ? 4 : 1) : (dh == 128 ? 1 : 2);
   return need >= 3 && most == 4 ? 4 : need >= 2 && most >= 2 ? 2 : 1;
 }
 

@@ -41,9 +41,6 @@ namespace ops {
 constexpr int kRagged = 0, kPagedBf16 = 1, kPagedInt8 = 2;
 constexpr float kSlack = 8.f;  // 2^8: sums and products stay far inside fp32 and bf16 ranges
 
-#ifndef EU8
-#define EU8 2
-#endif
 
 // LDS of a workgroup before the dynamic part's tables.
 template <int DH> constexpr int kCombineFloats = kWaves * 16 * (DH + 2);
@@ -152,19 +149,16 @@ __device__ __forceinline__ bool odd_bf16(uint32_t w) {  // a half of w is not fi
   return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u;
 }
 
-// Waves a SIMD is to hold: what the registers of a block, its output and its
-// rows allow without spills.
-#ifndef EU64
-#define EU64 2
-#endif
-#ifndef EU128
-#define EU128 1
-#endif
-template <typename T, int KV, int DH, int MT>
-constexpr int kFwdWaves = KV == kPagedInt8 ? EU8 : DH == 128 ? EU128 : DH == 64 && MT > 1 ? EU64 : 2;
+// Two waves a SIMD, where the registers hold a block, the next one on its way,
+// the output and the rows.  Of 128 features they do without the next block (one
+// wave that has it: 32 targets on 8-bit pages 276 us for 202, rows of 16 targets
+// 190 for 157); with two tiles of bf16 even that spills, and one wave that
+// fetches ahead is better (16 x 4 rows on bf16 pages 177 us for 268).
+template <int KV, int DH, int MT> constexpr bool kOneWave = DH == 128 && MT > 1 && KV != kPagedInt8;
+template <int KV, int DH, int MT> constexpr bool kAhead = DH < 128 || kOneWave<KV, DH, MT>;
 
 template <typename T, int KV, int DH, int MT>
-__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kFwdWaves<T, KV, DH, MT>))) void attn_fwd_kernel(const AttnArgs a) {
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kOneWave<KV, DH, MT> ? 1 : 2))) void attn_fwd_kernel(const AttnArgs a) {
   constexpr bool kF32 = !Elem<T>::bf16;
   constexpr bool kPaged = KV != kRagged;
   constexpr int NT = 2;
@@ -464,7 +458,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kFwdWa
 #pragma unroll
           for (int i = 0; i < NJ; ++i) {
             const float y = S[mt][i / 4][i % 4] * row_gain[KV == kPagedInt8 ? i : 0];
-            S[mt][i / 4][i % 4] = kF32 ? tanhf(y) : tanh_fast(y);
+            S[mt][i / 4][i % 4] = kF32 ? tanhf(y) : tanh_fast(y, a.cap > kPlainCap);
           }
         }
         if (!slow) {
@@ -636,8 +630,11 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kFwdWa
     const int jstop = min(jend, jb + share * BJ);
     if (jb < jstop) {
       Blk blk;
-      load(blk, jb);
-      for (; jb < jstop; jb += BJ) compute(blk, jb, jb + BJ < jstop);
+      if constexpr (kAhead<KV, DH, MT>) load(blk, jb);
+      for (; jb < jstop; jb += BJ) {
+        if constexpr (!kAhead<KV, DH, MT>) load(blk, jb);
+        compute(blk, jb, kAhead<KV, DH, MT> && jb + BJ < jstop);
+      }
     }
 
     // ---- join the waves: lane group g4 of wave w holds features NE (4 g4 + i) + e of column c16

@@ -20,39 +20,65 @@ hipError_t forward_dh(const AttnArgs& a, int tiles, hipStream_t st) {
   return launch_fwd<T, kRagged, DH, 1>(a, st);
 }
 
-// One row (target, head) per 16 lanes: partials of its request's chunks joined
-// in chunk order.
-template <typename T, int DH>
+// Partials of a row (target, head) joined, in an order that depends on their
+// number alone: 16 lanes a row, DH / 16 features each, times kSplit lanes that
+// take every kSplit-th chunk.
+template <typename T, int DH, int kSplit>
 __global__ __launch_bounds__(256) void attn_merge_kernel(const AttnArgs a, bool paged) {
-  constexpr int NE = DH / 16;
-  const int64_t row = static_cast<int64_t>(blockIdx.x) * 16 + (threadIdx.x >> 4);
-  if (row >= a.n_tgt * a.H) return;
-  const int64_t t = row / a.H;
-  const int h = static_cast<int>(row % a.H), f0 = (threadIdx.x & 15) * NE;
-  int lo = 0, hi = a.R;  // the request of target t
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) / 2;
-    if (a.tgt_off[mid] <= t) lo = mid;
-    else hi = mid;
+  constexpr int NE = DH / 16, kRows = 16 / kSplit;
+  __shared__ float part[kSplit > 1 ? 16 : 1][kSplit > 1 ? DH + 2 : 1];
+  const int f0 = (threadIdx.x & 15) * NE, s = (threadIdx.x >> 4) % kSplit, slot = threadIdx.x >> 4;
+  const int64_t row = static_cast<int64_t>(blockIdx.x) * kRows + slot / kSplit;
+  const int64_t step = a.n_tgt * a.H, t = row / a.H;
+  int n = 0;
+  if (row < step) {
+    int lo = 0, hi = a.R;  // the request of target t
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) / 2;
+      if (a.tgt_off[mid] <= t) lo = mid;
+      else hi = mid;
+    }
+    int len;
+    if (paged) len = min(max(a.lens[lo], 0), a.max_len);
+    else len = clamp_off(a.hist_off[lo + 1], a.n_hist) - clamp_off(a.hist_off[lo], a.n_hist);
+    if (len > a.chunk) n = min(a.max_chunks, (len + a.chunk - 1) / a.chunk);  // (else written by the attention itself)
   }
-  int len;
-  if (paged) len = min(max(a.lens[lo], 0), a.max_len);
-  else len = clamp_off(a.hist_off[lo + 1], a.n_hist) - clamp_off(a.hist_off[lo], a.n_hist);
-  if (len <= a.chunk) return;  // written by the attention itself
-  const int n = min(a.max_chunks, (len + a.chunk - 1) / a.chunk);
-  const int64_t step = a.n_tgt * a.H;
   float M = -INFINITY, L = 0.f, acc[NE] = {};
-  for (int c = 0; c < n; ++c) M = fmaxf(M, a.part_ml[2 * (c * step + row)]);
-  for (int c = 0; c < n; ++c) {
+#pragma unroll 4
+  for (int c = s; c < n; c += kSplit) {
     const int64_t at = c * step + row;
-    const float m = a.part_ml[2 * at], l = a.part_ml[2 * at + 1];
-    const float f = m == -INFINITY ? (l != l ? l : 0.f) : exp2_fast(m - M);
-    L += f * l;
+    const float m = a.part_ml[2 * at], l = a.part_ml[2 * at + 1], mn = fmaxf(M, m);
+    const float f = m == -INFINITY ? (l != l ? l : 0.f) : exp2_fast(m - mn), keep = M == -INFINITY ? (L != L ? L : 0.f) : exp2_fast(M - mn);
+    L = keep * L + f * l;
 #pragma unroll
-    for (int e = 0; e < NE; ++e) acc[e] += f * a.part_o[at * DH + f0 + e];
+    for (int e = 0; e < NE; ++e) acc[e] = keep * acc[e] + f * a.part_o[at * DH + f0 + e];
+    M = mn;
+  }
+  if constexpr (kSplit > 1) {
+#pragma unroll
+    for (int e = 0; e < NE; ++e) part[slot][f0 + e] = acc[e];
+    if (f0 == 0) {
+      part[slot][DH] = M;
+      part[slot][DH + 1] = L;
+    }
+    __syncthreads();
+    if (s != 0 || n == 0) return;
+    for (int k = 1; k < kSplit; ++k) M = fmaxf(M, part[slot + k][DH]);
+    L = 0.f;
+#pragma unroll
+    for (int e = 0; e < NE; ++e) acc[e] = 0.f;
+    for (int k = 0; k < kSplit; ++k) {
+      const float m = part[slot + k][DH], l = part[slot + k][DH + 1];
+      const float f = m == -INFINITY ? (l != l ? l : 0.f) : exp2_fast(m - M);
+      L += f * l;
+#pragma unroll
+      for (int e = 0; e < NE; ++e) acc[e] += f * part[slot + k][f0 + e];
+    }
+  } else if (n == 0) {
+    return;
   }
   const float inv = L == 0.f ? 0.f : 1.f / L;
-  const int64_t at = (t * a.H + h) * DH + f0;
+  const int64_t at = row * DH + f0;
 #pragma unroll
   for (int e = 0; e < NE; ++e) {
     const float y = acc[e] * inv;
@@ -65,14 +91,21 @@ __global__ __launch_bounds__(256) void attn_merge_kernel(const AttnArgs a, bool 
   }
 }
 
+// (8 rows of 40 chunks: 16 lanes a row 16.7 us, 16 times 16 @@; 32768 rows of 8
+// chunks fill the card either way, and the split costs 40 us)
+template <typename T, int DH>
+hipError_t merge_dh(const AttnArgs& a, bool paged, hipStream_t st) {
+  const int split = a.max_chunks >= 8 && a.n_tgt * a.H <= 4096 ? 16 : 1;
+  const int64_t grid = ceil_div(a.n_tgt * a.H, 16 / split);
+  if (grid > 0x7fffffff) return hipErrorInvalidValue;
+  if (split == 16) attn_merge_kernel<T, DH, 16><<<static_cast<unsigned>(grid), 256, 0, st>>>(a, paged);
+  else attn_merge_kernel<T, DH, 1><<<static_cast<unsigned>(grid), 256, 0, st>>>(a, paged);
+  return hipGetLastError();
+}
+
 template <typename T>
 hipError_t merge_t(const AttnArgs& a, bool paged, int dh, hipStream_t st) {
-  const int64_t grid = ceil_div(a.n_tgt * a.H, 16);
-  if (grid > 0x7fffffff) return hipErrorInvalidValue;
-  if (dh == 32) attn_merge_kernel<T, 32><<<static_cast<unsigned>(grid), 256, 0, st>>>(a, paged);
-  else if (dh == 64) attn_merge_kernel<T, 64><<<static_cast<unsigned>(grid), 256, 0, st>>>(a, paged);
-  else attn_merge_kernel<T, 128><<<static_cast<unsigned>(grid), 256, 0, st>>>(a, paged);
-  return hipGetLastError();
+  return dh == 32 ? merge_dh<T, 32>(a, paged, st) : dh == 64 ? merge_dh<T, 64>(a, paged, st) : merge_dh<T, 128>(a, paged, st);
 }
 
 }  // namespace

@@ -148,11 +148,15 @@ __device__ __forceinline__ uint32_t cut_bf16(float& a, float& b) {
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// tanh(x) to about 1e-7 relative: 1 - 2 / (e^2x + 1) away from zero, the odd
-// series up to x^9 near it, where the difference would cancel.
-__device__ __forceinline__ float tanh_fast(float x) {
-  const float e = __builtin_amdgcn_exp2f(x * (2.f * kLog2e));
-  const float far = 1.f - 2.f * __builtin_amdgcn_rcpf(e + 1.f);
+// tanh(x) as 1 - 2 / (e^2x + 1), within 2e-7; where `fine`, also relative to
+// small values: there the odd series up to x^9, since the difference cancels.
+// A cap of up to kPlainCap turns 2e-7 into no more than the 2^-16 that two bf16
+// terms leave of a weight, and does without (a third of the cost).
+constexpr float kPlainCap = 64.f;
+__device__ __forceinline__ float tanh_fast(float x, bool fine) {
+  const float e = exp2_fast(x * (2.f * kLog2e));
+  const float far = fmaf(-2.f, __builtin_amdgcn_rcpf(e + 1.f), 1.f);
+  if (!fine) return far;
   const float x2 = x * x;
   float p = fmaf(x2, 62.f / 2835.f, -17.f / 315.f);
   p = fmaf(x2, p, 2.f / 15.f);
