@@ -499,7 +499,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kBwdWa
             for (int i = 0; i < 4; ++i) {
               float x = S[mt][jt][i], slope = 1.f;
               if (a.cap > 0.f) {
-                x = kBf16 ? tanh_fast(x * cap_in, a.cap > kPlainCap) : tanhf(x * cap_in);
+                x = kBf16 ? tanh_fast(x * cap_in, true) : tanhf(x * cap_in);
                 slope = 1.f - x * x;
               }
               x = fmaf(x, gain, dx[jt][i]);

@@ -458,7 +458,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kOneWa
 #pragma unroll
           for (int i = 0; i < NJ; ++i) {
             const float y = S[mt][i / 4][i % 4] * row_gain[KV == kPagedInt8 ? i : 0];
-            S[mt][i / 4][i % 4] = kF32 ? tanhf(y) : tanh_fast(y, a.cap > kPlainCap);
+            S[mt][i / 4][i % 4] = kF32 ? tanhf(y) : tanh_fast(y, whole || a.cap > kPlainCap);
           }
         }
         if (!slow) {

@@ -151,7 +151,8 @@ __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_ex
 // tanh(x) as 1 - 2 / (e^2x + 1), within 2e-7; where `fine`, also relative to
 // small values: there the odd series up to x^9, since the difference cancels.
 // A cap of up to kPlainCap turns 2e-7 into no more than the 2^-16 that two bf16
-// terms leave of a weight, and does without (a third of the cost).
+// terms leave of a weight: where the weights have two, it does without (a third
+// of the cost).
 constexpr float kPlainCap = 64.f;
 __device__ __forceinline__ float tanh_fast(float x, bool fine) {
   const float e = exp2_fast(x * (2.f * kLog2e));

@@ -9,8 +9,13 @@
 // with an infinity or a NaN gets the byte 255 and n = 0: it reads as NaN.
 //
 // One workgroup takes 64 consecutive slots (aligned, so they fill cache lines
-// of V) of one request and kv head, four threads a row; V turns in LDS.  Both
-// directions are bound by their bytes.
+// of V) of one request and up to 128 features' worth of kv heads (whole cache
+// lines of the packed rows), four threads a row; V turns in LDS.  Both
+// directions are bound by their bytes; with one head a workgroup they waited for
+// the look-ups of request and pages instead (128 MB of 8-bit rows of 8 heads
+// read back: @@).
+#include <type_traits>
+
 #include "attn_ops.h"
 
 namespace stca {
@@ -140,72 +145,81 @@ __device__ __forceinline__ uint32_t quantise4(const float* x, uint32_t byte) {
   return w;
 }
 
-template <typename T, bool kInt8, int DH>
+template <typename T, bool kInt8, int DH, int HB>
 __global__ __launch_bounds__(256) void cache_write_kernel(const CacheArgs a) {
-  constexpr int N = DH / 4;  // elements of a thread
+  constexpr int N = DH / 4;  // elements of a thread and head
   using S = typename std::conditional<kInt8, uint8_t, uint16_t>::type;
-  constexpr int kLd = kSlots + 16 / sizeof(S);  // V tile [DH][slots], 16-byte rows
-  __shared__ __align__(16) S tile[DH * kLd];
+  constexpr int kLd = kSlots + 16 / sizeof(S);  // V tile [HB DH][slots], 16-byte rows
+  __shared__ __align__(16) S tile[HB * DH * kLd];
   if (blockIdx.x == gridDim.x - 1) {
     check_rows(a);
     return;
   }
-  const int unit = static_cast<int>(blockIdx.x) / a.Hk, g = static_cast<int>(blockIdx.x) % a.Hk;
+  const int groups = a.Hk / HB, unit = static_cast<int>(blockIdx.x) / groups, g0 = static_cast<int>(blockIdx.x) % groups * HB;
   Span s;
   if (!find_span(a, unit, s)) return;
   const int slot = threadIdx.x >> 2, part = threadIdx.x & 3, pos = s.p0 + slot;
   const bool have = pos >= s.lo && pos < s.hi;
   const int page = have ? page_of(a, s.r, pos) : -1;
   const int P = 1 << a.page_shift, at = pos & (P - 1);
-  float x[N];
-  uint32_t byte[2];
+  float x[2][HB][N];
 #pragma unroll
-  for (int kv = 0; kv < 2; ++kv) {
+  for (int kv = 0; kv < 2; ++kv)
 #pragma unroll
-    for (int i = 0; i < N; ++i) x[i] = 0.f;
-    if (have)
-      load_row<T, N>(static_cast<const T*>(kv ? a.xv : a.xk) + (s.row + pos) * (kv ? a.ldv : a.ldk) + g * DH + part * N, x);
-    uint32_t w[kInt8 ? N / 4 : N / 2];
-    if constexpr (kInt8) {
-      byte[kv] = step_byte<N>(x);
+    for (int h = 0; h < HB; ++h) {
 #pragma unroll
-      for (int i = 0; i < N / 4; ++i) w[i] = quantise4(x + 4 * i, byte[kv]);
-    } else {
-#pragma unroll
-      for (int i = 0; i < N / 2; ++i) w[i] = pack_bf16(x[2 * i], x[2 * i + 1]);
+      for (int i = 0; i < N; ++i) x[kv][h][i] = 0.f;
+      if (have)
+        load_row<T, N>(static_cast<const T*>(kv ? a.xv : a.xk) + (s.row + pos) * (kv ? a.ldv : a.ldk) + (g0 + h) * DH +
+                           part * N, x[kv][h]);
     }
-    if (kv == 0) {
-      if (page >= 0) {
-        uint32_t* p = reinterpret_cast<uint32_t*>(static_cast<S*>(a.k) +
-                                                  ((static_cast<int64_t>(page) * a.Hk + g) * P + at) * DH + part * N);
-        constexpr int W = sizeof(w) / 4;
 #pragma unroll
-        for (int i = 0; i < W / 2; ++i) reinterpret_cast<uint2*>(p)[i] = make_uint2(w[2 * i], w[2 * i + 1]);
+  for (int h = 0; h < HB; ++h) {
+    uint32_t byte[2];
+#pragma unroll
+    for (int kv = 0; kv < 2; ++kv) {
+      uint32_t w[kInt8 ? N / 4 : N / 2];
+      if constexpr (kInt8) {
+        byte[kv] = step_byte<N>(x[kv][h]);
+#pragma unroll
+        for (int i = 0; i < N / 4; ++i) w[i] = quantise4(x[kv][h] + 4 * i, byte[kv]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) w[i] = pack_bf16(x[kv][h][2 * i], x[kv][h][2 * i + 1]);
       }
-    } else {
+      if (kv == 0) {
+        if (page >= 0) {
+          uint32_t* p = reinterpret_cast<uint32_t*>(static_cast<S*>(a.k) +
+                                                    ((static_cast<int64_t>(page) * a.Hk + g0 + h) * P + at) * DH + part * N);
+          constexpr int W = sizeof(w) / 4;
 #pragma unroll
-      for (int i = 0; i < N; ++i)
-        tile[(part * N + i) * kLd + slot] = kInt8 ? static_cast<S>(w[i / 4] >> (8 * (i % 4)))
-                                                  : static_cast<S>(w[i / 2] >> (16 * (i % 2)));
+          for (int i = 0; i < W / 2; ++i) reinterpret_cast<uint2*>(p)[i] = make_uint2(w[2 * i], w[2 * i + 1]);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+          tile[(h * DH + part * N + i) * kLd + slot] = kInt8 ? static_cast<S>(w[i / 4] >> (8 * (i % 4)))
+                                                             : static_cast<S>(w[i / 2] >> (16 * (i % 2)));
+      }
     }
+    if constexpr (kInt8)
+      if (page >= 0 && part == 0) {
+        const int64_t e = (static_cast<int64_t>(page) * a.Hk + g0 + h) * P + at;
+        a.ke[e] = static_cast<uint8_t>(byte[0]);
+        a.ve[e] = static_cast<uint8_t>(byte[1]);
+      }
   }
-  if (page >= 0 && part == 0) {
-    const int64_t e = (static_cast<int64_t>(page) * a.Hk + g) * P + at;
-    if constexpr (kInt8) {
-      a.ke[e] = static_cast<uint8_t>(byte[0]);
-      a.ve[e] = static_cast<uint8_t>(byte[1]);
-    }
-    if (a.pos && a.xpos && g == 0) a.pos[static_cast<int64_t>(page) * P + at] = a.xpos[s.row + pos];
-  }
+  if (page >= 0 && part == 0 && g0 == 0 && a.pos && a.xpos) a.pos[static_cast<int64_t>(page) * P + at] = a.xpos[s.row + pos];
   __syncthreads();
   // V: 16 bytes of one feature's slots at a time (within one page), or the
   // slots that exist one by one
   constexpr int kRun = 16 / sizeof(S);
-  for (int i = threadIdx.x; i < DH * (kSlots / kRun); i += 256) {
+#pragma unroll 2
+  for (int i = threadIdx.x; i < HB * DH * (kSlots / kRun); i += 256) {
     const int d = i / (kSlots / kRun), c = i % (kSlots / kRun) * kRun, p = s.p0 + c;
     const int pg = p < s.hi && p + kRun > s.lo ? page_of(a, s.r, p) : -1;
     if (pg < 0) continue;
-    S* out = static_cast<S*>(a.v) + ((static_cast<int64_t>(pg) * a.Hk + g) * DH + d) * P + (p & (P - 1));
+    S* out = static_cast<S*>(a.v) + ((static_cast<int64_t>(pg) * a.Hk + g0) * DH + d) * P + (p & (P - 1));
     const S* in = tile + d * kLd + c;
     if (p >= s.lo && p + kRun <= s.hi) {
       *reinterpret_cast<uint4*>(out) = *reinterpret_cast<const uint4*>(in);
@@ -216,75 +230,110 @@ __global__ __launch_bounds__(256) void cache_write_kernel(const CacheArgs a) {
   }
 }
 
-template <typename T, bool kInt8, int DH>
+template <typename T, bool kInt8, int DH, int HB>
 __global__ __launch_bounds__(256) void cache_read_kernel(const CacheArgs a) {
   constexpr int N = DH / 4;
   using S = typename std::conditional<kInt8, uint8_t, uint16_t>::type;
-  constexpr int kLd = kSlots + 16 / sizeof(S);
-  __shared__ __align__(16) S tile[DH * kLd];
+  constexpr int kLd = kSlots + 16 / sizeof(S), W = N * static_cast<int>(sizeof(S)) / 4;
+  __shared__ __align__(16) S tile[HB * DH * kLd];
   if (blockIdx.x == gridDim.x - 1) {
     check_rows(a);
     return;
   }
-  const int unit = static_cast<int>(blockIdx.x) / a.Hk, g = static_cast<int>(blockIdx.x) % a.Hk;
+  const int groups = a.Hk / HB, unit = static_cast<int>(blockIdx.x) / groups, g0 = static_cast<int>(blockIdx.x) % groups * HB;
   Span s;
   if (!find_span(a, unit, s)) return;
   const int P = 1 << a.page_shift;
-  constexpr int kRun = 16 / sizeof(S);
-  for (int i = threadIdx.x; i < DH * (kSlots / kRun); i += 256) {
-    const int d = i / (kSlots / kRun), c = i % (kSlots / kRun) * kRun, p = s.p0 + c;
-    const int pg = p < s.hi && p + kRun > s.lo ? page_of(a, s.r, p) : -1;
-    if (pg < 0) continue;
-    *reinterpret_cast<uint4*>(tile + d * kLd + c) = *reinterpret_cast<const uint4*>(
-        static_cast<const S*>(a.v) + ((static_cast<int64_t>(pg) * a.Hk + g) * DH + d) * P + (p & (P - 1)));
+  constexpr int kRun = 16 / sizeof(S), kPieces = HB * DH * (kSlots / kRun), kMine = (kPieces + 255) / 256;
+  // everything on its way first: V's pieces, then this thread's part of K's rows
+  uint4 vq[kMine];
+#pragma unroll
+  for (int n = 0; n < kMine; ++n) {
+    const int i = threadIdx.x + 256 * n, d = i / (kSlots / kRun), p = s.p0 + i % (kSlots / kRun) * kRun;
+    const int pg = i < kPieces && p < s.hi && p + kRun > s.lo ? page_of(a, s.r, p) : -1;
+    vq[n] = uint4{};
+    if (pg >= 0)
+      vq[n] = *reinterpret_cast<const uint4*>(static_cast<const S*>(a.v) +
+                                              ((static_cast<int64_t>(pg) * a.Hk + g0) * DH + d) * P + (p & (P - 1)));
   }
   const int slot = threadIdx.x >> 2, part = threadIdx.x & 3, pos = s.p0 + slot;
   const bool have = pos >= s.lo && pos < s.hi;
   const int page = have ? page_of(a, s.r, pos) : -1;
-  const int64_t row = (static_cast<int64_t>(max(page, 0)) * a.Hk + g) * P + (pos & (P - 1));
+  const int64_t row = (static_cast<int64_t>(max(page, 0)) * a.Hk + g0) * P + (pos & (P - 1));  // of head g0; others P on
+  uint32_t kq[HB][W];
+  uint8_t ke[HB], ve[HB];
+#pragma unroll
+  for (int h = 0; h < HB; ++h) {
+    if (page >= 0) {
+      const uint2* p = reinterpret_cast<const uint2*>(static_cast<const S*>(a.k) + (row + h * P) * DH + part * N);
+#pragma unroll
+      for (int i = 0; i < W / 2; ++i) {
+        kq[h][2 * i] = p[i].x;
+        kq[h][2 * i + 1] = p[i].y;
+      }
+      if constexpr (kInt8) {
+        ke[h] = a.ke[row + h * P];
+        ve[h] = a.ve[row + h * P];
+      }
+    }
+  }
+#pragma unroll
+  for (int n = 0; n < kMine; ++n) {
+    const int i = threadIdx.x + 256 * n;
+    if (i < kPieces)
+      *reinterpret_cast<uint4*>(tile + i / (kSlots / kRun) * kLd + i % (kSlots / kRun) * kRun) = vq[n];
+  }
   float x[N];
   if (page >= 0) {
-    const uint32_t* p = reinterpret_cast<const uint32_t*>(static_cast<const S*>(a.k) + row * DH + part * N);
-    const float step = kInt8 ? __uint_as_float(static_cast<uint32_t>(a.ke[row]) << 23) : 0.f;
 #pragma unroll
-    for (int i = 0; i < N; ++i)
-      x[i] = kInt8 ? static_cast<float>(static_cast<int8_t>(p[i / 4] >> (8 * (i % 4)))) * step
-                   : __uint_as_float((p[i / 2] >> (16 * (i % 2))) << 16);
-    store_row<T, N>(static_cast<T*>(const_cast<void*>(a.xk)) + (s.row + pos) * a.ldk + g * DH + part * N, x);
-    if (a.pos && a.xpos && g == 0 && part == 0)
+    for (int h = 0; h < HB; ++h) {
+      const float step = kInt8 ? __uint_as_float(static_cast<uint32_t>(ke[h]) << 23) : 0.f;
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        x[i] = kInt8 ? static_cast<float>(static_cast<int8_t>(kq[h][i / 4] >> (8 * (i % 4)))) * step
+                     : __uint_as_float((kq[h][i / 2] >> (16 * (i % 2))) << 16);
+      store_row<T, N>(static_cast<T*>(const_cast<void*>(a.xk)) + (s.row + pos) * a.ldk + (g0 + h) * DH + part * N, x);
+    }
+    if (a.pos && a.xpos && g0 == 0 && part == 0)
       const_cast<int32_t*>(a.xpos)[s.row + pos] = a.pos[static_cast<int64_t>(page) * P + (pos & (P - 1))];
   }
   __syncthreads();
   if (page >= 0) {
-    const float step = kInt8 ? __uint_as_float(static_cast<uint32_t>(a.ve[row]) << 23) : 0.f;
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const S v = tile[(part * N + i) * kLd + slot];
-      x[i] = kInt8 ? static_cast<float>(static_cast<int8_t>(v)) * step : __uint_as_float(static_cast<uint32_t>(v) << 16);
+    for (int h = 0; h < HB; ++h) {
+      const float step = kInt8 ? __uint_as_float(static_cast<uint32_t>(ve[h]) << 23) : 0.f;
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const S v = tile[(h * DH + part * N + i) * kLd + slot];
+        x[i] = kInt8 ? static_cast<float>(static_cast<int8_t>(v)) * step : __uint_as_float(static_cast<uint32_t>(v) << 16);
+      }
+      store_row<T, N>(static_cast<T*>(const_cast<void*>(a.xv)) + (s.row + pos) * a.ldv + (g0 + h) * DH + part * N, x);
     }
-    store_row<T, N>(static_cast<T*>(const_cast<void*>(a.xv)) + (s.row + pos) * a.ldv + g * DH + part * N, x);
   }
 }
 
-template <typename T, bool kInt8, int DH>
+template <typename T, bool kInt8, int DH, int HB>
 hipError_t launch(const CacheArgs& a, bool write, hipStream_t st) {
-  const int64_t grid = (a.n_rows / kSlots + 2 * static_cast<int64_t>(a.R)) * a.Hk + 1;
+  const int64_t grid = (a.n_rows / kSlots + 2 * static_cast<int64_t>(a.R)) * (a.Hk / HB) + 1;
   if (grid > 0x7fffffff) return hipErrorInvalidValue;
-  if (write) cache_write_kernel<T, kInt8, DH><<<static_cast<unsigned>(grid), 256, 0, st>>>(a);
-  else cache_read_kernel<T, kInt8, DH><<<static_cast<unsigned>(grid), 256, 0, st>>>(a);
+  if (write) cache_write_kernel<T, kInt8, DH, HB><<<static_cast<unsigned>(grid), 256, 0, st>>>(a);
+  else cache_read_kernel<T, kInt8, DH, HB><<<static_cast<unsigned>(grid), 256, 0, st>>>(a);
   return hipGetLastError();
+}
+
+template <typename T, bool kInt8, int DH>
+hipError_t heads(const CacheArgs& a, bool write, hipStream_t st) {
+  if constexpr (DH == 32)
+    if (a.Hk % 4 == 0) return launch<T, kInt8, DH, 4>(a, write, st);
+  if constexpr (DH <= 64)
+    if (a.Hk % 2 == 0) return launch<T, kInt8, DH, 2>(a, write, st);
+  return launch<T, kInt8, DH, 1>(a, write, st);
 }
 
 template <typename T>
 hipError_t move(const CacheArgs& a, bool int8, int dh, bool write, hipStream_t st) {
-  if (int8) {
-    if (dh == 32) return launch<T, true, 32>(a, write, st);
-    if (dh == 64) return launch<T, true, 64>(a, write, st);
-    return launch<T, true, 128>(a, write, st);
-  }
-  if (dh == 32) return launch<T, false, 32>(a, write, st);
-  if (dh == 64) return launch<T, false, 64>(a, write, st);
-  return launch<T, false, 128>(a, write, st);
+  if (int8) return dh == 32 ? heads<T, true, 32>(a, write, st) : dh == 64 ? heads<T, true, 64>(a, write, st) : heads<T, true, 128>(a, write, st);
+  return dh == 32 ? heads<T, false, 32>(a, write, st) : dh == 64 ? heads<T, false, 64>(a, write, st) : heads<T, false, 128>(a, write, st);
 }
 
 }  // namespace
