@@ -11,17 +11,11 @@ using namespace stca;
 using namespace stca::api;
 using namespace stca::ops;
 
-#ifndef PCP
-#define PCP 4
-#endif
-#ifndef PCU
-#define PCU 8
-#endif
 namespace {
 
 constexpr int64_t kMaxRows = 0x7fff0000;  // rows of one call: indices a few blocks past the end stay int32
 constexpr int kNoHostChunks = 16;         // chunks per request where the host knows no lengths
-constexpr int kMostChunks = 512;           // of a request, in a backward of several passes
+constexpr int kMostChunks = 512;          // of a request, in a backward of several passes
 constexpr int kMaxPagesOfChunk = 1024;    // a chunk's pages are listed in LDS
 
 bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
@@ -114,36 +108,29 @@ struct Plan {
 // costs its start, the join of its waves and a partial to merge, and the last
 // ones to run leave CUs idle, the less the more there are (window of 256
 // requests, 16 targets, 2048 rows, d_h = 32: 4 a CU 145 us forward, 354
-// backward, 8 134 and 320, 16 142 and 336).
+// backward, 8 134 and 320, 16 142 and 336; pages, whose chunks are whole runs of
+// 256 rows, take 4).
+constexpr int kPackedPerCu = 8, kPagedPerCu = 4;
+// ... and the fewest rows a wave is to have of it: shorter chunks are mostly
+// start and join.
+constexpr int kWaveRows = 128, kWaveRowsBack = 64;
 int chunk_for(int64_t rows, int64_t per_row, int per_cu, int step) {
   const int64_t want = static_cast<int64_t>(per_cu) * device_cus();
   const int64_t c = round_up(std::max<int64_t>(1, ceil_div(rows * per_row, want)), step);
   return static_cast<int>(std::min<int64_t>(c, kMaxRows / step * step));
 }
 
-#ifndef HWF
-#define HWF 4
-#endif
-#ifndef CMINF
-#define CMINF 128
-#endif
-#ifndef CMINB
-#define CMINB 64
-#endif
-#ifndef HWB
-#define HWB 2
-#endif
-#ifndef PCB
-#define PCB 8
-#endif
-// kv heads a workgroup takes (see attn_fwd.h): as many as there are to four (two
-// in the backward, one where it holds several tiles: its rows of every head
-// wait in LDS), where a wave to a head then has 256 history rows on every SIMD
-// of the card.
+// kv heads a workgroup takes: 32 features of bf16 are half a cache line, and a
+// line whose other half another workgroup reads later comes from memory twice
+// (window of 256 requests of 2048 rows, 8 heads of 32: 4 heads a workgroup 145
+// us forward for 204 with one, 2 heads 360 us backward for 549).  In the
+// backward two (rows of every head wait in LDS), and one where each holds four
+// tiles; only where a wave to a head then has 256 history rows on every SIMD of
+// the card, since fewer heads a workgroup are shorter chunks for as many waves.
 int heads_of(int Hk, int64_t n_hist, bool backward, int tiles) {
-  int most = Hk % 4 == 0 ? 4 : Hk % 2 == 0 ? 2 : 1;
-  most = std::min(most, backward ? (tiles > 1 ? 1 : HWB) : HWF);
-  return n_hist * Hk >= 256 * 4 * static_cast<int64_t>(device_cus()) ? most : 1;
+  const int most = !backward ? 4 : tiles < 4 ? 2 : 1;
+  const int some = most % 4 == 0 && Hk % 4 == 0 ? 4 : most % 2 == 0 && Hk % 2 == 0 ? 2 : 1;
+  return n_hist * Hk >= 256 * 4 * static_cast<int64_t>(device_cus()) ? some : 1;
 }
 
 bool ragged_plan(const stca_attn_t* a, const stca_batch_t* b, bool backward, Plan* p) {
@@ -156,11 +143,11 @@ bool ragged_plan(const stca_attn_t* a, const stca_batch_t* b, bool backward, Pla
       max_l = std::max<int64_t>(max_l, b->hist_off_host[r + 1] - b->hist_off_host[r]);
     }
   }
-  p->tiles = forward_tiles(a->dtype, dh, static_cast<int>(std::min<int64_t>(max_m * G, 1 << 20)));
+  p->tiles = forward_tiles(a->dtype, dh, static_cast<int>(std::min<int64_t>(max_m * G, 1 << 20)), false);
   p->zgroups = static_cast<int>(std::min<int64_t>(std::max<int64_t>(1, ceil_div(max_m * G, 16 * p->tiles)),
                                                   b->hist_off_host ? 1024 : 8));
   const int64_t need = ceil_div(max_m, 16);
-  p->btiles = backward_tiles(a->dtype, dh, static_cast<int>(std::min<int64_t>(need, 1 << 20)));
+  p->btiles = backward_tiles(a->dtype, dh, static_cast<int>(std::min<int64_t>(need, 1 << 20)), G);
   p->passes = static_cast<int>(std::max<int64_t>(1, ceil_div(need, p->btiles) * G));
   p->hw = backward && p->passes > 1 ? 1 : heads_of(Hk, b->n_hist, backward, p->btiles);
   const int parts = 4 / p->hw;
@@ -168,9 +155,8 @@ bool ragged_plan(const stca_attn_t* a, const stca_batch_t* b, bool backward, Pla
     // one step a wave, unless that makes more chunks than dq's partials are worth
     p->chunk = static_cast<int>(std::max<int64_t>(16 * parts, round_up(ceil_div(max_l, kMostChunks), 16 * parts)));
   } else {
-    p->chunk = chunk_for(b->n_hist, static_cast<int64_t>(Hk / p->hw) * (backward ? 1 : p->zgroups), backward ? PCB : PCU,
-                         16 * parts);
-    p->chunk = std::max(p->chunk, (backward ? CMINB : CMINF) * parts);
+    p->chunk = chunk_for(b->n_hist, static_cast<int64_t>(Hk / p->hw) * (backward ? 1 : p->zgroups), kPackedPerCu, 16 * parts);
+    p->chunk = std::max(p->chunk, (backward ? kWaveRowsBack : kWaveRows) * parts);
   }
   if (!b->hist_off_host)
     p->chunk = static_cast<int>(std::max<int64_t>(p->chunk, round_up(ceil_div(b->n_hist, kNoHostChunks), 64)));
@@ -256,10 +242,10 @@ bool paged_plan(const stca_attn_t* a, const stca_cache_t* c, const stca_cache_ba
     for (int r = 0; r < b->n_requests; ++r)
       max_m = std::max<int64_t>(max_m, b->tgt_off_host[r + 1] - b->tgt_off_host[r]);
   }
-  p->tiles = forward_tiles(STCA_BF16, dh, static_cast<int>(std::min<int64_t>(max_m * G, 1 << 20)));
+  p->tiles = forward_tiles(STCA_BF16, dh, static_cast<int>(std::min<int64_t>(max_m * G, 1 << 20)), true);
   p->zgroups = static_cast<int>(std::min<int64_t>(std::max<int64_t>(1, ceil_div(max_m * G, 16 * p->tiles)),
                                                   b->tgt_off_host ? 1024 : 8));
-  p->chunk = chunk_for(static_cast<int64_t>(b->n_requests) * b->max_len, static_cast<int64_t>(Hk) * p->zgroups, PCP, kPageStep);
+  p->chunk = chunk_for(static_cast<int64_t>(b->n_requests) * b->max_len, static_cast<int64_t>(Hk) * p->zgroups, kPagedPerCu, kPageStep);
   p->chunk = std::min(p->chunk, kMaxPagesOfChunk * c->page_size);
   p->chunk = static_cast<int>(std::min<int64_t>(p->chunk, std::max<int64_t>(kPageStep, round_up(b->max_len, kPageStep))));
   p->max_chunks = static_cast<int>(std::max<int64_t>(1, ceil_div(b->max_len, p->chunk)));

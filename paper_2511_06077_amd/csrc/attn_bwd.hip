@@ -6,15 +6,16 @@
 //   dv_j += w dout,  dk_j += scale dz q,  dq_t += scale dz k_j
 //
 // One workgroup takes one chunk of one request's history for hw kv heads; 4 / hw
-// of its four waves share a head, each with consecutive steps of 16 JT history
-// rows (see attn_fwd.h), and hold dK^T, dV^T of a step in registers while they go through the pass's MT tiles of 16 targets (of
-// one query head each), whose q and dout rows wait in LDS.  dq of a pass stays
-// in registers over the whole chunk.  More tiles than MT are further passes
-// over the chunk; a chunk is then one step a wave, whose K, V, dK and dV stay in
-// registers from pass to pass (or, where that would make too many chunks, dK
-// and dV of the passes so far wait in fp32 in the workspace, written and read by
-// the same lanes).  So K, V are read and dK, dV written
-// once, nothing is added in order of arrival, and gradients repeat bitwise.
+// of its four waves share a head, each with consecutive steps of 16 history rows
+// (see attn_fwd.h).  A wave holds dK^T, dV^T of its step in registers while it
+// goes through the pass's MT tiles of 16 targets (of one query head each), whose
+// q and dout rows wait in LDS.  dq of a pass stays in registers over the whole
+// chunk.  More tiles than MT are further passes over the chunk; a chunk is then
+// one step a wave, whose K, V, dK and dV stay in registers from pass to pass
+// (or, where that would make too many chunks, dK and dV of the passes so far
+// wait in fp32 in the workspace, written and read by the same lanes).  So K, V
+// are read and dK, dV written once, nothing is added in order of arrival, and
+// gradients repeat bitwise.
 //
 // Scores are formed as S^T = K Q^T: a lane holds one target, column t = lane %
 // 16, and rows j = 4 (lane / 16) + i, so that the target's constants and its
@@ -172,21 +173,22 @@ __device__ __forceinline__ f32x4 cleared(f32x4 x, uint32_t h) {
 template <typename T> constexpr int kPRow = Elem<T>::bf16 ? 4 * 32 + 16 : 2 * 64 + 16;
 
 // LDS of a workgroup, in bytes.
-template <typename T, int DH, int MT, int JT>
+template <typename T, int DH, int MT>
 struct BwdLds {
   static constexpr int kHead = 16 * MT * (2 * kRowBytes<T, DH> + 16);  // per head of the pass: q rows, dout rows,
   static constexpr int kDo = 16 * MT * kRowBytes<T, DH>;               // and per row maximum, 1 / sum, D, position
   static constexpr int kRow = 2 * kDo;
   static constexpr int kK = 0;                                       // per wave: K rows of the step
-  static constexpr int kKWave = 16 * JT * kRowBytes<T, DH>;
+  static constexpr int kKWave = 16 * kRowBytes<T, DH>;
   static constexpr int kDz = kK + kWaves * kKWave;                   // per wave: w and dz tiles, both terms
-  static constexpr int kDzWave = JT * kPRow<T> * 16;
-  static constexpr int kComb = kDz + kWaves * kDzWave;               // dq of the waves
-  static constexpr int kTables = kComb + kWaves * 16 * (DH + 4) * 4;       // heads, cells, edges, biases, dbias per head, bins
+  static constexpr int kDzWave = 16 * kPRow<T>;
+  static constexpr int kComb = 0;                                    // dq of the waves, between passes
+  static constexpr int kSteps = kDz + kWaves * kDzWave, kJoin = kWaves * 16 * (DH + 4) * 4;
+  static constexpr int kTables = kSteps > kJoin ? kSteps : kJoin;    // heads, cells, edges, biases, bins
   static size_t bytes(int hw, int G, int n, int copies) {
     const size_t slots = n > 1 ? n : 1, heads = static_cast<size_t>(hw) * G;
     return kTables + hw * kHead + 8 * (kCells + 1) +
-           4 * (kMaxBuckets + (heads * (slots + 1) + heads * n + 3) / 4 * 4 + (n ? kWaves * (slots + 1) * copies : 0));
+           4 * (kMaxBuckets + (heads * (slots + 1) + 3) / 4 * 4 + (n ? kWaves * (slots + 1) * copies : 0));
   }
 };
 
@@ -194,18 +196,19 @@ struct BwdLds {
 // sums stay within 36 KB, else every second or fourth, which then take turns.
 inline __host__ __device__ int bin_copies(int n) { return n <= 34 ? 64 : n <= 70 ? 32 : 16; }
 
-// Waves a SIMD is to hold: what the registers allow without spills.
-template <typename T, int DH, int MT>
-constexpr int kBwdWaves = DH == 128 ? 1 : 2;
+// Waves a SIMD is to hold: what the registers allow with few spills (4 tiles of
+// 64 features: one 394 us for two 547; 2 tiles: two 379 for one 461).
+template <typename T, int DH, int MT> constexpr int kBwdWaves = DH == 128 || (DH == 64 && MT == 4) ? 1 : 2;
 
-template <typename T, int DH, int MT, int JT>
+constexpr int kStep = 16;  // history rows of a wave's step
+
+template <typename T, int DH, int MT>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kBwdWaves<T, DH, MT>))) void attn_bwd_kernel(const AttnArgs a) {
   constexpr bool kBf16 = Elem<T>::bf16;
-  constexpr int KS = DH / 32, NE = DH / 16, BJ = 16 * JT;
-  static_assert(JT == 1, "a lane's rows are one run of four");
+  constexpr int KS = DH / 32, NE = DH / 16;
   using F4 = typename Four<T>::type;
   using E8 = Eight<T>;
-  using Lds = BwdLds<T, DH, MT, JT>;
+  using Lds = BwdLds<T, DH, MT>;
   extern __shared__ __align__(16) unsigned char smem[];
   const int nb = a.b.n;
   float* s_comb = reinterpret_cast<float*>(smem + Lds::kComb);
@@ -213,8 +216,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kBwdWa
   int2* s_cells = reinterpret_cast<int2*>(smem + Lds::kTables + a.hw * Lds::kHead);
   int32_t* s_edges = reinterpret_cast<int32_t*>(s_cells + kCells + 1);
   float* s_bias = reinterpret_cast<float*>(s_edges + kMaxBuckets);
-  float* s_db = s_bias + a.hw * a.G * (slots + 1);
-  float* s_bins = s_db + (a.hw * a.G * nb + a.hw * a.G * (slots + 1) + 3) / 4 * 4 - a.hw * a.G * (slots + 1);
+  float* s_bins = s_bias + (a.hw * a.G * (slots + 1) + 3) / 4 * 4;
 
   const int tid = threadIdx.x, lane = tid & 63, c16 = lane & 15, g4 = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -238,7 +240,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kBwdWa
 
   const BucketLds bl{s_cells, s_bias, s_edges, slots, a.b.multi};  // (pointers that are known to be LDS)
   if (a.placed) fill_buckets(a, g0, heads, s_cells, s_bias, s_edges);
-  for (int i = tid; i < heads * nb; i += kThreads) s_db[i] = 0.f;
+  if (ttiles == 0)
+    for (int i = tid; i < heads * nb; i += kThreads) part_db[i] = 0.f;
   unsigned char* mine = smem + Lds::kTables + hs * Lds::kHead;  // q, dout and rows of this wave's head
   const float* s_row = reinterpret_cast<const float*>(mine + Lds::kRow);
   unsigned char* kt = smem + Lds::kK + wave * Lds::kKWave;
@@ -247,36 +250,31 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kBwdWa
   const float gain = kLog2e * (a.cap > 0.f ? a.cap : a.scale), cap_in = a.cap > 0.f ? a.scale / a.cap : 0.f;
 
   const int passes = max(1, groups * a.G);
-  const bool single = a.chunk <= BJ * parts;  // one step a wave
-  f32x4 dk[JT][NE], dv[JT][NE];
-  E8 kf[JT][KS], vf[JT][KS];  // the step's rows, or the next one's once they are used
-  int pj[JT][4];              // positions of rows 4 g4 + i
+  const bool single = a.chunk <= kStep * parts;  // one step a wave
+  f32x4 dk[NE], dv[NE];
+  E8 kf[KS], vf[KS];  // the step's rows, or the next one's once they are used
+  int pj[4];          // positions of rows 4 g4 + i
   const uint32_t lk = static_cast<uint32_t>(a.ldk * sizeof(T)), lv = static_cast<uint32_t>(a.ldv * sizeof(T));
   auto load = [&](int jb) {
     const int last = len - 1 - jb;
     const gptr kp = uniform(static_cast<const T*>(a.k) + (h0 + jb) * a.ldk + g * DH);
     const gptr vp = uniform(static_cast<const T*>(a.v) + (h0 + jb) * a.ldv + g * DH);
+    const int jr = min(c16, last);
+    const uint32_t ak = __umul24(jr, lk) + 8 * g4 * sizeof(T), av = __umul24(jr, lv) + 8 * g4 * sizeof(T);
 #pragma unroll
-    for (int jt = 0; jt < JT; ++jt) {
-      const int jr = min(16 * jt + c16, last);
-      const uint32_t ak = __umul24(jr, lk) + 8 * g4 * sizeof(T), av = __umul24(jr, lv) + 8 * g4 * sizeof(T);
-#pragma unroll
-      for (int s = 0; s < KS; ++s) {
-        kf[jt][s] = load8_at<T>(kp + 32 * s * sizeof(T), ak);
-        vf[jt][s] = load8_at<T>(vp + 32 * s * sizeof(T), av);
-      }
+    for (int s = 0; s < KS; ++s) {
+      kf[s] = load8_at<T>(kp + 32 * s * sizeof(T), ak);
+      vf[s] = load8_at<T>(vp + 32 * s * sizeof(T), av);
     }
     if (a.hist_pos) {
       const gptr hp = uniform(a.hist_pos + h0 + jb);
 #pragma unroll
-      for (int jt = 0; jt < JT; ++jt)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) pj[jt][i] = load_at<int>(hp, 4u * min(16 * jt + 4 * g4 + i, last));
+      for (int i = 0; i < 4; ++i) pj[i] = load_at<int>(hp, 4u * min(4 * g4 + i, last));
     }
   };
   // a pass's rows on their way to LDS, 16 bytes of q and of dout a thread
   constexpr int kPieces = DH * static_cast<int>(sizeof(T)) / 16;
-  constexpr int kHeadsMost = MT == 1 ? kWaves : 1;  // (several heads a workgroup: one tile, see the host)
+  constexpr int kHeadsMost = MT < 4 ? 2 : 1;  // (heads a workgroup, see the host)
   constexpr int kFetch = (16 * MT * kHeadsMost * kPieces + kThreads - 1) / kThreads;
   uint4 fq[kFetch], fd[kFetch];
   f32x4 frow;
@@ -320,7 +318,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kBwdWa
     if (tid < 16 * MT * a.hw)
       reinterpret_cast<f32x4*>(smem + Lds::kTables + tid / (16 * MT) * Lds::kHead + Lds::kRow)[tid % (16 * MT)] = frow;
     if (pass + 1 < passes) fetch(pass + 1);
-    if (nb)
+    if (nb && first == 0)  // (a head's first pass)
       for (int i = 4 * tid; i < kWaves * (slots + 1) * copies; i += 4 * kThreads)
         *reinterpret_cast<f32x4*>(s_bins + i) = f32x4{};
     odd_rows = __syncthreads_or(odd_rows);
@@ -371,79 +369,62 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kBwdWa
     };
 
     // each wave takes consecutive steps (a lane's bucket changes seldom then)
-    const int steps = (j1 - j0 + BJ - 1) / BJ, share = (steps + parts - 1) / parts;
-    const int jfirst = j0 + part * share * BJ, jstop = min(j1, jfirst + share * BJ);
+    const int steps = (j1 - j0 + kStep - 1) / kStep, share = (steps + parts - 1) / parts;
+    const int jfirst = j0 + part * share * kStep, jstop = min(j1, jfirst + share * kStep);
     if (jfirst < min(jstop, single ? j1 : jend) && (pass == 0 || !single)) load(jfirst);
-    for (int jb = jfirst; jb < jstop; jb += BJ) {
-      const int64_t acc_at = ((h0 + jb) * a.Hk + g) * DH;  // fp32 sums of the earlier passes: row jt 16 + c16
+    for (int jb = jfirst; jb < jstop; jb += kStep) {
+      const int64_t acc_at = ((h0 + jb) * a.Hk + g) * DH;  // fp32 sums of the earlier passes: row c16
       const int64_t acc_v = a.n_hist * a.Hk * DH;
       if (pass == 0 || !single) {
 #pragma unroll
-        for (int jt = 0; jt < JT; ++jt)
-#pragma unroll
-          for (int e = 0; e < NE; ++e) {
-            dk[jt][e] = dv[jt][e] = f32x4{};
-            const int j = 16 * jt + c16;
-            if (pass > 0 && jb + j < j1) {
-              const float* p = a.acc_kv + acc_at + static_cast<int64_t>(j) * a.Hk * DH + 4 * (NE * g4 + e);
-              dk[jt][e] = *reinterpret_cast<const f32x4*>(p);
-              dv[jt][e] = *reinterpret_cast<const f32x4*>(p + acc_v);
-            }
+        for (int e = 0; e < NE; ++e) {
+          dk[e] = dv[e] = f32x4{};
+          if (pass > 0 && jb + c16 < j1) {
+            const float* p = a.acc_kv + acc_at + static_cast<int64_t>(c16) * a.Hk * DH + 4 * (NE * g4 + e);
+            dk[e] = *reinterpret_cast<const f32x4*>(p);
+            dv[e] = *reinterpret_cast<const f32x4*>(p + acc_v);
           }
+        }
       }
       if (jb < jend) {
         // K in the other order: rows of the step along the operand
         bool odd_k = false;
 #pragma unroll
-        for (int jt = 0; jt < JT; ++jt)
-#pragma unroll
-          for (int s = 0; s < KS; ++s)
-            store8<T>(reinterpret_cast<T*>(kt + (16 * jt + c16) * kRowBytes<T, DH>) + 32 * s + 8 * g4, kf[jt][s]);
-        f32x4 S[MT][JT], dP[MT][JT];
+        for (int s = 0; s < KS; ++s)
+          store8<T>(reinterpret_cast<T*>(kt + c16 * kRowBytes<T, DH>) + 32 * s + 8 * g4, kf[s]);
+        f32x4 S[MT], dP[MT];
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
-#pragma unroll
-          for (int jt = 0; jt < JT; ++jt) S[mt][jt] = dP[mt][jt] = f32x4{};
+          S[mt] = dP[mt] = f32x4{};
 #pragma unroll
           for (int s = 0; s < KS; ++s) {
             const unsigned char* row = mine + (16 * mt + c16) * kRowBytes<T, DH> + (32 * s + 8 * g4) * sizeof(T);
             const E8 qf = load8<T>(reinterpret_cast<const T*>(row));
             const E8 df = load8<T>(reinterpret_cast<const T*>(row + Lds::kDo));
-#pragma unroll
-            for (int jt = 0; jt < JT; ++jt) {
-              S[mt][jt] = mma32(kf[jt][s], qf, S[mt][jt]);
-              dP[mt][jt] = mma32(vf[jt][s], df, dP[mt][jt]);
-            }
+            S[mt] = mma32(kf[s], qf, S[mt]);
+            dP[mt] = mma32(vf[s], df, dP[mt]);
           }
         }
-        const bool tail = jb + BJ > jend;
-        int pos[JT][4];
+        const bool tail = jb + kStep > jend;
+        int pos[4];
 #pragma unroll
-        for (int jt = 0; jt < JT; ++jt)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) pos[jt][i] = a.hist_pos ? pj[jt][i] : jb + 16 * jt + 4 * g4 + i;
+        for (int i = 0; i < 4; ++i) pos[i] = a.hist_pos ? pj[i] : jb + 4 * g4 + i;
         if (a.placed) {
 #pragma unroll
-          for (int jt = 0; jt < JT; ++jt)
-#pragma unroll
-            for (int s = 0; s < KS; ++s) odd_k |= odd8<T>(kf[jt][s]);
+          for (int s = 0; s < KS; ++s) odd_k |= odd8<T>(kf[s]);
         }
-        if (!single && jb + BJ < min(jstop, jend)) load(jb + BJ);
-        F4 kc[JT][NE];
+        if (!single && jb + kStep < min(jstop, jend)) load(jb + kStep);
+        F4 kc[NE];
         __builtin_amdgcn_wave_barrier();
 #pragma unroll
-        for (int jt = 0; jt < JT; ++jt)
-#pragma unroll
-          for (int e = 0; e < NE; ++e) kc[jt][e] = column4<T, DH>(kt, 16 * jt, e, c16, g4);
+        for (int e = 0; e < NE; ++e) kc[e] = column4<T, DH>(kt, 0, e, c16, g4);
         __builtin_amdgcn_wave_barrier();
-        int pmin = pos[0][0], pmax = pos[0][0];
+        int pmin = pos[0], pmax = pos[0];
 #pragma unroll
-        for (int jt = 0; jt < JT; ++jt)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            pmin = min(pmin, pos[jt][i]);
-            pmax = max(pmax, pos[jt][i]);
-          }
+        for (int i = 0; i < 4; ++i) {
+          pmin = min(pmin, pos[i]);
+          pmax = max(pmax, pos[i]);
+        }
 
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
@@ -452,9 +433,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kBwdWa
           const unsigned char* dt = qt + Lds::kDo;
           const bool slow =
               __ballot(tail || (a.placed && (place_of(tp[mt], pmax) < blo[mt] || place_of(tp[mt], pmin) > bhi[mt]))) != 0;
-          uint32_t hid = 0;  // bit 4 jt + i
-          float w[JT][4], dz[JT][4], dx[JT][4];
-          // (JT = 1) a lane's rows in two buckets at most, or each in its own
+          uint32_t hid = 0;  // bit i
+          float w[4], dz[4], dx[4];
+          // a lane's rows in two buckets at most, or each in its own
           int kk[4];
           TwoBuckets two{0, 0, 0};
           bool each = false;
@@ -465,63 +446,61 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kBwdWa
               if (!each) {
                 const float near = hb[two.near], far = hb[two.far];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) dx[0][i] = sub_sat(tp[mt], pos[0][i]) >= two.edge ? far : near;
+                for (int i = 0; i < 4; ++i) dx[i] = sub_sat(tp[mt], pos[i]) >= two.edge ? far : near;
               } else {
                 int at[4];
                 int2 cell[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                  at[i] = place_of(tp[mt], pos[0][i]);
+                  at[i] = place_of(tp[mt], pos[i]);
                   cell[i] = bl.cells[cell_of(at[i])];
                 }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                   kk[i] = bucket_in(bl, at[i], cell[i]);
-                  dx[0][i] = hb[kk[i]];
+                  dx[i] = hb[kk[i]];
                 }
               }
             } else {
 #pragma unroll
-              for (int i = 0; i < 4; ++i) dx[0][i] = 0.f;
+              for (int i = 0; i < 4; ++i) dx[i] = 0.f;
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-              if (tail && jb + 4 * g4 + i >= jend) dx[0][i] = -INFINITY;
-              hid |= dx[0][i] == -INFINITY ? 1u << i : 0u;
+              if (tail && jb + 4 * g4 + i >= jend) dx[i] = -INFINITY;
+              hid |= dx[i] == -INFINITY ? 1u << i : 0u;
             }
           } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) dx[0][i] = bias[mt];
+            for (int i = 0; i < 4; ++i) dx[i] = bias[mt];
           }
 #pragma unroll
-          for (int jt = 0; jt < JT; ++jt)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              float x = S[mt][jt][i], slope = 1.f;
-              if (a.cap > 0.f) {
-                x = kBf16 ? tanh_fast(x * cap_in, true) : tanhf(x * cap_in);
-                slope = 1.f - x * x;
-              }
-              x = fmaf(x, gain, dx[jt][i]);
-              float p = exp2_fast(x - mx[mt]) * il[mt];
-              float d = p * (dP[mt][jt][i] - D[mt]);
-              if (slow && ((hid >> (4 * jt + i)) & 1)) p = d = 0.f;
-              w[jt][i] = p;
-              dz[jt][i] = d * slope;
-              dx[jt][i] = d;
+          for (int i = 0; i < 4; ++i) {
+            float x = S[mt][i], slope = 1.f;
+            if (a.cap > 0.f) {
+              x = kBf16 ? tanh_fast(x * cap_in, true) : tanhf(x * cap_in);
+              slope = 1.f - x * x;
             }
+            x = fmaf(x, gain, dx[i]);
+            float p = exp2_fast(x - mx[mt]) * il[mt];
+            float d = p * (dP[mt][i] - D[mt]);
+            if (slow && ((hid >> i) & 1)) p = d = 0.f;
+            w[i] = p;
+            dz[i] = d * slope;
+            dx[i] = d;
+          }
           if (nb) {
             if (!slow) {
-              dsum[mt] += (dx[0][0] + dx[0][1]) + (dx[0][2] + dx[0][3]);
+              dsum[mt] += (dx[0] + dx[1]) + (dx[2] + dx[3]);
             } else {
               // what the lane has kept so far goes along where it can
               if (!each) {
                 float near = 0.f, far = 0.f;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                  const bool is_far = sub_sat(tp[mt], pos[0][i]) >= two.edge;
-                  far += is_far ? dx[0][i] : 0.f;
-                  near += is_far ? 0.f : dx[0][i];
+                  const bool is_far = sub_sat(tp[mt], pos[i]) >= two.edge;
+                  far += is_far ? dx[i] : 0.f;
+                  near += is_far ? 0.f : dx[i];
                 }
                 if (__ballot(dsum[mt] != 0.f && bk[mt] != two.far) == 0) {
                   far += dsum[mt];
@@ -529,8 +508,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kBwdWa
                 }
                 add_bins(two.far, far, two.near == two.far ? -1 : two.near, near);
               } else {
-                add_bins(kk[0], dx[0][0], kk[1], dx[0][1]);
-                add_bins(kk[2], dx[0][2], kk[3], dx[0][3]);
+                add_bins(kk[0], dx[0], kk[1], dx[1]);
+                add_bins(kk[2], dx[2], kk[3], dx[3]);
               }
               if (__ballot(dsum[mt] != 0.f)) add_bins(bk[mt], dsum[mt], -1, 0.f);
               dsum[mt] = 0.f;
@@ -539,66 +518,57 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kBwdWa
               keep_bucket(bl, a.masked, bk[mt], bias[mt], blo[mt], bhi[mt]);
             }
           }
-          if (slow && __ballot(hid != (1u << (4 * JT)) - 1u) == 0) continue;
+          if (slow && __ballot(hid != (1u << 4) - 1u) == 0) continue;
 
           // ---- the terms of w and dz; by target in LDS
-          F4 zh[JT], zl[JT];
+          F4 zh, zl;
+          unsigned char* row = dzt + c16 * kPRow<T>;
+          if constexpr (kBf16) {
+            auto cut4 = [](float (&x)[4], bool last) {
+              return last ? make_uint2(high_halves(x[0], x[1]), high_halves(x[2], x[3]))
+                          : make_uint2(cut_bf16(x[0], x[1]), cut_bf16(x[2], x[3]));
+            };
+            *reinterpret_cast<uint2*>(row + 8 * g4) = cut4(w, false);
+            *reinterpret_cast<uint2*>(row + 32 + 8 * g4) = cut4(w, true);
+            const uint2 h = cut4(dz, false), l = cut4(dz, true);
+            *reinterpret_cast<uint2*>(row + 64 + 8 * g4) = h;
+            *reinterpret_cast<uint2*>(row + 96 + 8 * g4) = l;
+            zh = __builtin_bit_cast(s16x4, h);
+            zl = __builtin_bit_cast(s16x4, l);
+          } else {
 #pragma unroll
-          for (int jt = 0; jt < JT; ++jt) {
-            unsigned char* row = dzt + (16 * jt + c16) * kPRow<T>;
-            if constexpr (kBf16) {
-              auto cut4 = [](float (&x)[4], bool last) {
-                return last ? make_uint2(high_halves(x[0], x[1]), high_halves(x[2], x[3]))
-                            : make_uint2(cut_bf16(x[0], x[1]), cut_bf16(x[2], x[3]));
-              };
-              *reinterpret_cast<uint2*>(row + 8 * g4) = cut4(w[jt], false);
-              *reinterpret_cast<uint2*>(row + 32 + 8 * g4) = cut4(w[jt], true);
-              const uint2 h = cut4(dz[jt], false), l = cut4(dz[jt], true);
-              *reinterpret_cast<uint2*>(row + 64 + 8 * g4) = h;
-              *reinterpret_cast<uint2*>(row + 96 + 8 * g4) = l;
-              zh[jt] = __builtin_bit_cast(s16x4, h);
-              zl[jt] = __builtin_bit_cast(s16x4, l);
-            } else {
-#pragma unroll
-              for (int i = 0; i < 4; ++i) zh[jt][i] = dz[jt][i];
-              *reinterpret_cast<f32x4*>(row + 16 * g4) = f32x4{w[jt][0], w[jt][1], w[jt][2], w[jt][3]};
-              *reinterpret_cast<f32x4*>(row + 64 + 16 * g4) = zh[jt];
-            }
+            for (int i = 0; i < 4; ++i) zh[i] = dz[i];
+            *reinterpret_cast<f32x4*>(row + 16 * g4) = f32x4{w[0], w[1], w[2], w[3]};
+            *reinterpret_cast<f32x4*>(row + 64 + 16 * g4) = zh;
           }
           __builtin_amdgcn_wave_barrier();
           const bool careful = slow && (odd_rows || __ballot(odd_k)) && __ballot(hid != 0) != 0;
           // ---- sum over the step's rows: dQ^T += K^T dz; sums over targets:
           // dV^T += dout^T w, dK^T += q^T dz
-          F4 p[JT][4];  // w, dz (bf16: two terms each) of row c16, targets 4 g4 + i
+          F4 p[4];  // w, dz (bf16: two terms each) of row c16, targets 4 g4 + i
+          if constexpr (kBf16) {
+            const unsigned char* at = dzt + (4 * g4 + (c16 >> 2)) * kPRow<T> + 8 * (c16 & 3);
 #pragma unroll
-          for (int jt = 0; jt < JT; ++jt) {
-            if constexpr (kBf16) {
-              const unsigned char* at = dzt + (16 * jt + 4 * g4 + (c16 >> 2)) * kPRow<T> + 8 * (c16 & 3);
+            for (int i = 0; i < 4; ++i) p[i] = __builtin_bit_cast(s16x4, lds_read_tr16(at + 32 * i));
+          } else {
 #pragma unroll
-              for (int i = 0; i < 4; ++i) p[jt][i] = __builtin_bit_cast(s16x4, lds_read_tr16(at + 32 * i));
-            } else {
-#pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                const float* at = reinterpret_cast<const float*>(dzt + (16 * jt + 4 * g4 + i) * kPRow<T>) + c16;
-                p[jt][0][i] = at[0];
-                p[jt][2][i] = at[16];
-              }
+            for (int i = 0; i < 4; ++i) {
+              const float* at = reinterpret_cast<const float*>(dzt + (4 * g4 + i) * kPRow<T>) + c16;
+              p[0][i] = at[0];
+              p[2][i] = at[16];
             }
           }
           if (!careful) {
 #pragma unroll
             for (int e = 0; e < NE; ++e) {
               const F4 dT = column4<T, DH>(dt, 0, e, c16, g4), qT = column4<T, DH>(qt, 0, e, c16, g4);
-#pragma unroll
-              for (int jt = 0; jt < JT; ++jt) {
-                dq[mt][e] = mma16(kc[jt][e], zh[jt], dq[mt][e]);
-                dv[jt][e] = mma16(dT, p[jt][0], dv[jt][e]);
-                dk[jt][e] = mma16(qT, p[jt][2], dk[jt][e]);
-                if constexpr (kBf16) {
-                  dq[mt][e] = mma16(kc[jt][e], zl[jt], dq[mt][e]);
-                  dv[jt][e] = mma16(dT, p[jt][1], dv[jt][e]);
-                  dk[jt][e] = mma16(qT, p[jt][3], dk[jt][e]);
-                }
+              dq[mt][e] = mma16(kc[e], zh, dq[mt][e]);
+              dv[e] = mma16(dT, p[0], dv[e]);
+              dk[e] = mma16(qT, p[2], dk[e]);
+              if constexpr (kBf16) {
+                dq[mt][e] = mma16(kc[e], zl, dq[mt][e]);
+                dv[e] = mma16(dT, p[1], dv[e]);
+                dk[e] = mma16(qT, p[3], dk[e]);
               }
             }
           } else {
@@ -607,28 +577,25 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kBwdWa
 #pragma unroll 1
             for (int col = 0; col < 16; ++col) {
               const uint32_t hq = __shfl(hid, col + 16 * g4);
+              uint32_t hk = 0;  // targets 4 g4 + i that row `col` is hidden from
 #pragma unroll
-              for (int jt = 0; jt < JT; ++jt) {
-                uint32_t hk = 0;  // targets 4 g4 + i that row `col` is hidden from
+              for (int i = 0; i < 4; ++i)
+                hk |= ((__shfl(hid, 4 * g4 + i + 16 * (col >> 2)) >> (col & 3)) & 1u) << i;
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                  hk |= ((__shfl(hid, 4 * g4 + i + 16 * (col >> 2)) >> (4 * jt + (col & 3))) & 1u) << i;
-#pragma unroll
-                for (int e = 0; e < NE; ++e) {
-                  const F4 kx = cleared(kc[jt][e], hq >> (4 * jt)), dx = cleared(column4<T, DH>(dt, 0, e, c16, g4), hk),
-                           qx = cleared(column4<T, DH>(qt, 0, e, c16, g4), hk);
-                  f32x4 nq = mma16(kx, zh[jt], dq[mt][e]), nv = mma16(dx, p[jt][0], dv[jt][e]),
-                        nk = mma16(qx, p[jt][2], dk[jt][e]);
-                  if constexpr (kBf16) {
-                    nq = mma16(kx, zl[jt], nq);
-                    nv = mma16(dx, p[jt][1], nv);
-                    nk = mma16(qx, p[jt][3], nk);
-                  }
-                  if (c16 == col) {
-                    dq[mt][e] = nq;
-                    dv[jt][e] = nv;
-                    dk[jt][e] = nk;
-                  }
+              for (int e = 0; e < NE; ++e) {
+                const F4 kx = cleared(kc[e], hq), dx = cleared(column4<T, DH>(dt, 0, e, c16, g4), hk),
+                         qx = cleared(column4<T, DH>(qt, 0, e, c16, g4), hk);
+                f32x4 nq = mma16(kx, zh, dq[mt][e]), nv = mma16(dx, p[0], dv[e]),
+                      nk = mma16(qx, p[2], dk[e]);
+                if constexpr (kBf16) {
+                  nq = mma16(kx, zl, nq);
+                  nv = mma16(dx, p[1], nv);
+                  nk = mma16(qx, p[3], nk);
+                }
+                if (c16 == col) {
+                  dq[mt][e] = nq;
+                  dv[e] = nv;
+                  dk[e] = nk;
                 }
               }
             }
@@ -636,32 +603,27 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kBwdWa
           __builtin_amdgcn_wave_barrier();
         }
       }
-      // ---- this step's dK, dV: a lane holds DH / 4 consecutive features of row 16 jt + c16
+      // ---- this step's dK, dV: a lane holds DH / 4 consecutive features of row c16
+      if (jb + c16 >= j1 || (single && pass + 1 < passes)) continue;
+      if (pass + 1 < passes) {
+        float* p = a.acc_kv + acc_at + static_cast<int64_t>(c16) * a.Hk * DH + 4 * NE * g4;
 #pragma unroll
-      for (int jt = 0; jt < JT; ++jt) {
-        const int j = 16 * jt + c16;
-        if (jb + j >= j1) continue;
-        if (pass + 1 < passes) {
-          if (single) continue;
-          float* p = a.acc_kv + acc_at + static_cast<int64_t>(j) * a.Hk * DH + 4 * NE * g4;
+        for (int e = 0; e < NE; ++e) {
+          reinterpret_cast<f32x4*>(p)[e] = dk[e];
+          reinterpret_cast<f32x4*>(p + acc_v)[e] = dv[e];
+        }
+      } else {
+        T* kp = static_cast<T*>(a.dk) + (h0 + jb + c16) * a.lddk + g * DH + 4 * NE * g4;
+        T* vp = static_cast<T*>(a.dv) + (h0 + jb + c16) * a.lddv + g * DH + 4 * NE * g4;
 #pragma unroll
-          for (int e = 0; e < NE; ++e) {
-            reinterpret_cast<f32x4*>(p)[e] = dk[jt][e];
-            reinterpret_cast<f32x4*>(p + acc_v)[e] = dv[jt][e];
-          }
-        } else {
-          T* kp = static_cast<T*>(a.dk) + (h0 + jb + j) * a.lddk + g * DH + 4 * NE * g4;
-          T* vp = static_cast<T*>(a.dv) + (h0 + jb + j) * a.lddv + g * DH + 4 * NE * g4;
-#pragma unroll
-          for (int e = 0; e < NE; ++e) {
-            const f32x4 k = dk[jt][e] * a.scale, v = dv[jt][e];
-            if constexpr (kBf16) {
-              reinterpret_cast<uint2*>(kp)[e] = make_uint2(pack_bf16(k[0], k[1]), pack_bf16(k[2], k[3]));
-              reinterpret_cast<uint2*>(vp)[e] = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
-            } else {
-              reinterpret_cast<f32x4*>(kp)[e] = k;
-              reinterpret_cast<f32x4*>(vp)[e] = v;
-            }
+        for (int e = 0; e < NE; ++e) {
+          const f32x4 k = dk[e] * a.scale, v = dv[e];
+          if constexpr (kBf16) {
+            reinterpret_cast<uint2*>(kp)[e] = make_uint2(pack_bf16(k[0], k[1]), pack_bf16(k[2], k[3]));
+            reinterpret_cast<uint2*>(vp)[e] = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
+          } else {
+            reinterpret_cast<f32x4*>(kp)[e] = k;
+            reinterpret_cast<f32x4*>(vp)[e] = v;
           }
         }
       }
@@ -692,20 +654,16 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kBwdWa
       }
     }
     __syncthreads();
-    // dbias of the pass: 4 threads a bucket, one wave's sums each, added over the head's waves
-    for (int i = tid; i < (4 * nb + 63) / 64 * 64; i += kThreads) {
+    // dbias of a head: 4 threads a bucket, one wave's sums each, added over the head's waves
+    for (int i = tid; ttiles > 0 && first + MT >= ttiles && i < (4 * nb + 63) / 64 * 64; i += kThreads) {  // (a head's last pass)
       const int k = i >> 2, wv = i & 3;
       float v = 0.f;
       if (k < nb)
         for (int l = 0; l < copies; ++l) v += s_bins[(wv * (slots + 1) + k) * copies + ((l + k) & (copies - 1))];
       if (a.hw < 4) v += __shfl_xor(v, 2);
       if (a.hw < 2) v += __shfl_xor(v, 1);
-      if (k < nb && wv < a.hw) s_db[(wv * a.G + hh) * nb + k] += v;
+      if (k < nb && wv < a.hw) part_db[(wv * a.G + hh) * nb + k] = v;
     }
-  }
-  if (nb) {
-    __syncthreads();
-    for (int i = tid; i < heads * nb; i += kThreads) part_db[i] = s_db[i];
   }
 }
 
@@ -778,16 +736,15 @@ __global__ __launch_bounds__(256) void attn_bwd_sum_kernel(const AttnArgs a, int
 
 template <typename T, int DH, int MT>
 hipError_t launch_bwd(const AttnArgs& a, hipStream_t st) {
-  constexpr int JT = 1;
-  const size_t lds = BwdLds<T, DH, MT, JT>::bytes(a.hw, a.G, a.b.n, bin_copies(a.b.n));
+  const size_t lds = BwdLds<T, DH, MT>::bytes(a.hw, a.G, a.b.n, bin_copies(a.b.n));
   const int64_t grid = round_up(a.units, kXcds) * (a.Hk / a.hw), rows = ceil_div(a.n_tgt * a.H, 16) + 1;
   if (grid > 0x7fffffff || rows > 0x7fffffff) return hipErrorInvalidValue;
-  hipError_t e = allow_lds<&attn_bwd_kernel<T, DH, MT, JT>>(lds);
+  hipError_t e = allow_lds<&attn_bwd_kernel<T, DH, MT>>(lds);
   if (e != hipSuccess) return e;
   attn_bwd_rows_kernel<T, DH><<<static_cast<unsigned>(rows), 256, 0, st>>>(a);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
-  attn_bwd_kernel<T, DH, MT, JT><<<static_cast<unsigned>(grid), kThreads, lds, st>>>(a);
+  attn_bwd_kernel<T, DH, MT><<<static_cast<unsigned>(grid), kThreads, lds, st>>>(a);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
   const int64_t dq_blocks = a.max_chunks > 1 ? ceil_div(a.n_tgt * a.H, 16) : 0;
@@ -799,7 +756,7 @@ hipError_t launch_bwd(const AttnArgs& a, hipStream_t st) {
 
 template <typename T, int DH>
 hipError_t backward_dh(const AttnArgs& a, int tiles, hipStream_t st) {
-  if constexpr (DH < 128 && Elem<T>::bf16)
+  if constexpr (Elem<T>::bf16)
     if (tiles == 4) return launch_bwd<T, DH, 4>(a, st);
   if constexpr (DH < 128 || Elem<T>::bf16)
     if (tiles == 2) return launch_bwd<T, DH, 2>(a, st);
@@ -815,11 +772,18 @@ hipError_t backward_t(const AttnArgs& a, int dh, int tiles, hipStream_t st) {
 
 }  // namespace
 
-// Row tiles a wave holds: the fewest that take a request's tiles in one pass,
-// up to what registers (dq, DH / 16 x 4 a tile) and LDS allow.
-int backward_tiles(int dtype, int dh, int need) {
-  const int most = dtype == STCA_BF16 ? (dh == 32 ? 4 : 1) : (dh == 128 ? 1 : 2);
-  return need >= 3 && most == 4 ? 4 : need >= 2 && most >= 2 ? 2 : 1;
+// Row tiles a wave holds: the fewest that take a request's `need` tiles of a head
+// in one pass, up to what registers (dq, DH / 16 x 4 a tile) and LDS allow.  In
+// bf16 of 64 and 128 features four spill: they pay where one pass then takes the
+// chunk (128 requests of 2048, 48 targets, 8 heads of 64: 534 us for 1150; 4 of
+// 128: 782 for 1610), but not where the heads that share a kv head or more
+// targets make several passes anyway, whose chunks of one step a wave leave one
+// tile two waves a SIMD (48 requests, 4 heads to a kv head: 276 us for 394; 100
+// targets: 772 for 1101).
+int backward_tiles(int dtype, int dh, int need, int G) {
+  if (dtype != STCA_BF16) return dh < 128 && need >= 2 ? 2 : 1;
+  if (dh > 32 && (G > 1 || need > 4)) return 1;
+  return need >= 3 ? 4 : need == 2 ? 2 : 1;
 }
 
 hipError_t attn_backward(const AttnArgs& a, int dtype, int dh, int tiles, hipStream_t st) {

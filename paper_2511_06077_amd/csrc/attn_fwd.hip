@@ -7,15 +7,9 @@ namespace ops {
 
 namespace {
 
-// The fewest row tiles that hold a request's rows, up to what the registers
-// take beside K and V (the output alone is DH / 16 x 4 registers a tile).
-template <typename T, int DH> constexpr int kMaxTiles = Elem<T>::bf16 ? (DH == 128 ? 2 : 4) : (DH == 128 ? 1 : 2);
-
 template <typename T, int DH>
 hipError_t forward_dh(const AttnArgs& a, int tiles, hipStream_t st) {
-  if constexpr (kMaxTiles<T, DH> >= 4)
-    if (tiles == 4) return launch_fwd<T, kRagged, DH, 4>(a, st);
-  if constexpr (kMaxTiles<T, DH> >= 2)
+  if constexpr (DH < 128)
     if (tiles == 2) return launch_fwd<T, kRagged, DH, 2>(a, st);
   return launch_fwd<T, kRagged, DH, 1>(a, st);
 }
@@ -110,10 +104,14 @@ hipError_t merge_t(const AttnArgs& a, bool paged, int dh, hipStream_t st) {
 
 }  // namespace
 
-int forward_tiles(int dtype, int dh, int max_rows) {
-  const int most = dtype == STCA_BF16 ? (dh == 128 ? 2 : 4) : (dh == 128 ? 1 : 2);
-  const int need = static_cast<int>(ceil_div(max_rows, 16));
-  return need >= 4 && most == 4 ? 4 : need == 3 && most == 4 ? 4 : need >= 2 && most >= 2 ? 2 : 1;
+// Row tiles of 16 a wave holds.  More read K and V less often, fewer leave room
+// for a second wave on the SIMD: four of them were slower throughout (64 targets
+// on packed rows 110 us for 92, of 64 features 453 for 197), and of 128 features
+// two are, except where a page's rows are converted or looked up once for both
+// (8-bit 261 us for 197, bf16 274 for 177).
+int forward_tiles(int dtype, int dh, int max_rows, bool paged) {
+  const int most = dtype == STCA_BF16 ? (dh == 128 && !paged ? 1 : 2) : (dh == 128 ? 1 : 2);
+  return max_rows > 16 ? most : 1;
 }
 
 hipError_t attn_forward(const AttnArgs& a, int dtype, int dh, int tiles, hipStream_t st) {

@@ -76,8 +76,8 @@ hipError_t cache_attend(const AttnArgs& a, bool int8, int dh, int tiles, hipStre
 hipError_t attn_merge(const AttnArgs& a, bool bf16, bool paged, int dh, hipStream_t st);
 hipError_t attn_backward(const AttnArgs& a, int dtype, int dh, int tiles, hipStream_t st);
 
-int forward_tiles(int dtype, int dh, int max_rows);  // row tiles of 16 a wave holds
-int backward_tiles(int dtype, int dh, int need);      // ... of the `need` of a request
+int forward_tiles(int dtype, int dh, int max_rows, bool paged);  // row tiles of 16 a wave holds
+int backward_tiles(int dtype, int dh, int need, int G);  // ... of the `need` of a request's G heads
 
 struct CacheArgs {
   void *k, *v;

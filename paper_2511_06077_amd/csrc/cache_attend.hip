@@ -9,8 +9,6 @@ namespace {
 
 template <int KV, int DH>
 hipError_t attend_dh(const AttnArgs& a, int tiles, hipStream_t st) {
-  if constexpr (DH < 128)
-    if (tiles == 4) return launch_fwd<bf16_bits, KV, DH, 4>(a, st);
   if (tiles == 2) return launch_fwd<bf16_bits, KV, DH, 2>(a, st);
   return launch_fwd<bf16_bits, KV, DH, 1>(a, st);
 }
