@@ -234,7 +234,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kBwdWa
     for (int i = tid; i < heads * nb; i += kThreads) part_db[i] = 0.f;
     return;
   }
-  const int j0 = c * a.chunk, j1 = min(len, j0 + a.chunk);
+  const int j0 = c * a.chunk, j1 = j0 + min(len - j0, a.chunk);
   const int t0 = uniform(clamp_off(a.tgt_off[r], a.n_tgt)), m = max(0, uniform(clamp_off(a.tgt_off[r + 1], a.n_tgt)) - t0);
   const int ttiles = (m + 15) / 16, groups = (ttiles + MT - 1) / MT;  // groups of MT tiles of one head
 

@@ -6,9 +6,15 @@
 // 16 MT rows (target, query head of a kv head's group) and hw kv heads; 4 / hw
 // waves share a head, each with consecutive blocks of 16 NT history rows and
 // softmax statistics and an output of its own, joined in LDS at the end.  Four
-// heads a workgroup read packed rows in whole cache lines at one time (window
-// of 256 requests, 16 targets, 2048 rows, d_h = 32: @@); one head a workgroup
-// spreads a small batch over more of them.  Several chunks leave (output, maximum, sum) partials for attn_merge.
+// heads a workgroup read packed rows in whole cache lines at one time (256
+// requests, 16 targets, 2048 rows, 8 heads of 32 features: 145 us for 204); one
+// head a workgroup spreads a small batch over more of them.  Several chunks
+// leave (output, maximum, sum) partials for attn_merge.
+//
+// Packed rows are bound by their bytes (that window: 541 MB, 113 us at a large
+// copy's rate, takes 134 us, with mask and bias 147), pages by the vector
+// instructions of a score: 8-bit rows are converted for the matrix cores, and a
+// target of few rows fills a quarter of a tile or less.
 //
 // Everything of a block stays in one wave's registers.  Scores are formed
 // transposed, S^T = K Q^T (v_mfma 16x16x32 bf16, or 16x16x4 fp32), so that the
@@ -40,7 +46,6 @@ namespace ops {
 
 constexpr int kRagged = 0, kPagedBf16 = 1, kPagedInt8 = 2;
 constexpr float kSlack = 8.f;  // 2^8: sums and products stay far inside fp32 and bf16 ranges
-
 
 // LDS of a workgroup before the dynamic part's tables.
 template <int DH> constexpr int kCombineFloats = kWaves * 16 * (DH + 2);
@@ -206,7 +211,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kOneWa
   const int rows = m * a.G;
   if (z * 16 * MT >= rows) return;
   const bool split = len > a.chunk;
-  int j1 = min(len, j0 + a.chunk);
+  const int j1 = j0 + min(len - j0, a.chunk);
 
   // tables
   // (pointers that are known to be LDS: set whether used or not)
@@ -261,7 +266,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kOneWa
     if (a.masked && !a.hist_pos) {
 #pragma unroll
       for (int o = 1; o < 16; o <<= 1) seen_max = max(seen_max, __shfl_xor(seen_max, o));
-      jend = static_cast<int>(min<int64_t>(jend, static_cast<int64_t>(seen_max) + 1));
+      jend = max(j0, static_cast<int>(min<int64_t>(jend, static_cast<int64_t>(seen_max) + 1)));
       jend = __builtin_amdgcn_readfirstlane(jend);
     }
 
