@@ -489,6 +489,16 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kBwdWa
             dz[i] = d * slope;
             dx[i] = d;
           }
+          // a row that has all the weight has no gradient: its dP and D differ by
+          // the order of their sums alone (what is not finite stays so)
+          if (__ballot(fmaxf(fmaxf(w[0], w[1]), fmaxf(w[2], w[3])) >= 1.f)) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              if (w[i] >= 1.f) {
+                dz[i] *= 0.f;
+                dx[i] *= 0.f;
+              }
+          }
           if (nb) {
             if (!slow) {
               dsum[mt] += (dx[0] + dx[1]) + (dx[2] + dx[3]);

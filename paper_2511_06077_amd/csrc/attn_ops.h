@@ -94,8 +94,6 @@ struct CacheArgs {
 hipError_t cache_write(const CacheArgs& a, int dtype, bool int8, int dh, hipStream_t st);
 hipError_t cache_read(const CacheArgs& a, int dtype, bool int8, int dh, hipStream_t st);
 
-
-
 // Dynamic LDS beyond the default limit of a launch, granted once per kernel and
 // device.
 template <auto kernel>

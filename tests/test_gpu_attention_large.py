@@ -46,6 +46,21 @@ def test_the_largest_tables(torch, dtype, dh):  # noqa: F811
     assert max(e.values()) <= 1.0, e
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dh,H,Hk,cap", [(32, 2, 2, 0.0), (64, 4, 1, 3.0), (128, 2, 2, 0.0)])
+def test_a_single_visible_row_has_no_gradient(torch, dtype, dh, H, Hk, cap):  # noqa: F811
+    """Its weight is 1 whatever its score: dq, dk and dbias are 0, not what
+    rounding leaves of a difference; a value that is not finite still shows."""
+    c = Case(torch, [1, 700, 1], [3, 18, 40], dtype=dtype, dh=dh, H=H, Hk=Hk, nb=8, masked=True, cap=cap)
+    c.tgt_pos[:] = 0
+    got = c.step()
+    assert max(c.compare(dict(out=got["out"], dv=got["dv"]), c.oracle()).values()) <= 1.0
+    assert not any(got[n].any() for n in ("dq", "dk", "dbias"))
+    c.t["dout"][1, 0, 5] = float("nan")
+    got = c.step()
+    assert got["dq"][1, 0].isnan().all() and not got["dq"][2:].any()
+
+
 @pytest.mark.parametrize("m,H", [(1, 2), (530, 8)])
 def test_many_partials(torch, m, H):  # noqa: F811
     """Partials of few rows are joined by more lanes than those of many."""
