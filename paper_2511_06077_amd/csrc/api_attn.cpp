@@ -412,6 +412,7 @@ stca_status_t stca_attn_backward(const stca_attn_t* attn, const stca_batch_t* ba
   a.chunk = p.chunk;
   a.max_chunks = p.max_chunks;
   a.units = p.units;
+  a.bufs = p.passes > 1 ? 2 : 1;
   a.hw = p.hw;
   a.zgroups = 1;
   a.part_dq = at<float>(ws, p.part_dq);

@@ -44,6 +44,8 @@ namespace ops {
 
 namespace {
 
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
 __device__ __forceinline__ f32x4 mfma16_bf16(s16x4 a, s16x4 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(a, b, c, 0, 0, 0);
 }
@@ -184,10 +186,11 @@ struct BwdLds {
   static constexpr int kDzWave = 16 * kPRow<T>;
   static constexpr int kComb = 0;                                    // dq of the waves, between passes
   static constexpr int kSteps = kDz + kWaves * kDzWave, kJoin = kWaves * 16 * (DH + 4) * 4;
-  static constexpr int kTables = kSteps > kJoin ? kSteps : kJoin;    // heads, cells, edges, biases, bins
-  static size_t bytes(int hw, int G, int n, int copies) {
+  static constexpr int kTables = kSteps > kJoin ? kSteps : kJoin;    // heads (twice for several passes), flags, cells, edges, biases, bins
+  static constexpr int kFlags = 2 * kWaves * 4;  // of a pass (two at a time) and wave: a row is not finite
+  static size_t bytes(int bufs, int hw, int G, int n, int copies) {
     const size_t slots = n > 1 ? n : 1, heads = static_cast<size_t>(hw) * G;
-    return kTables + hw * kHead + 8 * (kCells + 1) +
+    return kTables + bufs * hw * kHead + kFlags + 8 * (kCells + 1) +
            4 * (kMaxBuckets + (heads * (slots + 1) + 3) / 4 * 4 + (n ? kWaves * (slots + 1) * copies : 0));
   }
 };
@@ -213,7 +216,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kBwdWa
   const int nb = a.b.n;
   float* s_comb = reinterpret_cast<float*>(smem + Lds::kComb);
   const int slots = max(nb, 1), copies = bin_copies(nb);
-  int2* s_cells = reinterpret_cast<int2*>(smem + Lds::kTables + a.hw * Lds::kHead);
+  int* s_flags = reinterpret_cast<int*>(smem + Lds::kTables + a.bufs * a.hw * Lds::kHead);
+  int2* s_cells = reinterpret_cast<int2*>(s_flags + 2 * kWaves);
   int32_t* s_edges = reinterpret_cast<int32_t*>(s_cells + kCells + 1);
   float* s_bias = reinterpret_cast<float*>(s_edges + kMaxBuckets);
   float* s_bins = s_bias + (a.hw * a.G * (slots + 1) + 3) / 4 * 4;
@@ -242,14 +246,13 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kBwdWa
   if (a.placed) fill_buckets(a, g0, heads, s_cells, s_bias, s_edges);
   if (ttiles == 0)
     for (int i = tid; i < heads * nb; i += kThreads) part_db[i] = 0.f;
-  unsigned char* mine = smem + Lds::kTables + hs * Lds::kHead;  // q, dout and rows of this wave's head
-  const float* s_row = reinterpret_cast<const float*>(mine + Lds::kRow);
   unsigned char* kt = smem + Lds::kK + wave * Lds::kKWave;
   unsigned char* dzt = smem + Lds::kDz + wave * Lds::kDzWave;
   float* bins = s_bins + wave * (slots + 1) * copies;
   const float gain = kLog2e * (a.cap > 0.f ? a.cap : a.scale), cap_in = a.cap > 0.f ? a.scale / a.cap : 0.f;
 
-  const int passes = max(1, groups * a.G);
+  constexpr bool kOnePass = DH > 32 && MT == 4;  // (the host's rule: these tiles only where they make one)
+  const int passes = kOnePass ? 1 : max(1, groups * a.G);
   const bool single = a.chunk <= kStep * parts;  // one step a wave
   f32x4 dk[NE], dv[NE];
   E8 kf[KS], vf[KS];  // the step's rows, or the next one's once they are used
@@ -278,50 +281,65 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kBwdWa
   constexpr int kFetch = (16 * MT * kHeadsMost * kPieces + kThreads - 1) / kThreads;
   uint4 fq[kFetch], fd[kFetch];
   f32x4 frow;
-  auto fetch = [&](int pass) {
-    const int hh = groups ? pass / groups : 0, first = groups ? pass % groups * MT : 0;
+  const uint32_t lq = static_cast<uint32_t>(a.ldq * sizeof(T)), ldo = static_cast<uint32_t>(a.H * DH * sizeof(T));
+  auto fetch = [&](int hh, int first) {
+    const int64_t row0 = t0 + 16 * static_cast<int64_t>(first), head0 = g0 * a.G + hh;
+    const int left = m - 16 * first;
+    const gptr qp = uniform(static_cast<const T*>(a.q) + row0 * a.ldq + head0 * DH);
+    const gptr dp = uniform(static_cast<const T*>(a.dout) + (row0 * a.H + head0) * DH);
 #pragma unroll
     for (int n = 0; n < kFetch; ++n) {
-      const int i = tid + n * kThreads, piece = i % kPieces, at = i / kPieces, hd = at / (16 * MT);
-      const int t = 16 * first + at % (16 * MT);
+      const int i = tid + n * kThreads, piece = i % kPieces, at = i / kPieces, hd = at / (16 * MT), row = at % (16 * MT);
       fq[n] = fd[n] = uint4{};
-      if (hd < a.hw && t < m) {
-        const int64_t h = (g0 + hd) * a.G + hh;
-        fq[n] = reinterpret_cast<const uint4*>(static_cast<const T*>(a.q) + (t0 + t) * a.ldq + h * DH)[piece];
-        fd[n] = reinterpret_cast<const uint4*>(static_cast<const T*>(a.dout) + ((t0 + t) * static_cast<int64_t>(a.H) + h) * DH)[piece];
+      if (hd < a.hw && row < left) {
+        const uint32_t in = hd * a.G * (DH * static_cast<int>(sizeof(T))) + 16 * piece;
+        fq[n] = __builtin_bit_cast(uint4, load_at<u32x4>(qp, __umul24(row, lq) + in));
+        fd[n] = __builtin_bit_cast(uint4, load_at<u32x4>(dp, __umul24(row, ldo) + in));
       }
     }
-    const int hd = tid / (16 * MT), t = 16 * first + tid % (16 * MT);
+    const int hd = tid / (16 * MT), row = tid % (16 * MT);
     frow = f32x4{INFINITY, 0.f, 0.f, 0.f};  // (a row without a target has no weight anywhere)
     if (hd < a.hw && m > 0) {
-      const f32x4 x = reinterpret_cast<const f32x4*>(a.rows)[(t0 + min(t, m - 1)) * static_cast<int64_t>(a.H) +
-                                                             (g0 + hd) * a.G + hh];
-      frow = t < m ? x : f32x4{INFINITY, 0.f, 0.f, x[3]};
+      const f32x4 x = load_at<f32x4>(uniform(a.rows + 4 * (row0 * a.H + head0)),
+                                     16u * (__umul24(min(row, left - 1), a.H) + hd * a.G));
+      frow = row < left ? x : f32x4{INFINITY, 0.f, 0.f, x[3]};
     }
   };
-  fetch(0);
+  fetch(0, 0);
+  if (nb)
+    for (int i = 4 * tid; i < kWaves * (slots + 1) * copies; i += 4 * kThreads) *reinterpret_cast<f32x4*>(s_bins + i) = f32x4{};
+  int hh = 0, first = 0;  // the pass's query head of the group and first tile
   for (int pass = 0; pass < passes; ++pass) {
-    const int hh = groups ? pass / groups : 0, first = groups ? pass % groups * MT : 0;
     const int held = min(MT, ttiles - first);
-    __syncthreads();
+    const bool last_of_head = first + MT >= ttiles;
+    // one pass's rows are read while the next one's arrive
+    const int buf = pass & (a.bufs - 1);
+    unsigned char* rows = smem + Lds::kTables + buf * a.hw * Lds::kHead;
     int odd_rows = 0;
 #pragma unroll
     for (int n = 0; n < kFetch; ++n) {
       const int i = tid + n * kThreads, piece = i % kPieces, at = i / kPieces, hd = at / (16 * MT), row = at % (16 * MT);
       if (hd < a.hw) {
-        unsigned char* to = smem + Lds::kTables + hd * Lds::kHead + row * kRowBytes<T, DH> + 16 * piece;
+        unsigned char* to = rows + hd * Lds::kHead + row * kRowBytes<T, DH> + 16 * piece;
         *reinterpret_cast<uint4*>(to) = fq[n];
         *reinterpret_cast<uint4*>(to + Lds::kDo) = fd[n];
         if (a.placed) odd_rows |= odd16<T>(fq[n]) || odd16<T>(fd[n]);
       }
     }
     if (tid < 16 * MT * a.hw)
-      reinterpret_cast<f32x4*>(smem + Lds::kTables + tid / (16 * MT) * Lds::kHead + Lds::kRow)[tid % (16 * MT)] = frow;
-    if (pass + 1 < passes) fetch(pass + 1);
-    if (nb && first == 0)  // (a head's first pass)
-      for (int i = 4 * tid; i < kWaves * (slots + 1) * copies; i += 4 * kThreads)
-        *reinterpret_cast<f32x4*>(s_bins + i) = f32x4{};
-    odd_rows = __syncthreads_or(odd_rows);
+      reinterpret_cast<f32x4*>(rows + tid / (16 * MT) * Lds::kHead + Lds::kRow)[tid % (16 * MT)] = frow;
+    if (a.placed) {
+      odd_rows = __ballot(odd_rows) != 0;
+      if (lane == 0) s_flags[buf * kWaves + wave] = odd_rows;
+    }
+    if (!kOnePass && pass + 1 < passes) fetch(last_of_head ? hh + 1 : hh, last_of_head ? 0 : first + MT);
+    __syncthreads();
+    if (a.placed) {
+      const int4 f = *reinterpret_cast<const int4*>(s_flags + buf * kWaves);
+      odd_rows = f.x | f.y | f.z | f.w;
+    }
+    const unsigned char* mine = rows + hs * Lds::kHead;  // q, dout and rows of this wave's head
+    const float* s_row = reinterpret_cast<const float*>(mine + Lds::kRow);
 
     // this lane's target of each tile: its constants, the bucket it keeps
     f32x4 dq[MT][NE];
@@ -649,31 +667,44 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kBwdWa
       for (int e = 0; e < NE; ++e)
         reinterpret_cast<f32x4*>(s_comb + (wave * 16 + c16) * (DH + 4) + 4 * NE * g4)[e] = dq[mt][e];
       __syncthreads();
-      const int row = tid >> 4, t = 16 * (first + mt) + row;
-      for (int hd = 0; hd < a.hw && t < m; ++hd) {
-        const int64_t tr = t0 + t, h = (g0 + hd) * a.G + hh;
-        const int f = (tid & 15) * NE;
+      const int row = tid >> 4, f = (tid & 15) * NE;
+      const int64_t row0 = t0 + 16 * static_cast<int64_t>(first + mt), head0 = g0 * a.G + hh;
+      for (int hd = 0; hd < a.hw && 16 * (first + mt) + row < m; ++hd) {
+        float v[NE];
 #pragma unroll
         for (int e = 0; e < NE; ++e) {
-          float v = 0.f;
-          for (int wv = hd; wv < kWaves; wv += a.hw) v += s_comb[(wv * 16 + row) * (DH + 4) + f + e];
-          v *= a.scale;
-          if (a.max_chunks > 1) a.part_dq[((static_cast<int64_t>(c) * a.n_tgt + tr) * a.H + h) * DH + f + e] = v;
-          else static_cast<T*>(a.dq)[tr * a.lddq + h * DH + f + e] = from_f32<T>(v);
+          v[e] = 0.f;
+          for (int wv = hd; wv < kWaves; wv += a.hw) v[e] += s_comb[(wv * 16 + row) * (DH + 4) + f + e];
+          v[e] *= a.scale;
+        }
+        if (a.max_chunks > 1) {
+          float* p = a.part_dq + ((c * a.n_tgt + row0) * a.H + head0) * DH + (row * a.H + hd * a.G) * DH + f;
+#pragma unroll
+          for (int e = 0; e < NE; e += 2) *reinterpret_cast<f32x2*>(p + e) = f32x2{v[e], v[e + 1]};
+        } else {
+          T* p = static_cast<T*>(a.dq) + (row0 + row) * a.lddq + (head0 + hd * a.G) * DH + f;
+#pragma unroll
+          for (int e = 0; e < NE; ++e) p[e] = from_f32<T>(v[e]);
         }
       }
     }
-    __syncthreads();
-    // dbias of a head: 4 threads a bucket, one wave's sums each, added over the head's waves
-    for (int i = tid; ttiles > 0 && first + MT >= ttiles && i < (4 * nb + 63) / 64 * 64; i += kThreads) {  // (a head's last pass)
+    // dbias of a head: 4 threads a bucket, one wave's sums each (cleared for the
+    // next head), added over the head's waves
+    for (int i = tid; last_of_head && ttiles > 0 && i < (4 * nb + 63) / 64 * 64; i += kThreads) {
       const int k = i >> 2, wv = i & 3;
       float v = 0.f;
       if (k < nb)
-        for (int l = 0; l < copies; ++l) v += s_bins[(wv * (slots + 1) + k) * copies + ((l + k) & (copies - 1))];
+        for (int l = 0; l < copies; ++l) {
+          float* p = s_bins + (wv * (slots + 1) + k) * copies + ((l + k) & (copies - 1));
+          v += *p;
+          *p = 0.f;
+        }
       if (a.hw < 4) v += __shfl_xor(v, 2);
       if (a.hw < 2) v += __shfl_xor(v, 1);
       if (k < nb && wv < a.hw) part_db[(wv * a.G + hh) * nb + k] = v;
     }
+    first = last_of_head ? 0 : first + MT;
+    hh += last_of_head;
   }
 }
 
@@ -746,7 +777,7 @@ __global__ __launch_bounds__(256) void attn_bwd_sum_kernel(const AttnArgs a, int
 
 template <typename T, int DH, int MT>
 hipError_t launch_bwd(const AttnArgs& a, hipStream_t st) {
-  const size_t lds = BwdLds<T, DH, MT>::bytes(a.hw, a.G, a.b.n, bin_copies(a.b.n));
+  const size_t lds = BwdLds<T, DH, MT>::bytes(a.bufs, a.hw, a.G, a.b.n, bin_copies(a.b.n));
   const int64_t grid = round_up(a.units, kXcds) * (a.Hk / a.hw), rows = ceil_div(a.n_tgt * a.H, 16) + 1;
   if (grid > 0x7fffffff || rows > 0x7fffffff) return hipErrorInvalidValue;
   hipError_t e = allow_lds<&attn_bwd_kernel<T, DH, MT>>(lds);
@@ -787,12 +818,13 @@ hipError_t backward_t(const AttnArgs& a, int dh, int tiles, hipStream_t st) {
 // bf16 of 64 and 128 features four spill: they pay where one pass then takes the
 // chunk (128 requests of 2048, 48 targets, 8 heads of 64: 534 us for 1150; 4 of
 // 128: 782 for 1610), but not where the heads that share a kv head or more
-// targets make several passes anyway, whose chunks of one step a wave leave one
-// tile two waves a SIMD (48 requests, 4 heads to a kv head: 276 us for 394; 100
-// targets: 772 for 1101).
+// targets make several passes anyway, of chunks of one step a wave: there two
+// waves a SIMD count, which two tiles of 64 features leave and one of 128 (48
+// requests, 4 heads of 64 to a kv head: two 249 us, one 254, four 394; 100
+// targets, heads of 64: 690, 717 and 1101; of 128: one 741, four 1017).
 int backward_tiles(int dtype, int dh, int need, int G) {
   if (dtype != STCA_BF16) return dh < 128 && need >= 2 ? 2 : 1;
-  if (dh > 32 && (G > 1 || need > 4)) return 1;
+  if (dh > 32 && (G > 1 || need > 4)) return dh == 64 && need > 1 ? 2 : 1;
   return need >= 3 ? 4 : need == 2 ? 2 : 1;
 }
 

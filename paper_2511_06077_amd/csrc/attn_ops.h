@@ -54,6 +54,7 @@ struct AttnArgs {
   float scale, cap;
   int64_t n_hist, n_tgt;
   int32_t chunk, max_chunks, units, zgroups;
+  int32_t bufs;                    // backward: a workgroup's rows in LDS, 2 where there are several passes
   int32_t hw;                      // kv heads of a workgroup (1, 2 or 4): a wave has one, 4 / hw waves share it
   // forward
   void* out;
