@@ -124,7 +124,8 @@ int chunk_for(int64_t rows, int64_t per_row, int per_cu, int step) {
 // line whose other half another workgroup reads later comes from memory twice
 // (window of 256 requests of 2048 rows, 8 heads of 32: 4 heads a workgroup 145
 // us forward for 204 with one, 2 heads 360 us backward for 549).  In the
-// backward two (rows of every head wait in LDS), and one where each holds four
+// backward two (rows of every head wait in LDS: four take 375 us where two take
+// 373, with a bias of 32 buckets 447 for 404), and one where each holds four
 // tiles; only where a wave to a head then has 256 history rows on every SIMD of
 // the card, since fewer heads a workgroup are shorter chunks for as many waves.
 int heads_of(int Hk, int64_t n_hist, bool backward, int tiles) {

@@ -199,14 +199,18 @@ struct BwdLds {
 // sums stay within 36 KB, else every second or fourth, which then take turns.
 inline __host__ __device__ int bin_copies(int n) { return n <= 34 ? 64 : n <= 70 ? 32 : 16; }
 
-// Waves a SIMD is to hold: what the registers allow with few spills (4 tiles of
-// 64 features: one 394 us for two 547; 2 tiles: two 379 for one 461).
+// Waves a SIMD is to hold: what the registers allow with few spills (48 requests,
+// 4 heads of 64 to a kv head, 4 tiles: one 394 us, two 547), and no more than
+// two, since the workgroups of a chunk's heads, which read parts of the same
+// DRAM pages, drift apart the more of them run (window of 256 requests, 16
+// targets, 2048 rows, 8 heads of 32: two 312 us, three 335, four 357).
 template <typename T, int DH, int MT> constexpr int kBwdWaves = DH == 128 || (DH == 64 && MT == 4) ? 1 : 2;
+template <typename T, int DH, int MT> constexpr int kBwdMost = kBwdWaves<T, DH, MT> == 1 ? 8 : 2;
 
 constexpr int kStep = 16;  // history rows of a wave's step
 
-template <typename T, int DH, int MT>
-__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kBwdWaves<T, DH, MT>))) void attn_bwd_kernel(const AttnArgs a) {
+template <typename T, int DH, int MT, bool kOnePass>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kBwdWaves<T, DH, MT>, kBwdMost<T, DH, MT>))) void attn_bwd_kernel(const AttnArgs a) {
   constexpr bool kBf16 = Elem<T>::bf16;
   constexpr int KS = DH / 32, NE = DH / 16;
   using F4 = typename Four<T>::type;
@@ -251,7 +255,6 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kBwdWa
   float* bins = s_bins + wave * (slots + 1) * copies;
   const float gain = kLog2e * (a.cap > 0.f ? a.cap : a.scale), cap_in = a.cap > 0.f ? a.scale / a.cap : 0.f;
 
-  constexpr bool kOnePass = DH > 32 && MT == 4;  // (the host's rule: these tiles only where they make one)
   const int passes = kOnePass ? 1 : max(1, groups * a.G);
   const bool single = a.chunk <= kStep * parts;  // one step a wave
   f32x4 dk[NE], dv[NE];
@@ -775,17 +778,17 @@ __global__ __launch_bounds__(256) void attn_bwd_sum_kernel(const AttnArgs a, int
   }
 }
 
-template <typename T, int DH, int MT>
+template <typename T, int DH, int MT, bool kOnePass>
 hipError_t launch_bwd(const AttnArgs& a, hipStream_t st) {
   const size_t lds = BwdLds<T, DH, MT>::bytes(a.bufs, a.hw, a.G, a.b.n, bin_copies(a.b.n));
   const int64_t grid = round_up(a.units, kXcds) * (a.Hk / a.hw), rows = ceil_div(a.n_tgt * a.H, 16) + 1;
   if (grid > 0x7fffffff || rows > 0x7fffffff) return hipErrorInvalidValue;
-  hipError_t e = allow_lds<&attn_bwd_kernel<T, DH, MT>>(lds);
+  hipError_t e = allow_lds<&attn_bwd_kernel<T, DH, MT, kOnePass>>(lds);
   if (e != hipSuccess) return e;
   attn_bwd_rows_kernel<T, DH><<<static_cast<unsigned>(rows), 256, 0, st>>>(a);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
-  attn_bwd_kernel<T, DH, MT><<<static_cast<unsigned>(grid), kThreads, lds, st>>>(a);
+  attn_bwd_kernel<T, DH, MT, kOnePass><<<static_cast<unsigned>(grid), kThreads, lds, st>>>(a);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
   const int64_t dq_blocks = a.max_chunks > 1 ? ceil_div(a.n_tgt * a.H, 16) : 0;
@@ -795,13 +798,21 @@ hipError_t launch_bwd(const AttnArgs& a, hipStream_t st) {
   return hipGetLastError();
 }
 
+// (A kernel of its own where one pass is all: without the state of the others
+// fewer registers spill, 48 targets of 4 heads of 128 features 589 us for 868.)
 template <typename T, int DH>
 hipError_t backward_dh(const AttnArgs& a, int tiles, hipStream_t st) {
-  if constexpr (Elem<T>::bf16)
-    if (tiles == 4) return launch_bwd<T, DH, 4>(a, st);
-  if constexpr (DH < 128 || Elem<T>::bf16)
-    if (tiles == 2) return launch_bwd<T, DH, 2>(a, st);
-  return launch_bwd<T, DH, 1>(a, st);
+  const bool one = a.bufs == 1;
+  if constexpr (Elem<T>::bf16) {
+    if (DH > 32 && tiles == 4) return launch_bwd<T, DH, 4, true>(a, st);  // (see backward_tiles)
+    if constexpr (DH == 32)
+      if (tiles == 4) return one ? launch_bwd<T, DH, 4, true>(a, st) : launch_bwd<T, DH, 4, false>(a, st);
+  }
+  if constexpr (DH < 128)
+    if (tiles == 2) return one ? launch_bwd<T, DH, 2, true>(a, st) : launch_bwd<T, DH, 2, false>(a, st);
+  if constexpr (DH == 128 && Elem<T>::bf16)
+    if (tiles == 2) return launch_bwd<T, DH, 2, true>(a, st);
+  return one ? launch_bwd<T, DH, 1, true>(a, st) : launch_bwd<T, DH, 1, false>(a, st);
 }
 
 template <typename T>
