@@ -207,6 +207,22 @@ inline __host__ __device__ int bin_copies(int n) { return n <= 34 ? 64 : n <= 70
 template <typename T, int DH, int MT> constexpr int kBwdWaves = DH == 128 || (DH == 64 && MT == 4) ? 1 : 2;
 template <typename T, int DH, int MT> constexpr int kBwdMost = kBwdWaves<T, DH, MT> == 1 ? 8 : 2;
 
+// The kernel's arguments, `kFresh`: as loads that are not moved out of a loop.
+// Kept from pass to pass they take more scalar registers than there are (48
+// requests, 4 heads of 64 to a kv head: 247 us for 238, without bias 158 for
+// 143); with one pass the loads cost more (415 us for 404).
+typedef const __attribute__((address_space(4))) AttnArgs KernelArgs;
+template <bool kFresh>
+__device__ __forceinline__ decltype(auto) again(const AttnArgs& a) {
+  if constexpr (kFresh) {
+    uint64_t p = reinterpret_cast<uint64_t>(__builtin_amdgcn_kernarg_segment_ptr());  // (`a` is the only argument)
+    asm volatile("" : "+s"(p));
+    return *reinterpret_cast<KernelArgs*>(p);
+  } else {
+    return (a);
+  }
+}
+
 constexpr int kStep = 16;  // history rows of a wave's step
 
 template <typename T, int DH, int MT, bool kOnePass>
@@ -261,7 +277,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kBwdWa
   E8 kf[KS], vf[KS];  // the step's rows, or the next one's once they are used
   int pj[4];          // positions of rows 4 g4 + i
   const uint32_t lk = static_cast<uint32_t>(a.ldk * sizeof(T)), lv = static_cast<uint32_t>(a.ldv * sizeof(T));
-  auto load = [&](int jb) {
+  auto load = [&](const auto& a, int jb) {
     const int last = len - 1 - jb;
     const gptr kp = uniform(static_cast<const T*>(a.k) + (h0 + jb) * a.ldk + g * DH);
     const gptr vp = uniform(static_cast<const T*>(a.v) + (h0 + jb) * a.ldv + g * DH);
@@ -285,7 +301,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kBwdWa
   uint4 fq[kFetch], fd[kFetch];
   f32x4 frow;
   const uint32_t lq = static_cast<uint32_t>(a.ldq * sizeof(T)), ldo = static_cast<uint32_t>(a.H * DH * sizeof(T));
-  auto fetch = [&](int hh, int first) {
+  auto fetch = [&](const auto& a, int hh, int first) {
     const int64_t row0 = t0 + 16 * static_cast<int64_t>(first), head0 = g0 * a.G + hh;
     const int left = m - 16 * first;
     const gptr qp = uniform(static_cast<const T*>(a.q) + row0 * a.ldq + head0 * DH);
@@ -308,11 +324,13 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kBwdWa
       frow = row < left ? x : f32x4{INFINITY, 0.f, 0.f, x[3]};
     }
   };
-  fetch(0, 0);
+  fetch(a, 0, 0);
   if (nb)
     for (int i = 4 * tid; i < kWaves * (slots + 1) * copies; i += 4 * kThreads) *reinterpret_cast<f32x4*>(s_bins + i) = f32x4{};
   int hh = 0, first = 0;  // the pass's query head of the group and first tile
+  const AttnArgs& once = a;
   for (int pass = 0; pass < passes; ++pass) {
+    const auto& a = again<!kOnePass>(once);
     const int held = min(MT, ttiles - first);
     const bool last_of_head = first + MT >= ttiles;
     // one pass's rows are read while the next one's arrive
@@ -335,7 +353,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kBwdWa
       odd_rows = __ballot(odd_rows) != 0;
       if (lane == 0) s_flags[buf * kWaves + wave] = odd_rows;
     }
-    if (!kOnePass && pass + 1 < passes) fetch(last_of_head ? hh + 1 : hh, last_of_head ? 0 : first + MT);
+    if (!kOnePass && pass + 1 < passes) fetch(a, last_of_head ? hh + 1 : hh, last_of_head ? 0 : first + MT);
     __syncthreads();
     if (a.placed) {
       const int4 f = *reinterpret_cast<const int4*>(s_flags + buf * kWaves);
@@ -392,7 +410,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kBwdWa
     // each wave takes consecutive steps (a lane's bucket changes seldom then)
     const int steps = (j1 - j0 + kStep - 1) / kStep, share = (steps + parts - 1) / parts;
     const int jfirst = j0 + part * share * kStep, jstop = min(j1, jfirst + share * kStep);
-    if (jfirst < min(jstop, single ? j1 : jend) && (pass == 0 || !single)) load(jfirst);
+    if (jfirst < min(jstop, single ? j1 : jend) && (pass == 0 || !single)) load(a, jfirst);
     for (int jb = jfirst; jb < jstop; jb += kStep) {
       const int64_t acc_at = ((h0 + jb) * a.Hk + g) * DH;  // fp32 sums of the earlier passes: row c16
       const int64_t acc_v = a.n_hist * a.Hk * DH;
@@ -434,7 +452,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kBwdWa
 #pragma unroll
           for (int s = 0; s < KS; ++s) odd_k |= odd8<T>(kf[s]);
         }
-        if (!single && jb + kStep < min(jstop, jend)) load(jb + kStep);
+        if (!single && jb + kStep < min(jstop, jend)) load(a, jb + kStep);
         F4 kc[NE];
         __builtin_amdgcn_wave_barrier();
 #pragma unroll
