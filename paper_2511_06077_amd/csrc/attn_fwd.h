@@ -11,7 +11,7 @@
 // head a workgroup spreads a small batch over more of them.  Several chunks
 // leave (output, maximum, sum) partials for attn_merge.
 //
-// Packed rows are bound by their bytes (that window: 541 MB, 113 us at a large
+// Packed rows are bound by their bytes (that window: 541 MB, 104 us at a large
 // copy's rate, takes 134 us, with mask and bias 147), pages by the vector
 // instructions of a score: 8-bit rows are converted for the matrix cores, and a
 // target of few rows fills a quarter of a tile or less.

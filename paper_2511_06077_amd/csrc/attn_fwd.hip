@@ -87,12 +87,11 @@ __global__ __launch_bounds__(256) void attn_merge_kernel(const AttnArgs a, bool 
 
 // A row's DH features by 16 lanes, its chunks one after the other; where there are
 // many chunks and too few rows to fill the card, by 16 times as many lanes, each
-// with every 16th chunk (8 rows of 40 chunks 4.2 us for 5.8, 384 of 128 features
-// 9.5 for 10.6; 32768 rows of 8 chunks fill it either way, and the split costs
-// 40 us).
+// with every 16th chunk (8 rows of 40 chunks 4.2 us for 5.8, 1536 of 10 9.5 for
+// 10.6; but 2048 rows of 8 chunks 1.6 us more, 4096 4.6, 32768 40).
 template <typename T, int DH>
 hipError_t merge_dh(const AttnArgs& a, bool paged, hipStream_t st) {
-  const int split = a.max_chunks >= 8 && a.n_tgt * a.H <= 4096 ? 16 : 1;
+  const int split = a.max_chunks >= 8 && a.n_tgt * a.H <= 1536 ? 16 : 1;
   const int64_t grid = ceil_div(a.n_tgt * a.H, 16 / split);
   if (grid > 0x7fffffff) return hipErrorInvalidValue;
   if (split == 16) attn_merge_kernel<T, DH, 16><<<static_cast<unsigned>(grid), 256, 0, st>>>(a, paged);
