@@ -156,6 +156,7 @@ class CrossAttention(_Scores):
         if backward:
             n = stca.stca_attn_saved_size(self.attn, self.batch)
             self.saved = torch.empty(max(n, 16), dtype=torch.uint8, device=self.device)
+        self.has_saved = False
 
     def _in(self, q, k, v, tgt_pos, hist_pos, bias):
         torch = _torch()
@@ -175,6 +176,7 @@ class CrossAttention(_Scores):
             out = torch.empty((self.n_tgt, self.n_heads, self.d_head), dtype=self.dtype, device=self.device)
             stca.stca_attn_forward(self.attn, self.batch, given, out, self.saved, self.ws, self.ws_bytes,
                                    self.stream() if stream is None else stream)
+        self.has_saved = self.saved is not None
         return out
 
     def backward(self, dout, q, k, v, tgt_pos=None, hist_pos=None, bias=None, stream: Optional[int] = None):
@@ -183,6 +185,8 @@ class CrossAttention(_Scores):
         torch = _torch()
         if self.saved is None:
             raise ValueError("backward: the plan was made without backward=True")
+        if not self.has_saved:
+            raise ValueError("backward: no forward before it")
         given = self._in(q, k, v, tgt_pos, hist_pos, bias)
         _flat("dout", dout, self.dtype, (self.n_tgt, self.n_heads, self.d_head), self.device)
         with _on(self.device):
@@ -203,7 +207,9 @@ class HistoryCache:
     """Pages of K and V rows, 8-bit ("int8") or bf16 ("bf16"); positions=True
     keeps every row's position beside it.  Pages are handed out by the caller:
     table [requests][..] (int32) lists each request's pages, and its row i is
-    slot i % page_size of page table[i // page_size]."""
+    slot i % page_size of page table[i // page_size].  Writes to slots of their own
+    and reads may overlap on several streams; device_status is then the last one's
+    to end."""
 
     def __init__(self, n_pages: int, page_size: int, n_kv_heads: int, d_head: int, fmt: str = "int8",
                  positions: bool = False, device="cuda"):

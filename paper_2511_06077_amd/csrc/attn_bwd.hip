@@ -310,14 +310,16 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kBwdWa
     for (int n = 0; n < kFetch; ++n) {
       const int i = tid + n * kThreads, piece = i % kPieces, at = i / kPieces, hd = at / (16 * MT), row = at % (16 * MT);
       fq[n] = fd[n] = uint4{};
-      if (hd < a.hw && row < left) {
-        const uint32_t in = hd * a.G * (DH * static_cast<int>(sizeof(T))) + 16 * piece;
-        fq[n] = __builtin_bit_cast(uint4, load_at<u32x4>(qp, __umul24(row, lq) + in));
-        fd[n] = __builtin_bit_cast(uint4, load_at<u32x4>(dp, __umul24(row, ldo) + in));
+      if (hd < a.hw && m > 0) {
+        const uint32_t in = hd * a.G * (DH * static_cast<int>(sizeof(T))) + 16 * piece, t = min(row, left - 1);
+        fq[n] = __builtin_bit_cast(uint4, load_at<u32x4>(qp, __umul24(t, lq) + in));
+        fd[n] = __builtin_bit_cast(uint4, load_at<u32x4>(dp, __umul24(t, ldo) + in));
       }
     }
     const int hd = tid / (16 * MT), row = tid % (16 * MT);
-    frow = f32x4{INFINITY, 0.f, 0.f, 0.f};  // (a row without a target has no weight anywhere)
+    // a row behind the last target is that target again without weight: of zeros,
+    // its product with an infinite K would be NaN where no target's score is
+    frow = f32x4{INFINITY, 0.f, 0.f, 0.f};
     if (hd < a.hw && m > 0) {
       const f32x4 x = load_at<f32x4>(uniform(a.rows + 4 * (row0 * a.H + head0)),
                                      16u * (__umul24(min(row, left - 1), a.H) + hd * a.G));

@@ -61,6 +61,35 @@ def test_a_single_visible_row_has_no_gradient(torch, dtype, dh, H, Hk, cap):  # 
     assert got["dq"][1, 0].isnan().all() and not got["dq"][2:].any()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("m", [3, 16, 37, 90])
+def test_infinite_scores_under_a_cap(torch, dtype, m):  # noqa: F811
+    """An infinite K is the cap's end as a score: out, dv and dbias stay finite,
+    also where a tile of targets is not full; dq is 0 times infinity."""
+    c = Case(torch, [70, 40], [m, 2], dtype=dtype, nb=4, cap=3.0)
+    c.t["q"], c.f["q"] = c.t["q"].abs(), np.abs(c.f["q"])
+    for row in (5, 69):
+        c.t["k"][row, 0, 7] = float("inf")
+        c.f["k"][row, 0, 7] = np.inf
+    with np.errstate(invalid="ignore"):
+        ref = c.oracle()
+    got = c.step()
+    # (an infinite score has no error under the cap: the largest finite one counts)
+    k = np.where(np.isfinite(c.f["k"]), np.abs(c.f["k"]), 0.0)
+    score = max(float((c.scale * c.f["q"][:, h] @ k[:, h].T).max()) for h in range(2))
+    assert max(c.compare({n: got[n] for n in ("out", "dv", "dbias")}, {**ref, "score": score}).values()) <= 1.0
+    assert got["dq"][:m, 0, 7].isnan().all() and bool(got["dk"].isfinite().all())
+
+
+def test_backward_needs_a_forward(torch):  # noqa: F811
+    c = Case(torch, [9], [2])
+    q, k, v, dout = c.dev("q", "k", "v", "dout")
+    with pytest.raises(ValueError, match="no forward"):
+        c.plan(backward=True).backward(dout, q, k, v)
+    with pytest.raises(ValueError, match="without backward"):
+        c.plan().backward(dout, q, k, v)
+
+
 @pytest.mark.parametrize("m,H", [(1, 2), (530, 8)])
 def test_many_partials(torch, m, H):  # noqa: F811
     """Partials of few rows are joined by more lanes than those of many."""
