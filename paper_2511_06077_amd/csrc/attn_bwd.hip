@@ -716,12 +716,14 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kBwdWa
     for (int i = tid; last_of_head && ttiles > 0 && i < (4 * nb + 63) / 64 * 64; i += kThreads) {
       const int k = i >> 2, wv = i & 3;
       float v = 0.f;
-      if (k < nb)
-        for (int l = 0; l < copies; ++l) {
-          float* p = s_bins + (wv * (slots + 1) + k) * copies + ((l + k) & (copies - 1));
-          v += *p;
-          *p = 0.f;
-        }
+      if (k < nb) {
+        float* p = s_bins + (wv * (slots + 1) + k) * copies;
+#pragma unroll 16
+        for (int l = 0; l < copies; ++l) v += p[(l + k) & (copies - 1)];
+        if (pass + 1 < passes)
+#pragma unroll 16
+          for (int l = 0; l < copies; ++l) p[(l + k) & (copies - 1)] = 0.f;
+      }
       if (a.hw < 4) v += __shfl_xor(v, 2);
       if (a.hw < 2) v += __shfl_xor(v, 1);
       if (k < nb && wv < a.hw) part_db[(wv * a.G + hh) * nb + k] = v;
