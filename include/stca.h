@@ -427,7 +427,10 @@ stca_status_t stca_forward_paper_profiled(const stca_dims_t* dims, const stca_ba
  * bf16 storage the weights enter the matrix cores as two bf16 terms.
  *
  * Calls of one batch on different streams need distinct workspaces.  Targets
- * of a request without history are legal here. */
+ * of a request without history are legal here.  Offsets are checked on the
+ * device too: a request of more rows, or in the backward targets, than a call
+ * planned on the host copies takes is STCA_ERR_INVALID_ARG there, its results are
+ * undefined, and nothing is written outside the buffers. */
 typedef struct {
   int32_t n_heads;           /* query heads, a multiple of n_kv_heads (at most 64 times as many) */
   int32_t n_kv_heads;        /* heads of K and V, each shared by n_heads / n_kv_heads query heads */

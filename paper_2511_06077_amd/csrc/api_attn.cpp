@@ -364,6 +364,7 @@ stca_status_t stca_attn_forward(const stca_attn_t* attn, const stca_batch_t* bat
   a.units = p.units;
   a.hw = p.hw;
   a.zgroups = p.zgroups;
+  a.max_tgt = INT32_MAX;
   a.out = out;
   if (saved) {
     stca_attn_saved_layout_t l;
@@ -416,6 +417,7 @@ stca_status_t stca_attn_backward(const stca_attn_t* attn, const stca_batch_t* ba
   a.bufs = p.passes > 1 ? 2 : 1;
   a.hw = p.hw;
   a.zgroups = 1;
+  a.max_tgt = p.passes > 1 ? INT32_MAX : 16 * p.btiles;
   a.part_dq = at<float>(ws, p.part_dq);
   a.part_db = at<float>(ws, p.part_db);
   a.acc_kv = at<float>(ws, p.acc_kv);
@@ -495,6 +497,7 @@ stca_status_t stca_cache_attn(const stca_attn_t* attn, const stca_cache_t* cache
   a.units = p.units;
   a.hw = p.hw;
   a.zgroups = p.zgroups;
+  a.max_tgt = INT32_MAX;
   a.out = out;
   a.part_o = at<float>(ws, p.part_o);
   a.part_ml = at<float>(ws, p.part_ml);

@@ -210,7 +210,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kOneWa
   const int t0 = uniform(clamp_off(a.tgt_off[r], a.n_tgt)), m = uniform(clamp_off(a.tgt_off[r + 1], a.n_tgt)) - t0;
   const int rows = m * a.G;
   if (z * 16 * MT >= rows) return;
-  const bool split = len > a.chunk;
+  // (one chunk on the host's offsets: there are no partials, whatever the device's say)
+  const bool split = a.max_chunks > 1 && len > a.chunk;
   const int j1 = j0 + min(len - j0, a.chunk);
 
   // tables

@@ -54,6 +54,7 @@ struct AttnArgs {
   float scale, cap;
   int64_t n_hist, n_tgt;
   int32_t chunk, max_chunks, units, zgroups;
+  int32_t max_tgt;                 // most targets of a request that the launch takes
   int32_t bufs;                    // backward: a workgroup's rows in LDS, 2 where there are several passes
   int32_t hw;                      // kv heads of a workgroup (1, 2 or 4): a wave has one, 4 / hw waves share it
   // forward
@@ -293,13 +294,16 @@ __device__ __forceinline__ int check_pages(const int32_t* table, int64_t row, in
 
 // The whole of a call's device offsets, lengths and pages as its status: one
 // workgroup of its own, the only writer of the status word.  As many threads a
-// request as there are (a wave a request took 0.3 us for each of them).
+// request as there are (a wave a request took 0.3 us for each of them).  A
+// request of more rows or targets than the host's offsets have, on which chunks,
+// passes and the workspace were planned, is not taken whole: an error as well.
 __device__ __forceinline__ void check_call(const AttnArgs& a, bool paged) {
   int bad = 0;
   const int per = max(1, static_cast<int>(blockDim.x) / a.R), sub = threadIdx.x % per;
   for (int r = threadIdx.x / per; r < a.R; r += blockDim.x / per) {
     bad |= a.tgt_off[r + 1] < a.tgt_off[r] || (r == 0 && a.tgt_off[0] != 0) ||
            (r == a.R - 1 && a.tgt_off[a.R] != a.n_tgt);
+    bad |= static_cast<int64_t>(a.tgt_off[r + 1]) - a.tgt_off[r] > a.max_tgt;
     if (paged) {
       const int len = a.lens[r];
       bad |= len < 0 || len > a.max_len;
@@ -308,6 +312,7 @@ __device__ __forceinline__ void check_call(const AttnArgs& a, bool paged) {
     } else {
       bad |= a.hist_off[r + 1] < a.hist_off[r] || (r == 0 && a.hist_off[0] != 0) ||
              (r == a.R - 1 && a.hist_off[a.R] != a.n_hist);
+      bad |= static_cast<int64_t>(a.hist_off[r + 1]) - a.hist_off[r] > static_cast<int64_t>(a.max_chunks) * a.chunk;
     }
   }
   bad = __syncthreads_or(bad);
