@@ -127,11 +127,15 @@ int chunk_for(int64_t rows, int64_t per_row, int per_cu, int step) {
 // backward two (rows of every head wait in LDS: four take 375 us where two take
 // 373, with a bias of 32 buckets 447 for 404), and one where each holds four
 // tiles; only where a wave to a head then has 256 history rows on every SIMD of
-// the card, since fewer heads a workgroup are shorter chunks for as many waves.
-int heads_of(int Hk, int64_t n_hist, bool backward, int tiles) {
+// the card, since fewer heads a workgroup are shorter chunks for as many waves;
+// and no more than the LDS holds the tables of (`lds` of a workgroup of hw heads).
+template <typename Lds>
+int heads_of(int Hk, int64_t n_hist, bool backward, int tiles, Lds lds) {
   const int most = !backward ? 4 : tiles < 4 ? 2 : 1;
-  const int some = most % 4 == 0 && Hk % 4 == 0 ? 4 : most % 2 == 0 && Hk % 2 == 0 ? 2 : 1;
-  return n_hist * Hk >= 256 * 4 * static_cast<int64_t>(device_cus()) ? some : 1;
+  int hw = most % 4 == 0 && Hk % 4 == 0 ? 4 : most % 2 == 0 && Hk % 2 == 0 ? 2 : 1;
+  if (n_hist * Hk < 256 * 4 * static_cast<int64_t>(device_cus())) hw = 1;
+  while (hw > 1 && lds(hw) > kMaxLds) hw /= 2;
+  return hw;
 }
 
 bool ragged_plan(const stca_attn_t* a, const stca_batch_t* b, bool backward, Plan* p) {
@@ -150,7 +154,12 @@ bool ragged_plan(const stca_attn_t* a, const stca_batch_t* b, bool backward, Pla
   const int64_t need = ceil_div(max_m, 16);
   p->btiles = backward_tiles(a->dtype, dh, static_cast<int>(std::min<int64_t>(need, 1 << 20)), G);
   p->passes = static_cast<int>(std::max<int64_t>(1, ceil_div(need, p->btiles) * G));
-  p->hw = backward && p->passes > 1 ? 1 : heads_of(Hk, b->n_hist, backward, p->btiles);
+  auto lds = [&](int hw) {
+    return backward ? backward_lds(a->dtype, dh, p->btiles, p->passes > 1 ? 2 : 1, hw, G, a->n_buckets)
+                    : forward_lds(dh, hw, G, a->n_buckets, 0);
+  };
+  p->hw = backward && p->passes > 1 ? 1 : heads_of(Hk, b->n_hist, backward, p->btiles, lds);
+  if (lds(p->hw) > kMaxLds) return false;
   const int parts = 4 / p->hw;
   if (backward && p->passes > 1) {
     // one step a wave, unless that makes more chunks than dq's partials are worth
@@ -254,6 +263,7 @@ bool paged_plan(const stca_attn_t* a, const stca_cache_t* c, const stca_cache_ba
   if (units * Hk * p->zgroups > 0x7f000000) return false;
   p->units = static_cast<int>(units);
   p->hw = 1;  // (a head's pages are contiguous)
+  if (forward_lds(dh, 1, G, a->n_buckets, p->chunk / c->page_size + 1) > kMaxLds) return false;
   Bump m;
   p->hdr = m.take(sizeof(WsHeader));
   const size_t rows = static_cast<size_t>(b->n_tgt) * H, split = p->max_chunks > 1 ? p->max_chunks : 0;

@@ -859,6 +859,21 @@ hipError_t backward_t(const AttnArgs& a, int dh, int tiles, hipStream_t st) {
 
 }  // namespace
 
+size_t backward_lds(int dtype, int dh, int tiles, int bufs, int hw, int G, int n) {
+  auto of = [&](auto lds) { return decltype(lds)::bytes(bufs, hw, G, n, bin_copies(n)); };
+  auto type = [&](auto t) {
+    using T = decltype(t);
+    auto width = [&](auto w) {
+      constexpr int DH = decltype(w)::value;
+      return tiles == 4 ? of(BwdLds<T, DH, 4>{}) : tiles == 2 ? of(BwdLds<T, DH, 2>{}) : of(BwdLds<T, DH, 1>{});
+    };
+    using std::integral_constant;
+    return dh == 32 ? width(integral_constant<int, 32>{}) : dh == 64 ? width(integral_constant<int, 64>{})
+                                                                       : width(integral_constant<int, 128>{});
+  };
+  return dtype == STCA_BF16 ? type(bf16_bits{}) : type(float{});
+}
+
 // Row tiles a wave holds: the fewest that take a request's `need` tiles of a head
 // in one pass, up to what registers (dq, DH / 16 x 4 a tile) and LDS allow.  In
 // bf16 of 64 and 128 features four spill: they pay where one pass then takes the

@@ -37,8 +37,6 @@
 // every score looks its bucket up.
 #pragma once
 
-#include <algorithm>
-
 #include "attn_ops.h"
 
 namespace stca {
@@ -47,8 +45,7 @@ namespace ops {
 constexpr int kRagged = 0, kPagedBf16 = 1, kPagedInt8 = 2;
 constexpr float kSlack = 8.f;  // 2^8: sums and products stay far inside fp32 and bf16 ranges
 
-// LDS of a workgroup before the dynamic part's tables.
-template <int DH> constexpr int kCombineFloats = kWaves * 16 * (DH + 2);
+template <int DH> constexpr int kCombineFloats = kWaves * 16 * (DH + 2);  // LDS before the tables (see forward_lds)
 
 template <typename T, int KV, int DH, int NT>
 struct Block {
@@ -710,8 +707,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kOneWa
 template <typename T, int KV, int DH, int MT>
 hipError_t launch_fwd(const AttnArgs& a, hipStream_t st) {
   const int64_t pages = KV == kRagged ? 0 : (a.chunk >> a.page_shift) + 1;
-  const size_t lds = 4 * (kCombineFloats<DH> + 2 * (kCells + 1) + kMaxBuckets +
-                          static_cast<int64_t>(a.hw) * a.G * (std::max(a.b.n, 1) + 1) + pages);
+  const size_t lds = forward_lds(DH, a.hw, a.G, a.b.n, pages);
   const int64_t grid = round_up(a.units, kXcds) * (a.Hk / a.hw) * a.zgroups + 1;
   if (grid > 0x7fffffff) return hipErrorInvalidValue;
   const hipError_t e = allow_lds<&attn_fwd_kernel<T, KV, DH, MT>>(lds);

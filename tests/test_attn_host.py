@@ -215,3 +215,25 @@ def test_oracle_quantises_to_the_nearest():
     err = np.abs(O.held(n, e) - x)
     assert (err <= step[:, None] * np.where(np.abs(x) > 127.5 * step[:, None], 1.0, 0.5)).all()
     assert O.quantise(np.zeros((1, 32)))[1][0] == 1 and O.quantise(np.full((1, 32), np.nan))[1][0] == 255
+
+
+@pytest.mark.parametrize("d_head", [32, 64, 128])
+@pytest.mark.parametrize("dtype", [stca.STCA_F32, stca.STCA_BF16])
+def test_every_accepted_table_has_its_lds(d_head, dtype):
+    """Query heads a kv head and buckets up to their limits, of one kv head and
+    of several to a workgroup, packed and paged, few targets, many and none:
+    every plan fits a CU's LDS (one that does not has no size)."""
+    for buckets in (0, 1, 34, 35, 70, 71, 100, 127, 128):
+        edges = np.arange(1, max(buckets, 1), dtype=np.int32)
+        for G in (1, 2, 3, 16, 31, 32, 33, 48, 61, 62, 63, 64):
+            for Hk in (1, 2, 4):
+                if Hk * G * d_head > 65536:
+                    continue
+                a = attn(n_heads=Hk * G, n_kv_heads=Hk, d_head=d_head, dtype=dtype, n_buckets=buckets, edges=edges)
+                for m in (0, 1, 16, 40, 70):
+                    b = batch([0, 300000, 300001], [0, m, m])
+                    assert stca.stca_attn_workspace_size(a, b, False) and stca.stca_attn_workspace_size(a, b, True)
+                if dtype == stca.STCA_BF16:
+                    c = cache(n_kv_heads=Hk, d_head=d_head, page_size=16)
+                    assert stca.stca_cache_attn_workspace_size(
+                        a, c, stca.cache_batch(1, 3, 0x10000, 0x20000, 1000000, 0x30000, 1 << 20))

@@ -65,3 +65,34 @@ def test_stale_host_offsets(torch, dtype, dh, H, Hk, L, m, dev_L, dev_m, forward
                            dv=g["dv"].view(torch, q.dtype, v.shape),
                            dbias=g["dbias"].view(torch, torch.float32, (H, 4))), ref)
         assert max(e.values()) <= 1.0, e
+
+
+def some_heads(c, heads):
+    """The case with the given query heads of each kv head's group alone."""
+    import copy
+    G = c.H // c.Hk
+    pick = [g * G + h for g in range(c.Hk) for h in heads]
+    s = copy.copy(c)
+    s.f = {n: x[:, pick] if n in ("q", "dout") else x for n, x in c.f.items()}
+    s.H, s.bias = len(pick), c.bias[pick]
+    return s, pick
+
+
+@pytest.mark.parametrize("dh,G,nb", [(32, 2, 16), (128, 64, 128), (128, 32, 128)])
+def test_tables_of_several_heads_a_workgroup(torch, dh, G, nb):  # noqa: F811
+    """Four kv heads a workgroup where their groups' biases fit the LDS, else
+    fewer; forward, the first and the last head of every group."""
+    c = Case(torch, [40000, 0, 33, 26000], [2, 3, 1, 2], H=4 * G, Hk=4, dh=dh, nb=nb, masked=True)
+    plan = c.plan()
+    out = plan.forward(*c.dev("q", "k", "v"), **c.given())
+    assert plan.device_status() == 0
+    s, pick = some_heads(c, (0, G - 1))
+    e = s.compare(dict(out=out[:, pick]), s.oracle(grads=False))
+    assert max(e.values()) <= 1.0, e
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_the_largest_tables_without_targets(torch, dtype):  # noqa: F811
+    c = Case(torch, [60000, 6000], [0, 0], H=256, Hk=4, dh=128, nb=128, dtype=dtype)
+    got = c.step()
+    assert not any(x.any() for x in got.values())
