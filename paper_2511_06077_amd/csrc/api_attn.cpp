@@ -128,13 +128,16 @@ int chunk_for(int64_t rows, int64_t per_row, int per_cu, int step) {
 // 373, with a bias of 32 buckets 447 for 404), and one where each holds four
 // tiles; only where a wave to a head then has 256 history rows on every SIMD of
 // the card, since fewer heads a workgroup are shorter chunks for as many waves;
-// and no more than the LDS holds the tables of (`lds` of a workgroup of hw heads).
+// and no more than the LDS holds the tables of (`lds` of a workgroup of hw heads),
+// forward of two workgroups, which is what the registers leave room for (32
+// requests of 4096 rows, 4 x 32 heads of 128 features, 128 buckets: one of 4 heads
+// a CU 342 us, two of 2 heads 151; 64 x 4096, 4 x 64 of 32: 840 and 406).
 template <typename Lds>
 int heads_of(int Hk, int64_t n_hist, bool backward, int tiles, Lds lds) {
   const int most = !backward ? 4 : tiles < 4 ? 2 : 1;
   int hw = most % 4 == 0 && Hk % 4 == 0 ? 4 : most % 2 == 0 && Hk % 2 == 0 ? 2 : 1;
   if (n_hist * Hk < 256 * 4 * static_cast<int64_t>(device_cus())) hw = 1;
-  while (hw > 1 && lds(hw) > kMaxLds) hw /= 2;
+  while (hw > 1 && lds(hw) > (backward ? kMaxLds : kMaxLds / 2)) hw /= 2;
   return hw;
 }
 
