@@ -583,7 +583,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kBwdWa
           unsigned char* row = dzt + c16 * kPRow<T>;
           if constexpr (kBf16) {
             auto cut4 = [](float (&x)[4], bool last) {
-              return last ? make_uint2(high_halves(x[0], x[1]), high_halves(x[2], x[3]))
+              return last ? make_uint2(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]))
                           : make_uint2(cut_bf16(x[0], x[1]), cut_bf16(x[2], x[3]));
             };
             *reinterpret_cast<uint2*>(row + 8 * g4) = cut4(w, false);

@@ -353,7 +353,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kOneWa
 
     // scores in units of log2 e: gain (q k) + bias, or with a cap gain tanh(cap_in (q k)) + bias
     const float gain = kLog2e * (a.cap > 0.f ? a.cap : a.scale), cap_in = a.cap > 0.f ? a.scale / a.cap : 0.f;
-    const bool whole = a.sa != nullptr;
+    const bool whole = !kPaged && a.sa != nullptr;
 
     auto compute = [&](Blk& b, int jb, bool more) {
       // V operand of O^T: rows NJ g4 + 8 s + 0..7, feature NE c16 + e
@@ -588,13 +588,14 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kOneWa
           }
         } else {
           // a term at a time: its operands, then its products
-          auto term = [&] {
+          auto term = [&](bool last) {
             bf16x8 p[NT / 2];
 #pragma unroll
             for (int s = 0; s < NT / 2; ++s) {
               uint32_t w[4];
 #pragma unroll
-              for (int k = 0; k < 4; ++k) w[k] = cut_bf16(x[8 * s + 2 * k], x[8 * s + 2 * k + 1]);
+              for (int k = 0; k < 4; ++k)
+                w[k] = last ? pack_bf16(x[8 * s + 2 * k], x[8 * s + 2 * k + 1]) : cut_bf16(x[8 * s + 2 * k], x[8 * s + 2 * k + 1]);
               p[s] = __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
             }
             if (!careful) {
@@ -620,9 +621,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kOneWa
               }
             }
           };
-          term();
-          term();
-          if (whole) term();
+          term(false);
+          term(!whole);
+          if (whole) term(true);
         }
       }
     };

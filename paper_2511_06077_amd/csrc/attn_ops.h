@@ -146,8 +146,10 @@ __device__ __forceinline__ uint32_t high_halves(float a, float b) {
   return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
 }
 // Splits a and b into bf16 terms by cutting bits off: the first returned, the
-// rest left in a and b.  Each term holds 8 significant bits, so two leave less
-// than 2^-16 of a value and three nothing of an fp32.
+// rest left in a and b.  Each term holds 8 significant bits, so three leave
+// nothing of an fp32.  Where two are all, the second is rounded (pack_bf16): that
+// leaves at most 2^-16 of a value, to either side; cut, it left up to 2^-15, always
+// towards zero, and a sum of many weights was low by 2^-17 of it.
 __device__ __forceinline__ uint32_t cut_bf16(float& a, float& b) {
   const uint32_t t = high_halves(a, b);
   a -= __uint_as_float(__float_as_uint(a) & 0xffff0000u);

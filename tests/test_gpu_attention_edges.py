@@ -96,3 +96,75 @@ def test_the_largest_tables_without_targets(torch, dtype):  # noqa: F811
     c = Case(torch, [60000, 6000], [0, 0], H=256, Hk=4, dh=128, nb=128, dtype=dtype)
     got = c.step()
     assert not any(x.any() for x in got.values())
+
+
+def balanced(plus, minus):
+    """An order of len(plus) + len(minus) terms whose running sum stays small:
+    indices of plus, and len(plus) + those of minus."""
+    order, total, i, j = [], 0.0, 0, 0
+    while i < len(plus) or j < len(minus):
+        if j == len(minus) or (i < len(plus) and total <= 0):
+            order.append(i)
+            total += plus[i]
+            i += 1
+        else:
+            order.append(len(plus) + j)
+            total -= minus[j]
+            j += 1
+    return np.array(order)
+
+
+# What two bf16 terms leave of a weight may lie on either side of it.  N weights
+# whose low bits are spread evenly, against exact ones (1, or 1/2) of the other
+# sign: what is left of the N adds up to no more than Hoeffding's bound for N
+# values within +-2^-16 of their power of two (chance 1e-9), beside 6e-7 of each
+# for exp2, the sum and its reciprocal (some ulps); cut to one side it is N 2^-16
+# of that power of two at the mean, four times as much.
+N_LOW = 4096
+HOEFFDING = np.sqrt(N_LOW * np.log(2e9) / 2)
+
+
+def test_weights_are_not_low_forward(torch):  # noqa: F811
+    rng = np.random.default_rng(0)
+    c = Case(torch, [1], [1], H=1, Hk=1)
+    k = np.zeros((N_LOW, 32))
+    k[:, :2] = torch.from_numpy(-rng.uniform(0.01, 0.68, size=(N_LOW, 2))).to(torch.bfloat16).double().numpy()
+    q = np.zeros((1, 1, 32))
+    q[0, 0, :2] = 1.0, 2.0 ** -8
+    w = np.exp(k @ q[0, 0])  # within 1/2 .. 1
+    ones = int(round(w.sum()))
+    at = balanced(np.ones(ones), w)
+    k = np.concatenate([np.zeros((ones, 32)), k])[at]
+    v = np.concatenate([np.ones(ones), -np.ones(N_LOW)])[at][:, None] * np.ones(32)
+    c.hoff, c.toff, c.scale = offsets([len(at)]), offsets([1]), 1.0
+    for n, x in (("q", q), ("k", k[:, None]), ("v", v[:, None])):
+        c.f[n], c.t[n] = x, torch.from_numpy(x).to(torch.bfloat16)
+        assert np.array_equal(c.t[n].double().numpy(), x)
+    out = c.plan().forward(*c.dev("q", "k", "v")).double().cpu().numpy()[0, 0]
+    want, total = (ones - w.sum()) / (ones + w.sum()), ones + w.sum()
+    bound = (HOEFFDING * 2.0 ** -16 + 6e-7 * total) / total + 2.0 ** -8 * abs(want)
+    print("[low]", np.abs(out - want).max() / bound)
+    assert (np.abs(out - want) <= bound).all()
+
+
+def test_weights_are_not_low_backward(torch):  # noqa: F811
+    rng = np.random.default_rng(1)
+    q = np.zeros((N_LOW, 1, 32))
+    q[:, 0, :2] = torch.from_numpy(rng.uniform(0.01, 1.0, size=(N_LOW, 2))).to(torch.bfloat16).double().numpy()
+    k = np.zeros((2, 1, 32))
+    k[1, 0, :2] = 1.0, 2.0 ** -8
+    w = 1 / (1 + np.exp(q[:, 0] @ k[1, 0]))  # of row 0: within 1/4 .. 1/2
+    halves = int(round(2 * w.sum()))
+    at = balanced(np.full(halves, 0.5), w)
+    q = np.concatenate([np.zeros((halves, 1, 32)), q])[at]
+    dout = np.concatenate([np.ones(halves), -np.ones(N_LOW)])[at][:, None, None] * np.ones((1, 1, 32))
+    c = Case(torch, [2], [len(at)], H=1, Hk=1)
+    c.scale = 1.0
+    for n, x in (("q", q), ("k", k), ("dout", dout)):
+        c.f[n], c.t[n] = x, torch.from_numpy(x).to(torch.bfloat16)
+        assert np.array_equal(c.t[n].double().numpy(), x)
+    dv = c.step()["dv"][0, 0].double().cpu().numpy()
+    want = 0.5 * halves - w.sum()
+    bound = HOEFFDING * 2.0 ** -17 + 6e-7 * 0.5 * len(at) + 2.0 ** -8 * abs(want)
+    print("[low]", np.abs(dv - want).max() / bound)
+    assert (np.abs(dv - want) <= bound).all()
