@@ -25,7 +25,8 @@
 // V of packed rows is read a row at a time, DH / 16 elements a lane, and pairs
 // of rows are merged by byte permutes; V pages hold rows along the fast axis.
 // A row's maximum is only raised (and O rescaled) when a score passes it by
-// kSlack: a vote per block instead of a reduction across lanes.
+// kSlack: a vote per block instead of a reduction across lanes.  (The maximum of rows
+// that are taken again, see kLargeSum, lies `above` the scores from the start.)
 //
 // P enters the matrix cores as bf16 terms: two (one term's rounding would show
 // in the output as a second rounding of its size, 1.7e-3 -> 2.4e-3 relative to
@@ -43,7 +44,12 @@ namespace stca {
 namespace ops {
 
 constexpr int kRagged = 0, kPagedBf16 = 1, kPagedInt8 = 2;
-constexpr float kSlack = 8.f;  // 2^8: sums and products stay far inside fp32 and bf16 ranges
+constexpr float kSlack = 8.f;  // a weight before the division is at most 2^8
+// ... and a sum of them times V may leave fp32 where the output does not.  A wave
+// whose sums reach 2^100 (or are not finite) takes its rows again with weights of
+// at most 1 / (the request's rows); sums below that stay finite through the joins.
+// (Not at once: so small a weight's exponent has fewer bits for its fraction.)
+constexpr float kLargeSum = 1.2676506002282294e30f;  // 2^100
 
 template <int DH> constexpr int kCombineFloats = kWaves * 16 * (DH + 2);  // LDS before the tables (see forward_lds)
 
@@ -157,10 +163,13 @@ __device__ __forceinline__ bool odd_bf16(uint32_t w) {  // a half of w is not fi
 // 190 for 157); with two tiles of bf16 even that spills, and one wave that
 // fetches ahead is better (16 x 4 rows on bf16 pages 177 us for 268).
 template <int KV, int DH, int MT> constexpr bool kOneWave = DH == 128 && MT > 1 && KV != kPagedInt8;
+// Three of 8-bit rows of 32 features: left to itself the compiler takes one register
+// too many for them (128 requests of 10240 rows, 32 targets 277 us, three 248).
+template <int KV, int DH, int MT> constexpr int kFwdWaves = kOneWave<KV, DH, MT> ? 1 : KV == kPagedInt8 && DH == 32 ? 3 : 2;
 template <int KV, int DH, int MT> constexpr bool kAhead = DH < 128 || kOneWave<KV, DH, MT>;
 
 template <typename T, int KV, int DH, int MT>
-__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kOneWave<KV, DH, MT> ? 1 : 2))) void attn_fwd_kernel(const AttnArgs a) {
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kFwdWaves<KV, DH, MT>))) void attn_fwd_kernel(const AttnArgs a) {
   constexpr bool kF32 = !Elem<T>::bf16;
   constexpr bool kPaged = KV != kRagged;
   constexpr int NT = 2;
@@ -169,7 +178,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kOneWa
   using Blk = Block<T, KV, DH, NT>;
   extern __shared__ __align__(16) unsigned char smem[];
   float* comb = reinterpret_cast<float*>(smem);
-  int2* s_cells = reinterpret_cast<int2*>(comb + kCombineFloats<DH>);
+  int* s_large = reinterpret_cast<int*>(comb + kCombineFloats<DH>);  // a joining wave has seen a large sum
+  int2* s_cells = reinterpret_cast<int2*>(s_large + kWaves);
   int32_t* s_edges = reinterpret_cast<int32_t*>(s_cells + kCells + 1);
   float* s_bias = reinterpret_cast<float*>(s_edges + kMaxBuckets);
   int32_t* s_table = reinterpret_cast<int32_t*>(s_bias + a.hw * a.G * (max(a.b.n, 1) + 1));
@@ -215,6 +225,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kOneWa
   // (pointers that are known to be LDS: set whether used or not)
   const BucketLds bl{s_cells, s_bias, s_edges, max(a.b.n, 1), a.b.multi};
   if (a.placed) fill_buckets(a, g0, a.hw * a.G, s_cells, s_bias, s_edges);
+  if (tid < kWaves) s_large[tid] = 0;
   bool holes = false;
   if constexpr (kPaged) {
     const int p0 = j0 >> a.page_shift, p1 = (j1 + (1 << a.page_shift) - 1) >> a.page_shift;
@@ -229,7 +240,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kOneWa
     __syncthreads();
   }
 
-  for (int zz = z; zz * 16 * MT < rows; zz += a.zgroups) {
+  float above = 0.f;  // of these rows
+  for (int zz = z; zz * 16 * MT < rows;) {
     // ---- this lane's rows: column c16 of each tile
     int tpos[MT], hbias[MT];  // hbias: this row's biases in the table
     int64_t trow[MT];
@@ -523,10 +535,10 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kOneWa
         float top = x[0];
 #pragma unroll
         for (int i = 1; i < NJ; ++i) top = fmaxf(top, x[i]);
-        if (__ballot(top > mx[mt] + kSlack)) {
+        if (__ballot(top > mx[mt] + (kSlack - above))) {
           top = fmaxf(top, __shfl_xor(top, 16));
           top = fmaxf(top, __shfl_xor(top, 32));
-          const float mn = fmaxf(mx[mt], top);
+          const float mn = fmaxf(mx[mt], top + above);
           const float f = mx[mt] == -INFINITY ? 0.f : exp2_fast(mx[mt] - mn);
           mx[mt] = mn;
           sum[mt] *= f;
@@ -675,6 +687,10 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kOneWa
 #pragma unroll
           for (int e = 0; e < NE; ++e) acc[e] += f * p[(f0 + e) * 16 + col];
         }
+        bool large = false;
+#pragma unroll
+        for (int e = 0; e < NE; ++e) large |= !(fabsf(acc[e]) < kLargeSum);
+        if (large) s_large[wave] = 1;
         const int64_t t = t0 + row / a.G;
         const int h = (g0 + hd) * a.G + row % a.G;
         if (split) {
@@ -701,6 +717,15 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kOneWa
         }
       }
       __syncthreads();
+    }
+    const int4 large = *reinterpret_cast<const int4*>(s_large);
+    if (above == 0.f && uniform(large.x | large.y | large.z | large.w) != 0) {
+      above = kSlack + static_cast<float>(32 - __builtin_clz(len));
+      __syncthreads();
+      if (tid < kWaves) s_large[tid] = 0;
+    } else {
+      above = 0.f;
+      zz += a.zgroups;
     }
   }
 }

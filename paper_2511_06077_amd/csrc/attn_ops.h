@@ -79,10 +79,10 @@ hipError_t attn_merge(const AttnArgs& a, bool bf16, bool paged, int dh, hipStrea
 hipError_t attn_backward(const AttnArgs& a, int dtype, int dh, int tiles, hipStream_t st);
 
 // LDS of a workgroup in bytes, of the kMaxLds that a CU has.  Forward: the join's
-// rows, the cells, the edges, the biases of hw kv heads' groups, a chunk's pages.
+// rows and flags, the cells, the edges, the biases of hw kv heads' groups, a chunk's pages.
 constexpr size_t kMaxLds = 160 << 10;
 inline size_t forward_lds(int dh, int hw, int G, int n, int64_t pages) {
-  return 4 * (kWaves * 16 * (dh + 2) + 2 * (kCells + 1) + kMaxBuckets +
+  return 4 * (kWaves * 16 * (dh + 2) + kWaves + 2 * (kCells + 1) + kMaxBuckets +
               static_cast<size_t>(hw) * G * ((n > 1 ? n : 1) + 1) + pages);
 }
 size_t backward_lds(int dtype, int dh, int tiles, int bufs, int hw, int G, int n);

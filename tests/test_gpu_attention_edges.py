@@ -1,5 +1,5 @@
 """The stand-alone attention at the ends of what its calls allow: device offsets
-that are not the host's."""
+that are not the host's, the largest tables and values, what is left of weights."""
 import numpy as np
 import pytest
 
@@ -168,3 +168,42 @@ def test_weights_are_not_low_backward(torch):  # noqa: F811
     bound = HOEFFDING * 2.0 ** -17 + 6e-7 * 0.5 * len(at) + 2.0 ** -8 * abs(want)
     print("[low]", np.abs(dv - want).max() / bound)
     assert (np.abs(dv - want) <= bound).all()
+
+
+# The largest V of the types: equal signs and nearly equal scores, so that every
+# sum before the division is the number of rows times larger.  (Rows are taken a
+# second time, with scores up to 8 + log2(rows) < 24 from their maximum: 24 u of a
+# weight, which the bounds' 2 (rows + ..) u hold many times over.)
+TOP = 3.3e38
+
+
+def large(torch, c, dtype):  # noqa: F811
+    from attn_common import rounded
+    rng = np.random.default_rng(5)
+    v = TOP * rng.uniform(0.5, 1.0, size=c.f["v"].shape)
+    return rounded(torch, v, dtype)
+
+
+@pytest.mark.parametrize("L,m", [([5000, 40, 1, 0], [3, 20, 2, 1]), ([300, 2000], [33, 5]), ([70000], [2])])
+@pytest.mark.parametrize("dtype,dh,H,Hk,masked", [("bf16", 32, 4, 4, True), ("bf16", 64, 2, 1, False),
+                                                  ("bf16", 128, 2, 2, False), ("f32", 32, 4, 4, False), ("f32", 64, 2, 2, True)])
+def test_the_largest_values(torch, dtype, dh, H, Hk, masked, L, m):  # noqa: F811
+    c = Case(torch, L, m, dtype=dtype, dh=dh, H=H, Hk=Hk, masked=masked, nb=8 if masked else 0, q_gain=0.1)
+    c.t["v"], c.f["v"] = large(torch, c, dtype)
+    c.t["dout"], c.f["dout"] = c.t["dout"] * 2.0 ** -90, c.f["dout"] * 2.0 ** -90
+    ref = c.oracle()
+    e = c.compare(dict(out=c.plan().forward(*c.dev("q", "k", "v"), **c.given())), ref)
+    assert max(e.values()) <= 1.0, e
+    e = c.compare(c.step(), ref)
+    assert max(e.values()) <= 1.0, e
+
+
+@pytest.mark.parametrize("fmt", ["int8", "bf16"])
+@pytest.mark.parametrize("page,dh,m,H", [(16, 32, [1, 20, 2, 1], 2), (64, 64, [3, 1, 9, 1], 8), (256, 128, [2, 30, 1, 1], 2)])
+def test_the_largest_values_cached(torch, fmt, page, dh, m, H):  # noqa: F811
+    from test_gpu_cache import Users, serve
+    u = Users(torch, [6000, 300, 1, 0], [0] * 4, page, dh=dh, fmt=fmt, gain=1.0)
+    u.t["v"], u.f["v"] = large(torch, u, "bf16")
+    u.write()
+    plan, _, e = serve(u, torch, m, H, nb=8, masked=True, q_gain=0.1)
+    assert plan.device_status() == 0 and e <= 1.0
