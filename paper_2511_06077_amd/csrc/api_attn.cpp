@@ -99,7 +99,7 @@ void fill_edges(const stca_attn_t* a, Buckets* b) {
 }
 
 struct Plan {
-  int chunk, max_chunks, units, tiles, zgroups, btiles, passes, hw;
+  int chunk, max_chunks, units, tiles, zgroups, btiles, passes, hw, part_tgt, max_tgt;
   size_t hdr, part_o, part_ml, part_dq, part_db, acc_kv, rows, total;
 };
 
@@ -141,6 +141,20 @@ int heads_of(int Hk, int64_t n_hist, bool backward, int tiles, Lds lds) {
   return hw;
 }
 
+// Rows of partials of chunks of that many rows (a row is a target's heads), and
+// which of the two layouts (see part_row) has fewer.
+int64_t part_rows_of(const stca_batch_t* b, int64_t max_m, int64_t max_l, int64_t chunk, int* part_tgt) {
+  const int64_t chunks = ceil_div(max_l, chunk), flat = chunks * b->n_tgt, units = (b->n_hist / chunk + b->n_requests) * max_m;
+  *part_tgt = chunks > 1 && units < flat ? static_cast<int>(max_m) : 0;
+  return chunks > 1 ? std::min(flat, units) : 0;
+}
+
+// Partials that are always taken, and how many times what the batch's chunks and
+// targets add up to, request by request: beyond both chunks become longer (one
+// history of 32768 rows and 512 targets among 2047 of 256 rows and 16).
+constexpr int64_t kFreePartials = 64 << 20;
+constexpr int kSparePartials = 2;
+
 bool ragged_plan(const stca_attn_t* a, const stca_batch_t* b, bool backward, Plan* p) {
   const int H = a->n_heads, Hk = a->n_kv_heads, G = H / Hk, dh = a->d_head;
   int64_t max_m = b->n_tgt, max_l = b->n_hist;
@@ -174,19 +188,33 @@ bool ragged_plan(const stca_attn_t* a, const stca_batch_t* b, bool backward, Pla
   if (!b->hist_off_host)
     p->chunk = static_cast<int>(std::max<int64_t>(p->chunk, round_up(ceil_div(b->n_hist, kNoHostChunks), 64)));
   p->chunk = static_cast<int>(std::min<int64_t>(p->chunk, std::max<int64_t>(64, round_up(max_l, 64))));
+  int64_t parts_rows = part_rows_of(b, max_m, max_l, p->chunk, &p->part_tgt);
+  if (b->hist_off_host && parts_rows * H * dh * 4 > kFreePartials) {
+    int64_t own = 0;
+    for (int r = 0; r < b->n_requests; ++r)
+      own += ceil_div(b->hist_off_host[r + 1] - b->hist_off_host[r], p->chunk) *
+             static_cast<int64_t>(b->tgt_off_host[r + 1] - b->tgt_off_host[r]);
+    const int64_t most = std::max(kSparePartials * own, kFreePartials / (static_cast<int64_t>(H) * dh * 4));
+    while (parts_rows > most) {
+      p->chunk *= 2;
+      parts_rows = part_rows_of(b, max_m, max_l, p->chunk, &p->part_tgt);
+    }
+  }
   p->max_chunks = static_cast<int>(std::max<int64_t>(1, ceil_div(max_l, p->chunk)));
+  // (the layout by units has room for that many)
+  p->max_tgt = p->part_tgt ? p->part_tgt : backward && p->passes == 1 ? 16 * p->btiles : INT32_MAX;
   const int64_t units = b->n_hist / p->chunk + b->n_requests;
   if (units * Hk * p->zgroups > 0x7f000000) return false;
   p->units = static_cast<int>(units);
   Bump m;
   p->hdr = m.take(sizeof(WsHeader));
-  const size_t rows = static_cast<size_t>(b->n_tgt) * H, split = p->max_chunks > 1 ? p->max_chunks : 0;
+  const size_t rows = static_cast<size_t>(b->n_tgt) * H, split = static_cast<size_t>(parts_rows) * H;
   if (!backward) {
-    p->part_o = m.take(4 * split * rows * dh);
-    p->part_ml = m.take(8 * split * rows);
+    p->part_o = m.take(4 * split * dh);
+    p->part_ml = m.take(8 * split);
   } else {
     p->rows = m.take(16 * rows);
-    p->part_dq = m.take(4 * split * rows * dh);
+    p->part_dq = m.take(4 * split * dh);
     p->part_db = m.take(4 * static_cast<size_t>(p->units) * H * a->n_buckets);
     p->acc_kv = m.take(p->passes > 1 && p->chunk > 16 * parts ? 8 * static_cast<size_t>(b->n_hist) * Hk * dh : 0);
   }
@@ -377,7 +405,8 @@ stca_status_t stca_attn_forward(const stca_attn_t* attn, const stca_batch_t* bat
   a.units = p.units;
   a.hw = p.hw;
   a.zgroups = p.zgroups;
-  a.max_tgt = INT32_MAX;
+  a.max_tgt = p.max_tgt;
+  a.part_tgt = p.part_tgt;
   a.out = out;
   if (saved) {
     stca_attn_saved_layout_t l;
@@ -430,7 +459,8 @@ stca_status_t stca_attn_backward(const stca_attn_t* attn, const stca_batch_t* ba
   a.bufs = p.passes > 1 ? 2 : 1;
   a.hw = p.hw;
   a.zgroups = 1;
-  a.max_tgt = p.passes > 1 ? INT32_MAX : 16 * p.btiles;
+  a.max_tgt = p.max_tgt;
+  a.part_tgt = p.part_tgt;
   a.part_dq = at<float>(ws, p.part_dq);
   a.part_db = at<float>(ws, p.part_db);
   a.acc_kv = at<float>(ws, p.acc_kv);

@@ -266,7 +266,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kBwdWa
     return;
   }
   const int j0 = c * a.chunk, j1 = j0 + min(len - j0, a.chunk);
-  const int t0 = uniform(clamp_off(a.tgt_off[r], a.n_tgt)), m = max(0, uniform(clamp_off(a.tgt_off[r + 1], a.n_tgt)) - t0);
+  const int t0 = uniform(clamp_off(a.tgt_off[r], a.n_tgt)), m = min(max(0, uniform(clamp_off(a.tgt_off[r + 1], a.n_tgt)) - t0), a.max_tgt);
   const int ttiles = (m + 15) / 16, groups = (ttiles + MT - 1) / MT;  // groups of MT tiles of one head
 
   const BucketLds bl{s_cells, s_bias, s_edges, slots, a.b.multi};  // (pointers that are known to be LDS)
@@ -708,7 +708,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kBwdWa
           v[e] *= a.scale;
         }
         if (a.max_chunks > 1) {
-          float* p = a.part_dq + ((c * a.n_tgt + row0) * a.H + head0) * DH + (row * a.H + hd * a.G) * DH + f;
+          float* p = a.part_dq + (part_row(a, c, unit, t0, row0) * a.H + head0) * DH + (row * a.H + hd * a.G) * DH + f;
 #pragma unroll
           for (int e = 0; e < NE; e += 2) *reinterpret_cast<f32x2*>(p + e) = f32x2{v[e], v[e + 1]};
         } else {
@@ -787,11 +787,13 @@ __global__ __launch_bounds__(256) void attn_bwd_sum_kernel(const AttnArgs a, int
     }
     const int len = clamp_off(a.hist_off[lo + 1], a.n_hist) - clamp_off(a.hist_off[lo], a.n_hist);
     const int n = max(1, min(a.max_chunks, (len + a.chunk - 1) / a.chunk));
+    int64_t first, step;
+    if (!part_rows(a, lo, t, static_cast<int>(row % a.H), first, step)) return;
     float acc[NE] = {};
 #pragma unroll 4
     for (int c = 0; c < n; ++c)
 #pragma unroll
-      for (int e = 0; e < NE; ++e) acc[e] += a.part_dq[(c * a.n_tgt * a.H + row) * DH + f0 + e];
+      for (int e = 0; e < NE; ++e) acc[e] += a.part_dq[(c * step + first) * DH + f0 + e];
     T* p = static_cast<T*>(a.dq) + t * a.lddq + (row % a.H) * DH + f0;
 #pragma unroll
     for (int e = 0; e < NE; ++e) p[e] = from_f32<T>(acc[e]);

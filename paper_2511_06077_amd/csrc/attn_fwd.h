@@ -214,8 +214,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kFwdWa
   }
   if (c < 0 || c >= a.max_chunks || (c > 0 && static_cast<int64_t>(c) * a.chunk >= len)) return;
   const int j0 = c * a.chunk;
-  const int t0 = uniform(clamp_off(a.tgt_off[r], a.n_tgt)), m = uniform(clamp_off(a.tgt_off[r + 1], a.n_tgt)) - t0;
-  const int rows = m * a.G;
+  const int t0 = uniform(clamp_off(a.tgt_off[r], a.n_tgt));
+  const int m = min(uniform(clamp_off(a.tgt_off[r + 1], a.n_tgt)) - t0, a.max_tgt), rows = m * a.G;
   if (z * 16 * MT >= rows) return;
   // (one chunk on the host's offsets: there are no partials, whatever the device's say)
   const bool split = a.max_chunks > 1 && len > a.chunk;
@@ -694,7 +694,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kFwdWa
         const int64_t t = t0 + row / a.G;
         const int h = (g0 + hd) * a.G + row % a.G;
         if (split) {
-          const int64_t at = (static_cast<int64_t>(c) * a.n_tgt + t) * a.H + h;
+          const int64_t at = part_row(a, c, unit, t0, t) * a.H + h;
 #pragma unroll
           for (int e = 0; e < NE; ++e) a.part_o[at * DH + f0 + e] = acc[e];
           if (f0 == 0) {

@@ -23,9 +23,10 @@ __global__ __launch_bounds__(256) void attn_merge_kernel(const AttnArgs a, bool 
   __shared__ float part[kSplit > 1 ? 16 : 1][kSplit > 1 ? DH + 2 : 1];
   const int f0 = (threadIdx.x & 15) * NE, s = (threadIdx.x >> 4) % kSplit, slot = threadIdx.x >> 4;
   const int64_t row = static_cast<int64_t>(blockIdx.x) * kRows + slot / kSplit;
-  const int64_t step = a.n_tgt * a.H, t = row / a.H;
+  const int64_t t = row / a.H;
+  int64_t first = 0, step = 0;
   int n = 0;
-  if (row < step) {
+  if (row < a.n_tgt * a.H) {
     int lo = 0, hi = a.R;  // the request of target t
     while (hi - lo > 1) {
       const int mid = (lo + hi) / 2;
@@ -35,12 +36,13 @@ __global__ __launch_bounds__(256) void attn_merge_kernel(const AttnArgs a, bool 
     int len;
     if (paged) len = min(max(a.lens[lo], 0), a.max_len);
     else len = clamp_off(a.hist_off[lo + 1], a.n_hist) - clamp_off(a.hist_off[lo], a.n_hist);
-    if (len > a.chunk) n = min(a.max_chunks, (len + a.chunk - 1) / a.chunk);  // (else written by the attention itself)
+    if (len > a.chunk && part_rows(a, lo, t, static_cast<int>(row % a.H), first, step))
+      n = min(a.max_chunks, (len + a.chunk - 1) / a.chunk);  // (else written by the attention itself)
   }
   float M = -INFINITY, L = 0.f, acc[NE] = {};
 #pragma unroll 4
   for (int c = s; c < n; c += kSplit) {
-    const int64_t at = c * step + row;
+    const int64_t at = c * step + first;
     const float m = a.part_ml[2 * at], l = a.part_ml[2 * at + 1], mn = fmaxf(M, m);
     const float f = m == -INFINITY ? (l != l ? l : 0.f) : exp2_fast(m - mn), keep = M == -INFINITY ? (L != L ? L : 0.f) : exp2_fast(M - mn);
     L = keep * L + f * l;

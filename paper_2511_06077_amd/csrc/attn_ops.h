@@ -55,12 +55,13 @@ struct AttnArgs {
   int64_t n_hist, n_tgt;
   int32_t chunk, max_chunks, units, zgroups;
   int32_t max_tgt;                 // most targets of a request that the launch takes
+  int32_t part_tgt;                // partials: see part_row
   int32_t bufs;                    // backward: a workgroup's rows in LDS, 2 where there are several passes
   int32_t hw;                      // kv heads of a workgroup (1, 2 or 4): a wave has one, 4 / hw waves share it
   // forward
   void* out;
   float *sa, *sm, *sl;             // saved (nullable): normalised output, score maximum, sum
-  float *part_o, *part_ml;         // [max_chunks][n_tgt][H][dh], [max_chunks][n_tgt][H][2]
+  float *part_o, *part_ml;         // [part rows][H][dh], [part rows][H][2]
   // backward
   const void* dout;
   const float *fa, *fm, *fl;       // what the forward saved
@@ -284,6 +285,27 @@ __device__ __forceinline__ V load_at(gptr base, uint32_t at) {
 
 __device__ __forceinline__ int clamp_off(int32_t v, int64_t n) {
   return static_cast<int>(min<int64_t>(max(v, 0), n));
+}
+
+// Partials of target t (of its request's from t0 on) and chunk c, which is unit u:
+// a row a chunk and target of the batch, or, where that would be more (a few long
+// histories among short ones), a row a unit and target of a request, part_tgt each.
+template <typename Args>
+__device__ __forceinline__ int64_t part_row(const Args& a, int c, int64_t u, int64_t t0, int64_t t) {
+  return a.part_tgt ? u * a.part_tgt + (t - t0) : c * a.n_tgt + t;
+}
+// ... of the first chunk, for a row (target, head) of request r, and how far apart
+// its chunks' lie; false where offsets that are not the host's leave it none.
+__device__ __forceinline__ bool part_rows(const AttnArgs& a, int r, int64_t t, int h, int64_t& at, int64_t& step) {
+  int64_t u = 0, t0 = 0;
+  if (a.part_tgt) {
+    u = clamp_off(a.hist_off[r], a.n_hist) / a.chunk + r;
+    t0 = clamp_off(a.tgt_off[r], a.n_tgt);
+    if (t < t0 || t - t0 >= a.part_tgt) return false;
+  }
+  at = part_row(a, 0, u, t0, t) * a.H + h;
+  step = (a.part_tgt ? a.part_tgt : a.n_tgt) * a.H;
+  return true;
 }
 
 __device__ __forceinline__ void set_status(WsHeader* hdr, int bad) {

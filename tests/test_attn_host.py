@@ -237,3 +237,19 @@ def test_every_accepted_table_has_its_lds(d_head, dtype):
                     c = cache(n_kv_heads=Hk, d_head=d_head, page_size=16)
                     assert stca.stca_cache_attn_workspace_size(
                         a, c, stca.cache_batch(1, 3, 0x10000, 0x20000, 1000000, 0x30000, 1 << 20))
+
+
+@pytest.mark.parametrize("L,m,fwd,bwd", [
+    ([256] * 255 + [10240], [16] * 256, 16, 64),
+    ([256] * 2047 + [32768], [16] * 2048, 128, 512),
+    ([1] * 1000 + [100000], [1] * 1001, 16, 128),
+    # both ends at once: longer chunks, dk and dv of the passes wait in fp32 (543 MiB)
+    ([256] * 2047 + [32768], [16] * 2047 + [512], 256, 2048), ([256] * 2047 + [32768], [512] + [16] * 2047, 256, 2048)])
+def test_one_long_history_among_short_ones(L, m, fwd, bwd):
+    """Workspaces (MiB) of the order of the batch's own rows, not of the longest
+    history times all targets (4 and 33 GB for the second batch)."""
+    def off(n):
+        return np.concatenate([[0], np.cumsum(n)])
+    a, b = attn(n_heads=8, n_kv_heads=2, d_head=64), batch(off(L), off(m))
+    assert 0 < stca.stca_attn_workspace_size(a, b, False) <= fwd << 20
+    assert 0 < stca.stca_attn_workspace_size(a, b, True) <= bwd << 20

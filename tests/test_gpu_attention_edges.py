@@ -21,6 +21,7 @@ pytestmark = pytest.mark.gpu
     ([40000, 40000], [2, 2], [79990, 10], [2, 2], False, False),
     ([50, 50], [3, 6], [60, 40], [6, 3], True, True),
     ([50, 50], [16, 16], [50, 50], [32, 0], True, None),  # (shared heads go in several passes, any number of them)
+    ([5000] + [40] * 30, [2] * 31, [5000] + [40] * 30, [2] * 29 + [4, 0], False, False),  # (partials by unit)
 ])
 def test_stale_host_offsets(torch, dtype, dh, H, Hk, L, m, dev_L, dev_m, forward, backward):  # noqa: F811
     """Nothing is written outside the buffers, and a request that was not taken
@@ -207,3 +208,23 @@ def test_the_largest_values_cached(torch, fmt, page, dh, m, H):  # noqa: F811
     u.write()
     plan, _, e = serve(u, torch, m, H, nb=8, masked=True, q_gain=0.1)
     assert plan.device_status() == 0 and e <= 1.0
+
+
+# Partials by the chunk and target of each request, where one history is much
+# longer than the others; and longer chunks where one request has most of the
+# targets as well (the 64 MB that are always taken are passed by 8 heads of 128).
+@pytest.mark.parametrize("dtype,dh,H,Hk,L,m", [
+    ("bf16", 32, 2, 2, [40] * 30 + [5000, 0] + [40] * 20, [2] * 52),
+    ("bf16", 64, 4, 1, [40] * 30 + [5000, 0] + [40] * 20, [i % 4 for i in range(52)]),
+    ("f32", 32, 2, 2, [3000] + [7] * 60, [3] * 61),
+    ("bf16", 128, 8, 4, [20] * 500 + [5000], [3, 60] + [3] * 499),
+    ("f32", 128, 8, 4, [5000] + [20] * 500, [3, 60] + [3] * 499),
+])
+def test_one_long_history_among_short_ones(torch, dtype, dh, H, Hk, L, m):  # noqa: F811
+    c = Case(torch, L, m, dtype=dtype, dh=dh, H=H, Hk=Hk, nb=8, masked=True)
+    ref = c.oracle()
+    plan = c.plan()
+    e = c.compare(dict(out=plan.forward(*c.dev("q", "k", "v"), **c.given())), ref)
+    assert plan.device_status() == 0 and max(e.values()) <= 1.0, e
+    e = c.compare(c.step(), ref)
+    assert max(e.values()) <= 1.0, e
