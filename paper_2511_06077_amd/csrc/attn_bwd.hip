@@ -400,19 +400,26 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kBwdWa
     }
     if (held <= 0) jend = 0;
 
-    // v to bucket k and u to bucket l of this lane's sums (l = -1: nothing)
+    // v to bucket k and u to bucket l of this lane's sums (l = -1: nothing); lanes
+    // that share a sum take turns, each of which ends before the next one reads
     auto add_bins = [&](int k, float v, int l, float u) {
       if (l == k) {
         v += u;
         l = -1;
       }
       for (int turn = 0; turn < 64 / copies; ++turn) {
-        if (copies < 64 && lane / copies != turn) continue;
-        float* p = bins + k * copies + lane % copies;
-        float* q = bins + max(l, 0) * copies + lane % copies;
-        const float x = *p, y = *q;
-        *p = x + v;
-        if (l >= 0) *q = y + u;
+        if (lane / copies == turn) {
+          float* p = bins + k * copies + lane % copies;
+          float* q = bins + max(l, 0) * copies + lane % copies;
+          const float x = *p, y = *q;
+          *p = x + v;
+          if (l >= 0) *q = y + u;
+        }
+        if (copies < 64) {
+          __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+          __builtin_amdgcn_wave_barrier();
+          __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        }
       }
     };
 

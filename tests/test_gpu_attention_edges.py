@@ -228,3 +228,20 @@ def test_one_long_history_among_short_ones(torch, dtype, dh, H, Hk, L, m):  # no
     assert plan.device_status() == 0 and max(e.values()) <= 1.0, e
     e = c.compare(c.step(), ref)
     assert max(e.values()) <= 1.0, e
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("nb", [34, 35, 70, 71, 128])
+def test_lanes_that_share_a_bucket_sum(torch, nb, dtype):  # noqa: F811
+    """Up to 34 buckets every lane has sums of its own, up to 70 two lanes share
+    one, above four; every row of a step in a bucket of its own or all in one, so
+    that the sharing lanes meet; the same bits each time."""
+    c = Case(torch, [400, 90], [40, 7], H=4, Hk=2, dtype=dtype, nb=nb, masked=True, time=True, seed=nb)
+    c.edges = np.arange(1, nb, dtype=np.int32)
+    c.hist_pos[200:400] = 50
+    ref = c.oracle()
+    got = [c.step() for _ in range(3)]
+    e = c.compare(got[0], ref)
+    assert max(e.values()) <= 1.0, e
+    for g in got[1:]:
+        assert torch.equal(g["dbias"], got[0]["dbias"])
