@@ -15,32 +15,26 @@ checks and pointer marshalling; all computation happens in libstca.so.
 
 A plan's workspace (and what its forward saved) belongs to one stream at a
 time: calls, or replays of captured graphs, that may overlap need a plan each.
-A forward replaces what the plan's backward reads.
+A forward replaces what the plan's backward reads.  stream= (a handle) is the
+stream of a call in place of the current one, as if it were made under
+torch.cuda.stream: the inputs have to be ready on it, and results belong to it
+(another stream waits for it, and records its use with Tensor.record_stream).
 """
 from __future__ import annotations
 
-import contextlib
 import math
 from typing import Optional
 
 import numpy as np
 
 from . import stca
+from .device import launch_on
 from .stca import bias_edges  # noqa: F401  (public here too)
 
 
 def _torch():
     import torch
     return torch
-
-
-def _on(device):
-    """Makes `device` current for a launch; nothing to do where it is."""
-    cuda = _torch().cuda
-    return _HERE if cuda.current_device() == device.index else cuda.device(device)
-
-
-_HERE = contextlib.nullcontext()
 
 
 def _dtype_code(dtype):
@@ -127,8 +121,8 @@ class _Scores:
     def stream(self):
         return _torch().cuda.current_stream(self.device.index).cuda_stream
 
-    def device_status(self) -> int:
-        return stca.stca_device_status(self.ws, self.stream())
+    def device_status(self, stream: Optional[int] = None) -> int:
+        return stca.stca_device_status(self.ws, self.stream() if stream is None else stream)
 
 
 class CrossAttention(_Scores):
@@ -172,7 +166,7 @@ class CrossAttention(_Scores):
         """out [n_tgt][n_heads][d_head]"""
         torch = _torch()
         given = self._in(q, k, v, tgt_pos, hist_pos, bias)
-        with _on(self.device):
+        with launch_on(self.device, stream):
             out = torch.empty((self.n_tgt, self.n_heads, self.d_head), dtype=self.dtype, device=self.device)
             stca.stca_attn_forward(self.attn, self.batch, given, out, self.saved, self.ws, self.ws_bytes,
                                    self.stream() if stream is None else stream)
@@ -189,7 +183,7 @@ class CrossAttention(_Scores):
             raise ValueError("backward: no forward before it")
         given = self._in(q, k, v, tgt_pos, hist_pos, bias)
         _flat("dout", dout, self.dtype, (self.n_tgt, self.n_heads, self.d_head), self.device)
-        with _on(self.device):
+        with launch_on(self.device, stream):
             t = dict(dtype=self.dtype, device=self.device)
             dq = torch.empty((self.n_tgt, self.n_heads, self.d_head), **t)
             dk = torch.empty((self.n_hist, self.n_kv_heads, self.d_head), **t)
@@ -246,9 +240,9 @@ class HistoryCache:
     def stream(self):
         return _torch().cuda.current_stream(self.device.index).cuda_stream
 
-    def device_status(self) -> int:
+    def device_status(self, stream: Optional[int] = None) -> int:
         """Of the last write or read."""
-        return stca.stca_device_status(self.ws, self.stream())
+        return stca.stca_device_status(self.ws, self.stream() if stream is None else stream)
 
     def write(self, k, v, row_off, start, table, pos=None, stream: Optional[int] = None):
         """Packed rows k, v [n][n_kv_heads][d_head]: request r's rows
@@ -262,7 +256,7 @@ class HistoryCache:
         if pos is not None:
             _flat("pos", pos, torch.int32, (n,), self.device)
         rows = self._rows(row_off, start, table, n)
-        with _on(self.device):
+        with launch_on(self.device, stream):
             stca.stca_cache_write(self.cache, rows, _dtype_code(k.dtype), k, v, ldk, ldv, pos, self.ws,
                                   self.stream() if stream is None else stream)
 
@@ -271,7 +265,7 @@ class HistoryCache:
         torch = _torch()
         dtype = dtype or torch.bfloat16
         rows = self._rows(row_off, start, table, n_rows)
-        with _on(self.device):
+        with launch_on(self.device, stream):
             k, v = (torch.empty((n_rows, self.n_kv_heads, self.d_head), dtype=dtype, device=self.device)
                     for _ in range(2))
             pos = None if self.pos is None else torch.empty(n_rows, dtype=torch.int32, device=self.device)
@@ -307,7 +301,7 @@ class CacheAttention(_Scores):
             raise ValueError(f"table: [{self.n_requests}][pages of {self.max_len} rows] is needed")
         _flat("table", table, torch.int32, table.shape, self.device)
         self._given(tgt_pos, bias, self.n_tgt)
-        with _on(self.device):
+        with launch_on(self.device, stream):
             out = torch.empty((self.n_tgt, self.n_heads, self.d_head), dtype=self.dtype, device=self.device)
             b = self.batch
             b.lens, b.table, b.table_ld = lens.data_ptr(), table.data_ptr(), table.shape[1]

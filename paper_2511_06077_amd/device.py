@@ -4,6 +4,7 @@ pointer marshalling); all computation happens in libstca.so.
 """
 from __future__ import annotations
 
+import contextlib
 from typing import Optional
 
 import numpy as np
@@ -15,6 +16,20 @@ from .workload import WEIGHT_NAMES, Batch
 def _torch():
     import torch
     return torch
+
+
+_HERE = contextlib.nullcontext()
+
+
+def launch_on(device, stream: Optional[int] = None):
+    """Where a call allocates and launches: `device` current and, given a stream's
+    handle, that stream, so that memory taken for the call belongs to the stream
+    that writes it (a block freed on the current stream may still be in use there)."""
+    cuda = _torch().cuda
+    if stream is None or stream == cuda.current_stream(device).cuda_stream:
+        return _HERE if device.index in (None, cuda.current_device()) else cuda.device(device)
+    at = cuda.current_device() if device.index is None else device.index
+    return cuda.stream(cuda.ExternalStream(stream, device=at) if stream else cuda.default_stream(at))
 
 
 def to_device(a: np.ndarray, device):
@@ -122,22 +137,23 @@ class DeviceBatch:
         wl = self.b.wl
         d, F, n = wl.d_model, wl.ffn_hidden, wl.n_layers
         f32 = dict(dtype=torch.float32, device=self.device)
-        g = {
-            "dhist": torch.empty((self.b.n_hist, d), **f32),
-            "dtgt": torch.empty((self.b.n_tgt_total, d), **f32),
-            "dwq": torch.empty((n, d, d), **f32), "dwk": torch.empty((n, d, d), **f32),
-            "dwv": torch.empty((n, d, d), **f32), "dwo": torch.empty((n, d, d), **f32),
-            "dw1": torch.empty((n, d, F), **f32), "dw2": torch.empty((n, F, d), **f32),
-        }
-        dw = stca.wgrads(g["dwq"], g["dwk"], g["dwv"], g["dwo"], g["dw1"], g["dw2"])
-        if use_record:
-            stca.stca_backward_record(self.dims, self.batch, self.hist, self.tgt, self.weights, self.record, dout,
-                                      g["dhist"], g["dtgt"], dw, self.bws, self.bws_bytes,
-                                      self.stream() if stream is None else stream)
-        else:
-            stca.stca_backward(self.dims, self.batch, self.hist, self.tgt, self.weights, dout,
-                               g["dhist"], g["dtgt"], dw, self.bws, self.bws_bytes,
-                               self.stream() if stream is None else stream)
+        with launch_on(self.device, stream):
+            g = {
+                "dhist": torch.empty((self.b.n_hist, d), **f32),
+                "dtgt": torch.empty((self.b.n_tgt_total, d), **f32),
+                "dwq": torch.empty((n, d, d), **f32), "dwk": torch.empty((n, d, d), **f32),
+                "dwv": torch.empty((n, d, d), **f32), "dwo": torch.empty((n, d, d), **f32),
+                "dw1": torch.empty((n, d, F), **f32), "dw2": torch.empty((n, F, d), **f32),
+            }
+            dw = stca.wgrads(g["dwq"], g["dwk"], g["dwv"], g["dwo"], g["dw1"], g["dw2"])
+            if use_record:
+                stca.stca_backward_record(self.dims, self.batch, self.hist, self.tgt, self.weights, self.record, dout,
+                                          g["dhist"], g["dtgt"], dw, self.bws, self.bws_bytes,
+                                          self.stream() if stream is None else stream)
+            else:
+                stca.stca_backward(self.dims, self.batch, self.hist, self.tgt, self.weights, dout,
+                                   g["dhist"], g["dtgt"], dw, self.bws, self.bws_bytes,
+                                   self.stream() if stream is None else stream)
         return g
 
 

@@ -245,3 +245,67 @@ def test_lanes_that_share_a_bucket_sum(torch, nb, dtype):  # noqa: F811
     assert max(e.values()) <= 1.0, e
     for g in got[1:]:
         assert torch.equal(g["dbias"], got[0]["dbias"])
+
+
+def test_results_of_a_given_stream(torch):  # noqa: F811
+    """A call with stream= takes no memory that the current stream has freed but
+    still uses; its results are those of the current stream."""
+    from paper_2511_06077_amd.attention import CacheAttention
+    from test_gpu_cache import Users
+    c = Case(torch, [900, 33, 0, 400], [50, 40, 2, 16], nb=16, masked=True, H=4, Hk=2)
+    want = c.step()
+    plan, given = c.plan(backward=True), c.given()
+    q, k, v, dout = c.dev("q", "k", "v", "dout")
+    u = Users(torch, [300, 20, 65], [0, 0, 0], 64, gain=1.0)
+    u.write()
+    cq, lens, table = torch.randn((9, 4, 32), device="cuda").bfloat16(), u.dev(u.n.astype(np.int32)), u.dev(u.table)
+    serve = CacheAttention(u.cache, offsets([7, 1, 1]), 4, 300)
+    where = u.where()
+    cached = (serve.forward(cq, lens, table), *u.cache.read(*where, n_rows=385))
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    calls = (
+        (lambda s: [plan.forward(q, k, v, **given, stream=s)], [want["out"]]),
+        (lambda s: plan.backward(dout, q, k, v, **given, stream=s), [want[n] for n in ("dq", "dk", "dv", "dbias")]),
+        (lambda s: [serve.forward(cq, lens, table, stream=s)], [cached[0]]),
+        (lambda s: u.cache.read(*where, n_rows=385, stream=s), cached[1:]))
+    for call, expect in calls:
+        held = [torch.full_like(x, 7.0) for x in expect]
+        seen = [torch.empty_like(x) for x in expect]
+        torch.cuda.synchronize()
+        torch.cuda._sleep(50_000_000)  # the current stream is behind
+        for a, b in zip(seen, held):
+            a.copy_(b)
+        del b
+        held.clear()  # freed, and still to be read
+        got = call(side.cuda_stream)
+        side.synchronize()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(got, expect))
+        assert all((x == 7.0).all() for x in seen)
+    assert plan.device_status(side.cuda_stream) == 0 and u.cache.device_status(side.cuda_stream) == 0
+
+
+def test_gradients_of_a_given_stream(torch):  # noqa: F811
+    """The layer stack's gradients likewise."""
+    from paper_2511_06077_amd import workload as W
+    from paper_2511_06077_amd.device import DeviceBatch, to_device
+    b = W.make_custom_batch("stream", [300, 45, 1], [5, 33, 2], d_model=128, n_heads=4, n_layers=1, dtype="bf16", seed=7,
+                            with_grad=True)
+    db = DeviceBatch(b, backward=True)
+    dout = to_device(b.grad_out, "cuda")
+    want = db.backward(dout)
+    side = torch.cuda.Stream()
+    held = [torch.full_like(x, 7.0) for x in want.values()]
+    seen = [torch.empty_like(x) for x in held]
+    torch.cuda.synchronize()
+    torch.cuda._sleep(50_000_000)
+    for x, y in zip(seen, held):
+        x.copy_(y)
+    del y
+    held.clear()
+    got = db.backward(dout, stream=side.cuda_stream)
+    side.synchronize()
+    torch.cuda.synchronize()
+    assert all(torch.equal(got[n], want[n]) for n in want)
+    assert all((x == 7.0).all() for x in seen)
