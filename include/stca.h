@@ -436,8 +436,8 @@ typedef struct {
   int32_t n_kv_heads;        /* heads of K and V, each shared by n_heads / n_kv_heads query heads */
   int32_t d_head;            /* 32, 64 or 128; n_heads d_head at most 65536 */
   int32_t dtype;             /* stca_dtype_t of q, k, v, out, dout, dq, dk, dv */
-  float scale;               /* finite */
-  float softcap;             /* >= 0, 0 = none */
+  float scale;               /* finite, times log2 e as well */
+  float softcap;             /* >= 0, 0 = none; likewise, and scale / softcap 0 or in fp32's normal range */
   int32_t masked;            /* nonzero: rows with hist_pos > tgt_pos are hidden */
   int32_t n_buckets;         /* 0 = no bias; at most 128 */
   const int32_t* edges_host; /* host [n_buckets - 1], strictly ascending in 1..2^31-2; read by the call */

@@ -27,6 +27,9 @@ stca_status_t check_attn(const stca_attn_t* a) {
       (a->dtype != STCA_F32 && a->dtype != STCA_BF16) || !std::isfinite(a->scale) || !std::isfinite(a->softcap) ||
       a->softcap < 0.f || a->n_buckets < 0 || a->n_buckets > kMaxBuckets)
     return STCA_ERR_INVALID_ARG;
+  // (the factors that the kernels multiply scores by, see attn_fwd.h)
+  const float most = std::fmax(std::fabs(a->scale), a->softcap) * kLog2e, in = std::fabs(a->scale) / a->softcap;
+  if (!std::isfinite(most) || (a->softcap > 0.f && a->scale != 0.f && !std::isnormal(in))) return STCA_ERR_INVALID_ARG;
   if (a->n_buckets > 1) {
     if (!a->edges_host || a->edges_host[0] < 1) return STCA_ERR_INVALID_ARG;
     for (int i = 1; i < a->n_buckets - 1; ++i)

@@ -51,6 +51,18 @@ def test_scores_are_checked(kw, status):
     assert stca.stca_attn_saved_size(a, batch()) == 0
 
 
+@pytest.mark.parametrize("kw", [
+    dict(softcap=3e38), dict(scale=-3e38), dict(scale=1e-3, softcap=1e37), dict(scale=1e20, softcap=1e-20),
+    dict(scale=1e-38, softcap=100.0)])
+def test_factors_of_a_score_have_to_fit_fp32(kw):
+    """Finite, but softcap log2 e is infinite, or scale / softcap is not a normal
+    number: scores would be NaN, or lose their bits."""
+    assert forward(attn(**kw)) == BAD and stca.stca_attn_workspace_size(attn(**kw), batch()) == 0
+    for ok in (dict(softcap=1e30), dict(scale=0.0, softcap=5.0), dict(scale=-1e30), dict(scale=1e-30, softcap=1.0),
+               dict(scale=2e38), dict(scale=0.1, softcap=1e-30)):
+        assert stca.stca_attn_workspace_size(attn(**ok), batch()) > 0, ok
+
+
 @pytest.mark.parametrize("h,t", [([0, 5, 3], [0, 1, 2]), ([1, 5, 6], [0, 1, 2]), ([0, 5, 6], [0, 3, 2])])
 def test_host_offsets_are_checked(h, t):
     assert forward(b=batch(h, t)) == BAD

@@ -309,3 +309,17 @@ def test_gradients_of_a_given_stream(torch):  # noqa: F811
     torch.cuda.synchronize()
     assert all(torch.equal(got[n], want[n]) for n in want)
     assert all((x == 7.0).all() for x in seen)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("cap", [1e4, 1e30])
+def test_a_cap_far_above_the_scores(torch, cap, dtype):  # noqa: F811
+    """tanh is relative to small values there: the results of no cap (at 1e4 what
+    it takes off, x^3 / (3 cap^2), is below 2^-24 of a score)."""
+    c = Case(torch, [200, 33], [9, 20], dtype=dtype, nb=8, masked=True)
+    ref = c.oracle()
+    c.cap = cap
+    got = c.step()
+    c.cap = 0.0
+    e = c.compare(got, ref)
+    assert max(e.values()) <= 1.0, e
