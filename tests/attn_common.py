@@ -41,3 +41,41 @@ def worst(got, want, mag, dtype, c):
         e = np.abs(got - want) / bound
     e = e[~odd]
     return float(e.max()) if e.size else 0.0
+
+
+# ---- long histories in which every block of 32 rows counts
+
+def deep(dtype, dh, L, ref, cap=0.0):
+    """rel with the depth that sums over a long history have: a wave takes at most
+    512 rows of a chunk (fewer than 2^20 rows times kv heads in all), and at most
+    one chunk in 64 rows is joined one after the other (a bucket's in fp64)."""
+    return rel(dtype, dh, 512 + -(-int(max(L)) // 64), ref, cap)
+
+
+def spread(rng, L, m, H, Hk, dh, buckets=128):
+    """Inputs as float64 arrays, options and offsets: block b of a request's rows has
+    its K and V mostly in feature b % dh, so that each feature of out and dq is a sum
+    over few blocks; buckets of equal width, so that each is one over few as well (the
+    short requests', whose weights are larger, in a bucket beyond the longest)."""
+    rows, off = int(np.sum(L)), offsets(L)
+    row = np.arange(rows) - np.repeat(off[:-1], L)
+    f = dict(q=rng.standard_normal((int(np.sum(m)), H, dh)), dout=rng.standard_normal((int(np.sum(m)), H, dh)))
+    for n, gain in (("k", 1.0), ("v", 2.0)):
+        x = 0.002 * rng.standard_normal((rows, Hk, dh))
+        x[np.arange(rows), :, row // 32 % dh] += gain
+        f[n] = x
+    edges = np.unique(np.linspace(1, max(L) - 1, buckets - 1).astype(np.int32))
+    far = [l + (max(L) if l < 1000 else 0) for l in L]
+    tgt_pos = np.repeat(far, m).astype(np.int32) + rng.integers(0, 9, size=int(np.sum(m)), dtype=np.int32)
+    bias = rng.standard_normal((H, len(edges) + 1)).astype(np.float32)
+    return f, dict(edges=edges, bias=bias, tgt_pos=tgt_pos)
+
+
+SPREAD = [  # Hk = H, d_head, history lengths, targets: several kv heads a workgroup, backward tiles 1, 2 and 4
+    (4, 32, [40000, 0, 33, 27000, 17], [3, 3, 1, 5, 5]),
+    (4, 32, [40000, 0, 33, 27000, 17], [20, 3, 1, 3, 5]),
+    (4, 32, [66000], [40]),
+    (6, 32, [30000, 1, 20000], [7, 2, 4]),
+    (4, 64, [34000, 100, 32000], [16, 4, 2]),
+    (2, 128, [80000, 500, 52000], [5, 17, 2]),
+]

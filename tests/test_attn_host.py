@@ -6,6 +6,7 @@ import ctypes
 import numpy as np
 import pytest
 
+import attn_common
 from oracle import attn_oracle as O
 from paper_2511_06077_amd import stca
 
@@ -265,3 +266,31 @@ def test_one_long_history_among_short_ones(L, m, fwd, bwd):
     a, b = attn(n_heads=8, n_kv_heads=2, d_head=64), batch(off(L), off(m))
     assert 0 < stca.stca_attn_workspace_size(a, b, False) <= fwd << 20
     assert 0 < stca.stca_attn_workspace_size(a, b, True) <= bwd << 20
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("Hk,dh,L,m", [s for i, s in enumerate(attn_common.SPREAD) if i != 1])
+def test_a_lost_block_is_seen(Hk, dh, L, m, dtype):
+    """The bounds of the long histories' test against the oracle without one block
+    of 32 rows: out, dq and dbias each show it."""
+    torch = pytest.importorskip("torch")
+    rng = np.random.default_rng(7)
+    m = [min(x, 3) for x in m]
+    f, opts = attn_common.spread(rng, L, m, Hk, Hk, dh)
+    f = {n: attn_common.rounded(torch, x, dtype)[1] for n, x in f.items()}
+    hoff, toff = attn_common.offsets(L), attn_common.offsets(m)
+    pos = np.arange(hoff[-1]) - np.repeat(hoff[:-1], L)
+    r = int(np.argmax(L))
+    for block in (0, L[r] // 64, L[r] // 32 - 1):
+        keep = np.ones(hoff[-1], dtype=bool)
+        keep[hoff[r] + 32 * block:hoff[r] + 32 * block + 32] = False
+        less = np.array([keep[a:b].sum() for a, b in zip(hoff[:-1], hoff[1:])])
+        kw = dict(scale=1.0, masked=True, **{n: x.astype(np.float64) if n == "bias" else x for n, x in opts.items()})
+        if block == 0:
+            ref = O.attention(f["q"], f["k"], f["v"], hoff, toff, dout=f["dout"], hist_pos=pos, **kw)
+        bad = O.attention(f["q"], f["k"][keep], f["v"][keep], attn_common.offsets(less), toff, dout=f["dout"],
+                          hist_pos=pos[keep], **kw)
+        c = attn_common.deep(dtype, dh, L, ref)
+        for n in ("out", "dq", "dbias"):
+            e = attn_common.worst(bad[n], ref[n], ref[n + "_abs"], "f32" if n == "dbias" else dtype, c)
+            assert e > 1.5, (n, block, e)  # (a result may be off by the bound itself)

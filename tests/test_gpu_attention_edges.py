@@ -3,6 +3,7 @@ that are not the host's, the largest tables and values, what is left of weights.
 import numpy as np
 import pytest
 
+import attn_common
 from attn_common import offsets
 from test_gpu_attention import Case, torch  # noqa: F401  (a fixture)
 from test_gpu_guards import Guarded
@@ -315,7 +316,7 @@ def test_gradients_of_a_given_stream(torch):  # noqa: F811
 @pytest.mark.parametrize("cap", [1e4, 1e30])
 def test_a_cap_far_above_the_scores(torch, cap, dtype):  # noqa: F811
     """tanh is relative to small values there: the results of no cap (at 1e4 what
-    it takes off, x^3 / (3 cap^2), is below 2^-24 of a score)."""
+    it takes off, x^3 / (3 cap^2), is about 2^-23 of a score)."""
     c = Case(torch, [200, 33], [9, 20], dtype=dtype, nb=8, masked=True)
     ref = c.oracle()
     c.cap = cap
@@ -323,3 +324,37 @@ def test_a_cap_far_above_the_scores(torch, cap, dtype):  # noqa: F811
     c.cap = 0.0
     e = c.compare(got, ref)
     assert max(e.values()) <= 1.0, e
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("Hk,dh,L,m", attn_common.SPREAD)
+def test_every_block_of_a_long_history(torch, Hk, dh, L, m, dtype):  # noqa: F811
+    """Several kv heads a workgroup, with bounds that a lost block exceeds."""
+    c = Case(torch, L, m, dtype=dtype, H=Hk, dh=dh, masked=True)
+    f, opts = attn_common.spread(np.random.default_rng(7), L, m, Hk, Hk, dh)
+    for n, x in f.items():
+        c.t[n], c.f[n] = attn_common.rounded(torch, x, dtype)
+    c.scale, c.edges, c.bias, c.tgt_pos = 1.0, opts["edges"], opts["bias"], opts["tgt_pos"]
+    ref, got = c.oracle(), c.step()
+    bound = attn_common.deep(dtype, dh, L, ref)
+    e = {n: attn_common.worst(x.double().cpu().numpy(), ref[n], ref[n + "_abs"], "f32" if n == "dbias" else dtype, bound)
+         for n, x in got.items()}
+    print("[spread]", {n: round(x, 3) for n, x in e.items()}, f"c={bound:.1e}", flush=True)
+    assert max(e.values()) <= 1.0, e
+
+
+@pytest.mark.parametrize("page,dh,H,nb", [(16, 32, 4, 8), (64, 64, 8, 0), (128, 128, 2, 16)])
+def test_eight_bit_rows_of_many_steps(torch, page, dh, H, nb):  # noqa: F811
+    """K rows from 2^-12 to 2 and V rows from 2^-20 to 2^20: neighbours in a block
+    have steps of their own, and the largest rows' do not spill into the others."""
+    from test_gpu_cache import Users, serve
+    u = Users(torch, [1500, 70, 33, 1], [0] * 4, page, dh=dh, gain=1.0, seed=8)
+    rng = np.random.default_rng(3)
+    for n, lo, hi in (("k", -12, 2), ("v", -20, 21)):
+        f = 2.0 ** rng.integers(lo, hi, size=u.f[n].shape[:2])[..., None]
+        u.f[n] = u.f[n] * f
+        u.t[n] = torch.from_numpy(u.f[n]).to(torch.bfloat16)
+        assert np.array_equal(u.t[n].double().numpy(), u.f[n])
+    u.write()
+    plan, _, e = serve(u, torch, [3, 20, 1, 2], H, nb=nb, masked=nb > 0, cap=20.0 if nb == 16 else 0.0)
+    assert plan.device_status() == 0 and e <= 1.0
