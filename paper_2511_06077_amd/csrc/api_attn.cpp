@@ -195,10 +195,10 @@ bool ragged_plan(const stca_attn_t* a, const stca_batch_t* b, bool backward, Pla
   if (b->hist_off_host && parts_rows * H * dh * 4 > kFreePartials) {
     int64_t own = 0;
     for (int r = 0; r < b->n_requests; ++r)
-      own += ceil_div(b->hist_off_host[r + 1] - b->hist_off_host[r], p->chunk) *
-             static_cast<int64_t>(b->tgt_off_host[r + 1] - b->tgt_off_host[r]);
+      own += std::max<int64_t>(1, ceil_div(b->hist_off_host[r + 1] - b->hist_off_host[r], p->chunk)) *
+             (b->tgt_off_host[r + 1] - b->tgt_off_host[r]);
     const int64_t most = std::max(kSparePartials * own, kFreePartials / (static_cast<int64_t>(H) * dh * 4));
-    while (parts_rows > most) {
+    while (parts_rows > most) {  // (two chunks are always few enough, so a chunk stays below 2^31 rows)
       p->chunk *= 2;
       parts_rows = part_rows_of(b, max_m, max_l, p->chunk, &p->part_tgt);
     }

@@ -268,6 +268,17 @@ def test_one_long_history_among_short_ones(L, m, fwd, bwd):
     assert 0 < stca.stca_attn_workspace_size(a, b, True) <= bwd << 20
 
 
+@pytest.mark.parametrize("G", [1, 4])
+@pytest.mark.parametrize("first", [1 << 20, 0x7fff0000 - 60, 0x5fff0001])
+def test_the_longest_history_beside_targets_without_one(G, first):
+    """Chunks of the longest history there may be stay below 2^31 rows."""
+    a = attn(n_heads=4 * G, n_kv_heads=4, d_head=128)
+    b = batch([0, first, first, first + 50], [0, 1, 1000001, 1000002])
+    for back in (False, True):
+        own = 8 * 1000002 * a.n_heads * (a.d_head + 2) * 4 + (8 * (first + 50) * 4 * 128 if back else 0) + (first << 4)
+        assert 0 < stca.stca_attn_workspace_size(a, b, back) < own
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("Hk,dh,L,m", [s for i, s in enumerate(attn_common.SPREAD) if i != 1])
 def test_a_lost_block_is_seen(Hk, dh, L, m, dtype):
