@@ -75,9 +75,19 @@ def _flat(name, t, dtype, shape, device):
     return t
 
 
+def _int32(name, a):
+    """a as a contiguous int32 array of the same values."""
+    given = np.asarray(a.cpu().numpy() if isinstance(a, _torch().Tensor) else a)
+    with np.errstate(invalid="ignore"):
+        host = np.ascontiguousarray(given.astype(np.int32))
+    if not np.array_equal(host, given):
+        raise ValueError(f"{name}: whole numbers of 32 bits are needed")
+    return host
+
+
 def _offsets(off, device):
     torch = _torch()
-    host = np.ascontiguousarray(off.cpu().numpy() if isinstance(off, torch.Tensor) else off, dtype=np.int32)
+    host = _int32("offsets", off)
     if host.ndim != 1 or len(host) < 2:
         raise ValueError("offsets: [requests + 1] is needed")
     return host, torch.from_numpy(host.copy()).to(device)
@@ -94,7 +104,7 @@ class _Scores:
 
     def _scores(self, n_heads, n_kv_heads, d_head, dtype, scale, softcap, edges, masked):
         self.n_heads, self.n_kv_heads, self.d_head, self.dtype = n_heads, n_kv_heads, d_head, dtype
-        self.edges = None if edges is None else np.ascontiguousarray(edges, dtype=np.int32)
+        self.edges = None if edges is None else _int32("edges", edges)
         if self.edges is not None and self.edges.ndim != 1:
             raise ValueError("edges: one-dimensional")
         self.n_buckets = 0 if self.edges is None else len(self.edges) + 1
@@ -203,7 +213,8 @@ class HistoryCache:
     table [requests][..] (int32) lists each request's pages, and its row i is
     slot i % page_size of page table[i // page_size].  Writes to slots of their own
     and reads may overlap on several streams; device_status is then the last one's
-    to end."""
+    to end.  The pages are cleared on the stream that is current here: other streams
+    wait for it before their first write."""
 
     def __init__(self, n_pages: int, page_size: int, n_kv_heads: int, d_head: int, fmt: str = "int8",
                  positions: bool = False, device="cuda"):
@@ -261,7 +272,8 @@ class HistoryCache:
                                   self.stream() if stream is None else stream)
 
     def read(self, row_off, start, table, n_rows: int, dtype=None, stream: Optional[int] = None):
-        """(k, v) [n_rows][n_kv_heads][d_head], and pos where the cache keeps them."""
+        """(k, v) [n_rows][n_kv_heads][d_head], and pos where the cache keeps them.
+        Rows without a page are not written, and hold anything (see device_status)."""
         torch = _torch()
         dtype = dtype or torch.bfloat16
         rows = self._rows(row_off, start, table, n_rows)

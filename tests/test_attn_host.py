@@ -268,6 +268,21 @@ def test_one_long_history_among_short_ones(L, m, fwd, bwd):
     assert 0 < stca.stca_attn_workspace_size(a, b, True) <= bwd << 20
 
 
+def test_edges_and_offsets_keep_their_values():
+    """Numbers that int32 cannot hold are refused, not wrapped or cut."""
+    pytest.importorskip("torch")
+    from paper_2511_06077_amd import attention
+    for bad in ([0, 2 ** 32 + 5], [0, -2 ** 31 - 1], [0, 1.5], [0, float("nan")], ["a"], np.array([0, 2 ** 31], dtype=np.uint32)):
+        with pytest.raises(ValueError):
+            attention._int32("edges", bad)
+        with pytest.raises(ValueError):
+            attention._offsets(bad, "cpu")
+    for good in ([0, 3], (0, 3), [0.0, 3.0], np.array([0, 3]), np.array([0, 3], dtype=np.uint8), np.array([0, 9, 3])[::2]):
+        host, dev = attention._offsets(good, "cpu")
+        assert host.dtype == np.int32 and host.flags.c_contiguous and list(host) == [0, 3] and dev.tolist() == [0, 3]
+    assert attention._int32("edges", []).shape == (0,)
+
+
 @pytest.mark.parametrize("G", [1, 4])
 @pytest.mark.parametrize("first", [1 << 20, 0x7fff0000 - 60, 0x5fff0001])
 def test_the_longest_history_beside_targets_without_one(G, first):
