@@ -159,17 +159,15 @@ __device__ __forceinline__ bool odd_bf16(uint32_t w) {  // a half of w is not fi
 
 // Two waves a SIMD, where the registers hold a block, the next one on its way,
 // the output and the rows.  Of 128 features they do without the next block (one
-// wave that has it: 32 targets on 8-bit pages 276 us for 202, rows of 16 targets
-// 190 for 157); with two tiles of bf16 even that spills, and one wave that
-// fetches ahead is better (16 x 4 rows on bf16 pages 177 us for 268).
-template <int KV, int DH, int MT> constexpr bool kOneWave = DH == 128 && MT > 1 && KV != kPagedInt8;
+// wave that has it, two tiles: 32 requests of 10240 8-bit rows, 32 targets, 4 heads
+// 169 us for 124; 24 of 10240 bf16 rows, 16 targets, 4 heads to a kv head 231 for 189).
 // Three of 8-bit rows of 32 features: left to itself the compiler takes one register
 // too many for them (128 requests of 10240 rows, 32 targets 277 us, three 248).
-template <int KV, int DH, int MT> constexpr int kFwdWaves = kOneWave<KV, DH, MT> ? 1 : KV == kPagedInt8 && DH == 32 ? 3 : 2;
-template <int KV, int DH, int MT> constexpr bool kAhead = DH < 128 || kOneWave<KV, DH, MT>;
+template <int KV, int DH> constexpr int kFwdWaves = KV == kPagedInt8 && DH == 32 ? 3 : 2;
+template <int DH> constexpr bool kAhead = DH < 128;
 
 template <typename T, int KV, int DH, int MT>
-__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kFwdWaves<KV, DH, MT>))) void attn_fwd_kernel(const AttnArgs a) {
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kFwdWaves<KV, DH>))) void attn_fwd_kernel(const AttnArgs a) {
   constexpr bool kF32 = !Elem<T>::bf16;
   constexpr bool kPaged = KV != kRagged;
   constexpr int NT = 2;
@@ -646,10 +644,10 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kFwdWa
     const int jstop = min(jend, jb + share * BJ);
     if (jb < jstop) {
       Blk blk;
-      if constexpr (kAhead<KV, DH, MT>) load(blk, jb);
+      if constexpr (kAhead<DH>) load(blk, jb);
       for (; jb < jstop; jb += BJ) {
-        if constexpr (!kAhead<KV, DH, MT>) load(blk, jb);
-        compute(blk, jb, kAhead<KV, DH, MT> && jb + BJ < jstop);
+        if constexpr (!kAhead<DH>) load(blk, jb);
+        compute(blk, jb, kAhead<DH> && jb + BJ < jstop);
       }
     }
 

@@ -109,10 +109,12 @@ hipError_t merge_t(const AttnArgs& a, bool paged, int dh, hipStream_t st) {
 }  // namespace
 
 // Row tiles of 16 a wave holds.  More read K and V less often, fewer leave room
-// for a second wave on the SIMD: four of them were slower throughout (64 targets
-// on packed rows 110 us for 92, of 64 features 453 for 197), and of 128 features
-// two are, except where a page's rows are converted or looked up once for both
-// (8-bit 261 us for 197, bf16 274 for 177).
+// for a second wave on the SIMD: four of them are slower throughout (128 requests
+// of 2048 packed rows, 64 targets, 8 heads of 32 features 170 us for 144, of 64 435
+// for 192), and of 128 features two are (32 targets, 4 heads 234 for 164), except
+// where a page's rows are converted or looked up once for both (one tile: 32 requests
+// of 10240 8-bit rows, 32 targets, 4 heads 145 us for 123; 24 of 10240 bf16 rows, 16
+// targets, 4 heads to a kv head 254 for 189).
 int forward_tiles(int dtype, int dh, int max_rows, bool paged) {
   const int most = dtype == STCA_BF16 ? (dh == 128 && !paged ? 1 : 2) : (dh == 128 ? 1 : 2);
   return max_rows > 16 ? most : 1;
