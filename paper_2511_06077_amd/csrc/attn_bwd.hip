@@ -206,12 +206,12 @@ struct BwdLds {
 // sums stay within 36 KB, else every second or fourth, which then take turns.
 inline __host__ __device__ int bin_copies(int n) { return n <= 34 ? 64 : n <= 70 ? 32 : 16; }
 
-// Waves a SIMD is to hold: what the registers allow with few spills (48 requests,
-// 4 heads of 64 to a kv head, 4 tiles: one 394 us, two 547), and no more than
-// two, since the workgroups of a chunk's heads, which read parts of the same
+// Waves a SIMD is to hold: what the registers allow with few spills (128 requests
+// of 2048 rows, 48 targets, 8 heads of 64, 4 tiles: two 376 us, one 514), and no more
+// than two, since the workgroups of a chunk's heads, which read parts of the same
 // DRAM pages, drift apart the more of them run (window of 256 requests, 16
-// targets, 2048 rows, 8 heads of 32: two 312 us, three 335, four 357).
-template <typename T, int DH, int MT> constexpr int kBwdWaves = DH == 128 || (DH == 64 && MT == 4) ? 1 : 2;
+// targets, 2048 rows, 8 heads of 32: one 366 us, two 288, three 327, four 363).
+template <typename T, int DH, int MT> constexpr int kBwdWaves = DH == 128 ? 1 : 2;
 template <typename T, int DH, int MT> constexpr int kBwdMost = kBwdWaves<T, DH, MT> == 1 ? 8 : 2;
 
 // The kernel's arguments, `kFresh`: as loads that are not moved out of a loop.
