@@ -35,12 +35,11 @@
 // one.  (LDS float atomics in their place take a cycle a lane: 2.3 times the
 // kernel's time, window of 256 requests with 32 buckets.)
 //
-// Of that window (16 targets, 2048 rows, 8 heads of 32) a call takes 308 us
-// without bias, 1.5 times what its bytes take at a large copy's rate, and 390 to
-// 400 with a mask and 32 buckets: instructions, of which an LDS turn of the bucket
-// sums takes most.  Several passes wait for each other's barriers instead (48
-// requests, 4 heads of 64 to a kv head, 228 us, 3 barriers a pass for 5 and two
-// passes' rows in LDS took 6% off).
+// Of that window (16 targets, 2048 rows, 8 heads of 32) a call takes 290 us
+// without bias, 1.4 times what its bytes take at a large copy's rate, and 392 to
+// 400 with a mask and 32 buckets: the turns of the bucket sums in LDS.  Several
+// passes wait for each other's barriers instead (48 requests, 4 heads of 64 to a kv
+// head, 227 us; 3 barriers a pass for 5 and two passes' rows in LDS took 6% off).
 #include <type_traits>
 
 #include "attn_ops.h"
@@ -216,8 +215,8 @@ template <typename T, int DH, int MT> constexpr int kBwdMost = kBwdWaves<T, DH, 
 
 // The kernel's arguments, `kFresh`: as loads that are not moved out of a loop.
 // Kept from pass to pass they take more scalar registers than there are (48
-// requests, 4 heads of 64 to a kv head: 247 us for 238, without bias 158 for
-// 143); with one pass the loads cost more (415 us for 404).
+// requests, 4 heads of 64 to a kv head: 238 us for 227, without bias 149 for 141, of
+// 128 455 for 342); with one pass the loads cost more (the window 400 us for 396).
 typedef const __attribute__((address_space(4))) AttnArgs KernelArgs;
 template <bool kFresh>
 __device__ __forceinline__ decltype(auto) again(const AttnArgs& a) {
@@ -841,8 +840,9 @@ hipError_t launch_bwd(const AttnArgs& a, hipStream_t st) {
   return hipGetLastError();
 }
 
-// (A kernel of its own where one pass is all: without the state of the others
-// fewer registers spill, 48 targets of 4 heads of 128 features 589 us for 868.)
+// (A kernel of its own where one pass is all, without the state of the others: 48
+// targets of 8 heads of 64 features 379 us for 486, the window 392 for 420; of 4 heads
+// of 128, whose four tiles spill either way, 603 for 573.)
 template <typename T, int DH>
 hipError_t backward_dh(const AttnArgs& a, int tiles, hipStream_t st) {
   const bool one = a.bufs == 1;
@@ -852,10 +852,8 @@ hipError_t backward_dh(const AttnArgs& a, int tiles, hipStream_t st) {
     if constexpr (DH == 32)
       if (tiles == 4) return one ? launch_bwd<T, DH, 4, true>(a, st) : launch_bwd<T, DH, 4, false>(a, st);
   }
-  if constexpr (DH < 128)
+  if constexpr (DH < 128 || Elem<T>::bf16)
     if (tiles == 2) return one ? launch_bwd<T, DH, 2, true>(a, st) : launch_bwd<T, DH, 2, false>(a, st);
-  if constexpr (DH == 128 && Elem<T>::bf16)
-    if (tiles == 2) return launch_bwd<T, DH, 2, true>(a, st);
   return one ? launch_bwd<T, DH, 1, true>(a, st) : launch_bwd<T, DH, 1, false>(a, st);
 }
 
@@ -886,15 +884,15 @@ size_t backward_lds(int dtype, int dh, int tiles, int bufs, int hw, int G, int n
 // Row tiles a wave holds: the fewest that take a request's `need` tiles of a head
 // in one pass, up to what registers (dq, DH / 16 x 4 a tile) and LDS allow.  In
 // bf16 of 64 and 128 features four spill: they pay where one pass then takes the
-// chunk (128 requests of 2048, 48 targets, 8 heads of 64: 534 us for 1150; 4 of
-// 128: 782 for 1610), but not where the heads that share a kv head or more
-// targets make several passes anyway, of chunks of one step a wave: there two
-// waves a SIMD count, which two tiles of 64 features leave and one of 128 (48
-// requests, 4 heads of 64 to a kv head: two 249 us, one 254, four 394; 100
-// targets, heads of 64: 690, 717 and 1101; of 128: one 741, four 1017).
+// chunk (128 requests of 2048 rows, 48 targets, 8 heads of 64: four tiles 379 us, two
+// 973; 4 heads of 128: four 603, two 1379, one 1462), but not where the heads that
+// share a kv head or more targets make several passes anyway, of chunks of one step a
+// wave (48 requests, 4 heads of 64 to a kv head: two 227 us, one 250, four 428; of 128:
+// two 342, one 375, four 397; 128 requests, 100 targets, 4 heads of 64: two 889, one
+// 1015, four 1302; of 128: two 2496, one 2758, four 2775).
 int backward_tiles(int dtype, int dh, int need, int G) {
   if (dtype != STCA_BF16) return dh < 128 && need >= 2 ? 2 : 1;
-  if (dh > 32 && (G > 1 || need > 4)) return dh == 64 && need > 1 ? 2 : 1;
+  if (dh > 32 && (G > 1 || need > 4)) return need > 1 ? 2 : 1;
   return need >= 3 ? 4 : need == 2 ? 2 : 1;
 }
 
