@@ -424,7 +424,12 @@ stca_status_t stca_forward_paper_profiled(const stca_dims_t* dims, const stca_ba
  * contribute nothing, whatever their K and V hold; a target that sees no row
  * (its request may have none) has the output 0, and no part in any gradient.
  * D saturates at the ends of int32.  Sums, maxima and weights are fp32; with
- * bf16 storage the weights enter the matrix cores as two bf16 terms.
+ * bf16 storage the weights enter the matrix cores as two bf16 terms, the second
+ * rounded (2^-16 of a weight), and as three, an fp32 whole, in a forward that
+ * saves: its output may differ in the last bit from one that does not.  A call
+ * repeats bitwise; how a request's sums are divided, and so their last bits,
+ * depends on the whole batch.  Any finite V whose weighted mean is finite may
+ * be given.
  *
  * Calls of one batch on different streams need distinct workspaces.  Targets
  * of a request without history are legal here.  Offsets are checked on the

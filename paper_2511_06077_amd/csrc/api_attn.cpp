@@ -110,12 +110,16 @@ struct Plan {
 // have `rows` history rows times `per_row` workgroups to itself: a workgroup
 // costs its start, the join of its waves and a partial to merge, and the last
 // ones to run leave CUs idle, the less the more there are (window of 256
-// requests, 16 targets, 2048 rows, d_h = 32: 4 a CU 145 us forward, 620
-// backward, 8 134 and 312, 16 142 and 347; pages, whose chunks are whole runs of
-// 256 rows, take 4: 128 requests of 10240 8-bit rows 259 us, 6 292, 8 269).
+// requests, 16 targets, 2048 rows, d_h = 32, no bias: 4 a CU 142 us forward, 504
+// backward, 8 131 and 291, 16 137 and 302).  Pages, whose chunks are whole runs of
+// 256 rows, take 4: 128 requests of 10240 8-bit rows, 32 targets: 2 250 us, 4 250, 6
+// 284, 8 255, one target 197, 197, 212, 183; 24 requests of 1 to 10240 bf16 rows of
+// 128 features 159, 110, 151, 107, all of 10240 180, 189, 200, 212.
 constexpr int kPackedPerCu = 8, kPagedPerCu = 4;
 // ... and the fewest rows a wave is to have of it: shorter chunks are mostly
-// start and join.
+// start and join, longer ones leave CUs idle (64 requests of 1024 rows, 4 heads of
+// 32, mask and 32 buckets: 64 rows 29.0 us forward, 128 25.0, 256 30.2; 32 rows 59.8
+// backward, 64 54.8, 128 56.8).
 constexpr int kWaveRows = 128, kWaveRowsBack = 64;
 int chunk_for(int64_t rows, int64_t per_row, int per_cu, int step) {
   const int64_t want = static_cast<int64_t>(per_cu) * device_cus();
@@ -125,11 +129,10 @@ int chunk_for(int64_t rows, int64_t per_row, int per_cu, int step) {
 
 // kv heads a workgroup takes: 32 features of bf16 are half a cache line, and a
 // line whose other half another workgroup reads later comes from memory twice
-// (window of 256 requests of 2048 rows, 8 heads of 32: 4 heads a workgroup 145
-// us forward for 204 with one, 2 heads 360 us backward for 549).  In the
-// backward two (rows of every head wait in LDS: four take 375 us where two take
-// 373, with a bias of 32 buckets 447 for 404), and one where each holds four
-// tiles; only where a wave to a head then has 256 history rows on every SIMD of
+// (window of 256 requests of 2048 rows, 8 heads of 32, no bias: 4 heads a workgroup
+// 131 us forward, two 136, one 182; two 291 us backward, one 500).  In the backward
+// two at most (registers fetch, and LDS holds, the rows of as many), and one where
+// each holds four tiles; only where a wave to a head then has 256 history rows on every SIMD of
 // the card, since fewer heads a workgroup are shorter chunks for as many waves;
 // and no more than the LDS holds the tables of (`lds` of a workgroup of hw heads),
 // forward of two workgroups, which is what the registers leave room for (32

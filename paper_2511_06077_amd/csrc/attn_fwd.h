@@ -7,12 +7,12 @@
 // waves share a head, each with consecutive blocks of 16 NT history rows and
 // softmax statistics and an output of its own, joined in LDS at the end.  Four
 // heads a workgroup read packed rows in whole cache lines at one time (256
-// requests, 16 targets, 2048 rows, 8 heads of 32 features: 145 us for 204); one
+// requests, 16 targets, 2048 rows, 8 heads of 32 features: 131 us, one 182); one
 // head a workgroup spreads a small batch over more of them.  Several chunks
 // leave (output, maximum, sum) partials for attn_merge.
 //
 // Packed rows are bound by their bytes (that window: 541 MB, 104 us at a large
-// copy's rate, takes 134 us, with mask and bias 147), pages by the vector
+// copy's rate, takes 131 us, with mask and bias 149), pages by the vector
 // instructions of a score: 8-bit rows are converted for the matrix cores, and a
 // target of few rows fills a quarter of a tile or less.
 //

@@ -15,7 +15,7 @@ hipError_t forward_dh(const AttnArgs& a, int tiles, hipStream_t st) {
 }
 
 // Partials of a row (target, head) joined, in an order that depends on their
-// number alone: 16 lanes a row, DH / 16 features each, times kSplit lanes that
+// number and the call's number of rows (see merge_dh) alone: 16 lanes a row, DH / 16 features each, times kSplit lanes that
 // take every kSplit-th chunk.
 template <typename T, int DH, int kSplit>
 __global__ __launch_bounds__(256) void attn_merge_kernel(const AttnArgs a, bool paged) {
