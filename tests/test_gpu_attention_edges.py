@@ -174,7 +174,7 @@ def test_weights_are_not_low_backward(torch):  # noqa: F811
 
 # The largest V of the types: equal signs and nearly equal scores, so that every
 # sum before the division is the number of rows times larger.  (Rows are taken a
-# second time, with scores up to 8 + log2(rows) < 24 from their maximum: 24 u of a
+# second time, with scores up to 8 + log2(rows) < 26 from their maximum: 26 u of a
 # weight, which the bounds' 2 (rows + ..) u hold many times over.)
 TOP = 3.3e38
 
