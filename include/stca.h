@@ -472,7 +472,7 @@ typedef struct {
 
 /* Byte offsets into the buffer that a forward saves for its backward, fp32:
  * a [n_tgt][n_heads][d_head] (the output before rounding), and per target and
- * head a score max near the largest, in units of log2 e, and the sum of
+ * head a score max near the largest (8 below to 40 above), in units of log2 e, and the sum of
  * 2^(x log2 e - max) [n_tgt][n_heads]. */
 typedef struct {
   size_t a, max, sum;

@@ -45,10 +45,10 @@ namespace ops {
 
 constexpr int kRagged = 0, kPagedBf16 = 1, kPagedInt8 = 2;
 constexpr float kSlack = 8.f;  // a weight before the division is at most 2^8
-// ... and a sum of them times V may leave fp32 where the output does not.  A wave
-// whose sums reach 2^100 (or are not finite) takes its rows again with weights of
-// at most 1 / (the request's rows); sums below that stay finite through the joins.
-// (Not at once: so small a weight's exponent has fewer bits for its fraction.)
+// ... and a sum of them times V may leave fp32 where the output does not.  Where one
+// of a workgroup's comes to 2^100 (or is not finite), it takes the rows again with
+// weights of at most 1 / (the request's rows); below that all joins stay finite.
+// (Not from the start: scores far below the maximum lose bits in the subtraction.)
 constexpr float kLargeSum = 1.2676506002282294e30f;  // 2^100
 
 template <int DH> constexpr int kCombineFloats = kWaves * 16 * (DH + 2);  // LDS before the tables (see forward_lds)
