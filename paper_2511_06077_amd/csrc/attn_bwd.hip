@@ -794,7 +794,7 @@ __global__ __launch_bounds__(256) void attn_bwd_sum_kernel(const AttnArgs a, int
     const int len = clamp_off(a.hist_off[lo + 1], a.n_hist) - clamp_off(a.hist_off[lo], a.n_hist);
     const int n = max(1, min(a.max_chunks, (len + a.chunk - 1) / a.chunk));
     int64_t first, step;
-    if (!part_rows(a, lo, t, static_cast<int>(row % a.H), first, step)) return;
+    if (!part_rows(a, lo, t, row, first, step)) return;
     float acc[NE] = {};
 #pragma unroll 4
     for (int c = 0; c < n; ++c)

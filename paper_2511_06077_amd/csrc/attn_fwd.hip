@@ -36,7 +36,7 @@ __global__ __launch_bounds__(256) void attn_merge_kernel(const AttnArgs a, bool 
     int len;
     if (paged) len = min(max(a.lens[lo], 0), a.max_len);
     else len = clamp_off(a.hist_off[lo + 1], a.n_hist) - clamp_off(a.hist_off[lo], a.n_hist);
-    if (len > a.chunk && part_rows(a, lo, t, static_cast<int>(row % a.H), first, step))
+    if (len > a.chunk && part_rows(a, lo, t, row, first, step))
       n = min(a.max_chunks, (len + a.chunk - 1) / a.chunk);  // (else written by the attention itself)
   }
   float M = -INFINITY, L = 0.f, acc[NE] = {};

@@ -294,17 +294,17 @@ template <typename Args>
 __device__ __forceinline__ int64_t part_row(const Args& a, int c, int64_t u, int64_t t0, int64_t t) {
   return a.part_tgt ? u * a.part_tgt + (t - t0) : c * a.n_tgt + t;
 }
-// ... of the first chunk, for a row (target, head) of request r, and how far apart
+// ... of the first chunk, for a row (target t, head) of request r, and how far apart
 // its chunks' lie; false where offsets that are not the host's leave it none.
-__device__ __forceinline__ bool part_rows(const AttnArgs& a, int r, int64_t t, int h, int64_t& at, int64_t& step) {
-  int64_t u = 0, t0 = 0;
+__device__ __forceinline__ bool part_rows(const AttnArgs& a, int r, int64_t t, int64_t row, int64_t& at, int64_t& step) {
+  at = row;
+  step = a.n_tgt * a.H;
   if (a.part_tgt) {
-    u = clamp_off(a.hist_off[r], a.n_hist) / a.chunk + r;
-    t0 = clamp_off(a.tgt_off[r], a.n_tgt);
-    if (t < t0 || t - t0 >= a.part_tgt) return false;
+    const int64_t u = clamp_off(a.hist_off[r], a.n_hist) / a.chunk + r, in = t - clamp_off(a.tgt_off[r], a.n_tgt);
+    if (in < 0 || in >= a.part_tgt) return false;
+    at = (u * a.part_tgt + in - t) * a.H + row;
+    step = static_cast<int64_t>(a.part_tgt) * a.H;
   }
-  at = part_row(a, 0, u, t0, t) * a.H + h;
-  step = (a.part_tgt ? a.part_tgt : a.n_tgt) * a.H;
   return true;
 }
 
