@@ -110,15 +110,15 @@ struct Plan {
 // have `rows` history rows times `per_row` workgroups to itself: a workgroup
 // costs its start, the join of its waves and a partial to merge, and the last
 // ones to run leave CUs idle, the less the more there are (window of 256
-// requests, 16 targets, 2048 rows, d_h = 32, no bias: 4 a CU 142 us forward, 504
-// backward, 8 131 and 291, 16 137 and 302).  Pages, whose chunks are whole runs of
-// 256 rows, take 4: 128 requests of 10240 8-bit rows, 32 targets: 2 250 us, 4 250, 6
-// 284, 8 255, one target 197, 197, 212, 183; 24 requests of 1 to 10240 bf16 rows of
-// 128 features 159, 110, 151, 107, all of 10240 180, 189, 200, 212.
+// requests, 16 targets, 2048 rows, d_h = 32, no bias: 4 a CU 139 us forward, 504
+// backward, 8 128 and 291, 16 136 and 302).  Pages, whose chunks are whole runs of
+// 256 rows, take 4: 128 requests of 10240 8-bit rows, 32 targets: 2 246 us, 4 246, 6
+// 284, 8 255, one target 199, 199, 216, 185; 24 requests of 1 to 10240 bf16 rows of
+// 128 features 160, 110, 153, 109, all of 10240 182, 190, 201, 214.
 constexpr int kPackedPerCu = 8, kPagedPerCu = 4;
 // ... and the fewest rows a wave is to have of it: shorter chunks are mostly
 // start and join, longer ones leave CUs idle (64 requests of 1024 rows, 4 heads of
-// 32, mask and 32 buckets: 64 rows 29.0 us forward, 128 25.0, 256 30.2; 32 rows 59.8
+// 32, mask and 32 buckets: 64 rows 28.8 us forward, 128 25.0, 256 29.5; 32 rows 59.8
 // backward, 64 54.8, 128 56.8).
 constexpr int kWaveRows = 128, kWaveRowsBack = 64;
 int chunk_for(int64_t rows, int64_t per_row, int per_cu, int step) {
@@ -130,7 +130,7 @@ int chunk_for(int64_t rows, int64_t per_row, int per_cu, int step) {
 // kv heads a workgroup takes: 32 features of bf16 are half a cache line, and a
 // line whose other half another workgroup reads later comes from memory twice
 // (window of 256 requests of 2048 rows, 8 heads of 32, no bias: 4 heads a workgroup
-// 131 us forward, two 136, one 182; two 291 us backward, one 500).  In the backward
+// 128 us forward, two 133, one 179; two 291 us backward, one 500).  In the backward
 // two at most (registers fetch, and LDS holds, the rows of as many), and one where
 // each holds four tiles; only where a wave to a head then has 256 history rows on every SIMD of
 // the card, since fewer heads a workgroup are shorter chunks for as many waves;

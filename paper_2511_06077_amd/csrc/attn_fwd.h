@@ -7,12 +7,12 @@
 // waves share a head, each with consecutive blocks of 16 NT history rows and
 // softmax statistics and an output of its own, joined in LDS at the end.  Four
 // heads a workgroup read packed rows in whole cache lines at one time (256
-// requests, 16 targets, 2048 rows, 8 heads of 32 features: 131 us, one 182); one
+// requests, 16 targets, 2048 rows, 8 heads of 32 features: 128 us, one 179); one
 // head a workgroup spreads a small batch over more of them.  Several chunks
 // leave (output, maximum, sum) partials for attn_merge.
 //
 // Packed rows are bound by their bytes (that window: 541 MB, 104 us at a large
-// copy's rate, takes 131 us, with mask and bias 149), pages by the vector
+// copy's rate, takes 128 us, with mask and bias 146), pages by the vector
 // instructions of a score: 8-bit rows are converted for the matrix cores, and a
 // target of few rows fills a quarter of a tile or less.
 //
@@ -162,9 +162,9 @@ __device__ __forceinline__ bool odd_bf16(uint32_t w) {  // a half of w is not fi
 // Two waves a SIMD, where the registers hold a block, the next one on its way,
 // the output and the rows.  Of 128 features they do without the next block (one
 // wave that has it, two tiles: 32 requests of 10240 8-bit rows, 32 targets, 4 heads
-// 169 us for 124; 24 of 10240 bf16 rows, 16 targets, 4 heads to a kv head 231 for 189).
+// 172 us for 126; 24 of 10240 bf16 rows, 16 targets, 4 heads to a kv head 231 for 190).
 // Three of 8-bit rows of 32 features: left to itself the compiler takes one register
-// too many for them (128 requests of 10240 rows, 32 targets 277 us, three 248).
+// too many for them (128 requests of 10240 rows, 32 targets 273 us, three 250).
 template <int KV, int DH> constexpr int kFwdWaves = KV == kPagedInt8 && DH == 32 ? 3 : 2;
 template <int DH> constexpr bool kAhead = DH < 128;
 

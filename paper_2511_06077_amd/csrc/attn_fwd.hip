@@ -110,11 +110,11 @@ hipError_t merge_t(const AttnArgs& a, bool paged, int dh, hipStream_t st) {
 
 // Row tiles of 16 a wave holds.  More read K and V less often, fewer leave room
 // for a second wave on the SIMD: four of them are slower throughout (128 requests
-// of 2048 packed rows, 64 targets, 8 heads of 32 features 170 us for 144, of 64 435
-// for 192), and of 128 features two are (32 targets, 4 heads 234 for 164), except
+// of 2048 packed rows, 64 targets, 8 heads of 32 features 155 us for 131, of 64 428
+// for 183), and of 128 features two are (32 targets, 4 heads 278 for 163), except
 // where a page's rows are converted or looked up once for both (one tile: 32 requests
-// of 10240 8-bit rows, 32 targets, 4 heads 145 us for 123; 24 of 10240 bf16 rows, 16
-// targets, 4 heads to a kv head 254 for 189).
+// of 10240 8-bit rows, 32 targets, 4 heads 145 us for 126; 24 of 10240 bf16 rows, 16
+// targets, 4 heads to a kv head 252 for 190).
 int forward_tiles(int dtype, int dh, int max_rows, bool paged) {
   const int most = dtype == STCA_BF16 ? (dh == 128 && !paged ? 1 : 2) : (dh == 128 ? 1 : 2);
   return max_rows > 16 ? most : 1;
