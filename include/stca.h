@@ -575,6 +575,144 @@ stca_status_t stca_cache_attn(const stca_attn_t* attn, const stca_cache_t* cache
                               const void* q, int64_t ldq, const int32_t* tgt_pos, const float* bias, void* out,
                               void* ws, size_t ws_bytes, hipStream_t stream);
 
+/* ---- Rows from ids, and the gradient of their tables.  What stands before the
+ * layers (Sec. 3.1, "Input encoding": a history row is fused from several looked-up
+ * embeddings) and behind their backward (dhist, dtgt):
+ *   out_i = scale sum_f table_f[ids_f[i]]       sums in fp32, fields in order, one rounding
+ * A negative id is no row and adds nothing.  An id behind its table is taken for
+ * none as well, and sets the status in ws (nullable; 256 device bytes, cleared by
+ * the caller: a lookup only sets it, so that several may share it). */
+typedef struct {
+  int32_t d;            /* features of a row: a multiple of 8, at most 8192 */
+  int32_t table_dtype;  /* stca_dtype_t of the tables */
+  int32_t out_dtype;    /* ... of out */
+  float scale;          /* finite */
+} stca_embed_t;
+typedef struct {
+  const void* table;    /* [n_rows][d] */
+  int64_t n_rows;       /* at least 1, below 2^31 - 2^16 */
+  int64_t ld;           /* row strides in elements as in stca_attn_in_t (0 = dense) */
+  const int32_t* ids;   /* device [n] */
+} stca_embed_field_t;
+#define STCA_EMBED_FIELDS 8 /* most fields of a call */
+stca_status_t stca_embed_forward(const stca_embed_t* embed, const stca_embed_field_t* fields, int32_t n_fields,
+                                 int64_t n, void* out, int64_t ldo, void* ws, hipStream_t stream);
+
+/* The gradient of one table, fp32, from up to four parts that look it up (a
+ * request's history and targets share the item table):
+ *   dT[v] = scale sum over the parts' rows i with ids[i] = v of dout_i
+ * The rows of an id are added in the order of the parts and of their rows,
+ * grouped by their place among all sorted ids; nothing is added in order of
+ * arrival, so a call repeats bitwise.  n below is the rows of all parts together.
+ *   dense   dtable [n_rows][d] (row stride ld), overwritten, or added to where
+ *           accumulate is nonzero (rows without an id keep what they hold)
+ *   sparse  rows [min(n, n_rows)]: the distinct ids in ascending order, grads
+ *           [min(n, n_rows)][d]: their gradients, count [1]: their number; what
+ *           lies behind it is left as it was
+ * ws_bytes >= stca_embed_grad_workspace_size(grad, n) (0 for invalid or unsupported
+ * arguments); an id behind the table sets stca_device_status. */
+typedef struct {
+  int32_t d;            /* a multiple of 8, at most 8192 */
+  int32_t dtype;        /* of dout */
+  int64_t n_rows;
+  float scale;
+} stca_embed_grad_t;
+typedef struct {
+  const int32_t* ids;   /* device [n] */
+  const void* dout;     /* [n][d] */
+  int64_t ld;
+  int64_t n;
+} stca_embed_part_t;
+#define STCA_EMBED_PARTS 4
+size_t stca_embed_grad_workspace_size(const stca_embed_grad_t* grad, int64_t n);
+stca_status_t stca_embed_grad_dense(const stca_embed_grad_t* grad, const stca_embed_part_t* parts, int32_t n_parts,
+                                    float* dtable, int64_t ld, int accumulate, void* ws, size_t ws_bytes,
+                                    hipStream_t stream);
+stca_status_t stca_embed_grad_sparse(const stca_embed_grad_t* grad, const stca_embed_part_t* parts, int32_t n_parts,
+                                     int32_t* rows, float* grads, int32_t* count, void* ws, size_t ws_bytes,
+                                     hipStream_t stream);
+
+/* ---- Norms before and after a block, its gate and its residual scale, for
+ * models that put their own blocks around the stand-alone attention.  For row i
+ * of x (the residual stream), block (what the block gave) and gate:
+ *   t = post(block) act(gate)      post: a norm with weight and bias, or nothing; act: sigmoid, silu or 1
+ *   h = x + scale layer_scale t    layer_scale [d], or 1
+ *   y = pre(h)                     the norm in front of the next block, or nothing
+ * norm(v) = weight (v - mean) / sqrt(var + eps) + bias (STCA_NORM_LAYER, biased
+ * variance), or weight v / sqrt(mean(v^2) + eps) + bias (STCA_NORM_RMS).  Weights
+ * and biases are fp32 [d], 4-byte aligned; NULL for ones and zeros.  Without a block
+ * h is x and y its norm.  Everything between the inputs and the outputs is fp32 and
+ * unrounded (y is the norm of h before its rounding).  Rows may have any finite
+ * values: squares that leave fp32 are taken smaller.  h and y may lie on x, block
+ * or gate, dx, dblock and dgate on those or on dh and dy, with the same stride. */
+typedef enum { STCA_NORM_RMS = 0, STCA_NORM_LAYER = 1 } stca_norm_kind_t;
+typedef enum { STCA_GATE_NONE = 0, STCA_GATE_SIGMOID = 1, STCA_GATE_SILU = 2 } stca_gate_t;
+typedef struct {
+  int32_t d;            /* a multiple of 8, at most 4096 */
+  int32_t dtype;        /* of rows and their gradients */
+  int32_t kind;         /* stca_norm_kind_t */
+  int32_t gate;         /* stca_gate_t; needs a block */
+  int32_t post;         /* nonzero: the block's rows are normed; needs a block */
+  int32_t pre;          /* nonzero: y is wanted; 0 needs a block */
+  float scale;          /* finite */
+  float eps;            /* finite, at least 1e-20 */
+} stca_norm_t;
+typedef struct {
+  const void* x;        /* [n][d] */
+  const void* block;    /* [n][d], nullable */
+  const void* gate;     /* [n][d], with a gate */
+  int64_t ldx, ldblock, ldgate;
+  const float* pre_w;
+  const float* pre_b;
+  const float* post_w;
+  const float* post_b;
+  const float* layer_scale;
+} stca_norm_in_t;
+/* Of f = sum <dh, h> + sum <dy, y>.  A NULL gradient is not computed.  The five of
+ * [d] are fp32 sums over the rows, joined in a fixed order. */
+typedef struct {
+  void* dx;
+  void* dblock;
+  void* dgate;
+  int64_t lddx, lddblock, lddgate;
+  float* dpre_w;
+  float* dpre_b;
+  float* dpost_w;
+  float* dpost_b;
+  float* dlayer_scale;
+} stca_norm_grads_t;
+/* h [n][d] (NULL without a block), y [n][d] (NULL without pre). */
+stca_status_t stca_norm_forward(const stca_norm_t* norm, const stca_norm_in_t* in, int64_t n, void* h, int64_t ldh,
+                                void* y, int64_t ldy, hipStream_t stream);
+/* dh nullable with pre (h is not used but for y); dy with pre.  Nothing is saved
+ * by a forward: the inputs are enough. */
+size_t stca_norm_workspace_size(const stca_norm_t* norm, int64_t n);
+stca_status_t stca_norm_backward(const stca_norm_t* norm, const stca_norm_in_t* in, int64_t n, const void* dh,
+                                 int64_t lddh, const void* dy, int64_t lddy, const stca_norm_grads_t* grads, void* ws,
+                                 size_t ws_bytes, hipStream_t stream);
+
+/* ---- The norm of many gradients together, and clipping:
+ *   norm = sqrt(sum over all elements g^2);  out = g min(1, max_norm / norm)
+ * Squares are added, and the factor is applied, in fp64: any finite gradient has
+ * its norm (written as fp32).  A norm that is not finite scales nothing: out = g,
+ * and the caller sees it.  A sparse gradient counts as far as *count rows of `row`
+ * elements; what lies behind is neither read nor written.  A result may lie on its
+ * own gradient (same type), and on nothing else of the list; the same result twice
+ * is refused. */
+typedef struct {
+  const void* g;          /* n elements, dense, aligned to an element */
+  void* out;              /* NULL: the gradient only counts */
+  int64_t n;              /* at most 2^40 */
+  int32_t dtype;
+  int32_t out_dtype;
+  const int32_t* count;   /* device [1], nullable: rows in use (0..n / row) */
+  int32_t row;            /* elements of a row, which divide n; with a count */
+} stca_grad_t;
+size_t stca_clip_workspace_size(int32_t n_grads);
+/* max_norm > 0; infinity only measures and copies.  norm: device [1], nullable. */
+stca_status_t stca_clip(const stca_grad_t* grads, int32_t n_grads, double max_norm, float* norm, void* ws,
+                        size_t ws_bytes, hipStream_t stream);
+
 /* Reads (synchronising on `stream`) the status the kernels recorded in `ws`
  * during the last call that used it: STCA_ERR_INVALID_ARG when the device
  * scheduler found bad offsets, else STCA_ERR_RANGE when the forward's target

@@ -27,7 +27,8 @@ FLAGS = [
 ]
 SOURCES = ["sched.hip", "generic.hip", "attn_mfma.hip", "fast.hip", "bwd_fused.hip", "bwd_update.hip",
            "reordered.hip", "gemm.hip", "gemm_ring.hip", "bwd_reordered.hip", "paper.hip", "attn_fwd.hip", "attn_bwd.hip",
-           "cache_attend.hip", "cache.hip", "api.cpp", "api_paper.cpp", "api_attn.cpp", "sl_batch.cpp", "noalloc.hip"]
+           "cache_attend.hip", "cache.hip", "embed.hip", "embed_grad.hip", "norm.hip", "clip.hip", "api.cpp", "api_paper.cpp",
+           "api_attn.cpp", "api_layers.cpp", "sl_batch.cpp", "noalloc.hip"]
 
 
 def _compile(src: str, extra) -> str:

@@ -1,0 +1,143 @@
+// The norm of many gradients together, and every one times min(1, max_norm /
+// norm).  Squares are added, and the factor is applied, in fp64, so no finite
+// gradient is too large or too small, and a result is rounded once.  Two launches
+// a list: sums of squares, one a workgroup, and the scaling, whose workgroups all
+// add up the same sums in the same order.  Bound by the bytes: every gradient is
+// read twice (the second time from the last-level cache as far as it holds them)
+// and written once.
+//
+// A list travels in the kernel's arguments, kGradsPerLaunch tensors a launch, so a
+// call needs no copy to the device and can be captured.
+#include "layer_ops.h"
+
+namespace stca {
+namespace layers {
+
+namespace {
+
+constexpr int kThreads = 256;
+
+__device__ __forceinline__ int64_t live_of(const Grad& t) {
+  if (!t.count) return t.n;
+  return min(t.n, static_cast<int64_t>(max(*t.count, 0)) * t.per);
+}
+
+__device__ __forceinline__ int tensor_of(const ClipArgs& a, int64_t piece) {
+  int lo = 0, hi = a.n_t;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) / 2;
+    if (a.t[mid].start <= piece) lo = mid;
+    else hi = mid;
+  }
+  return lo;
+}
+
+__device__ __forceinline__ double block_sum(double v, double* lds) {
+#pragma unroll
+  for (int o = 32; o > 0; o /= 2) v += __shfl_xor(v, o);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+  __syncthreads();
+  v = 0.;
+#pragma unroll
+  for (int w = 0; w < kThreads / 64; ++w) v += lds[w];
+  return v;
+}
+
+template <typename T>
+__device__ __forceinline__ double squares(const T* g, int64_t n) {
+  double v[4] = {};
+  const bool wide = (reinterpret_cast<uintptr_t>(g) & 15u) == 0;
+  int64_t done = 0;
+  if (wide) {
+    done = n / 8 * 8;
+#pragma unroll 4
+    for (int64_t i = 8 * threadIdx.x; i < done; i += 8 * kThreads) {
+      Oct<T> o;
+      o.load(g + i);
+      float x[8];
+      o.get(x);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e & 3] = fma(static_cast<double>(x[e]), static_cast<double>(x[e]), v[e & 3]);
+    }
+  }
+  for (int64_t i = done + threadIdx.x; i < n; i += kThreads) {
+    const double x = to_f32(g[i]);
+    v[0] = fma(x, x, v[0]);
+  }
+  return (v[0] + v[1]) + (v[2] + v[3]);
+}
+
+__global__ __launch_bounds__(kThreads) void sum_kernel(const ClipArgs a) {
+  __shared__ double lds[kThreads / 64];
+  double v = 0.;
+  for (int64_t piece = blockIdx.x; piece < a.pieces; piece += gridDim.x) {
+    const Grad& t = a.t[tensor_of(a, piece)];
+    const int64_t at = (piece - t.start) * kGradPiece, n = min<int64_t>(kGradPiece, live_of(t) - at);
+    if (n <= 0) continue;
+    v += t.flags & 1 ? squares(static_cast<const bf16_bits*>(t.g) + at, n) : squares(static_cast<const float*>(t.g) + at, n);
+  }
+  v = block_sum(v, lds);
+  if (threadIdx.x == 0) a.part[blockIdx.x] = v;
+}
+
+template <typename T, typename O>
+__device__ __forceinline__ void scale_piece(const T* g, O* out, int64_t n, double f) {
+  const bool wide = ((reinterpret_cast<uintptr_t>(g) | reinterpret_cast<uintptr_t>(out)) & 15u) == 0;
+  int64_t done = 0;
+  if (wide) {
+    done = n / 8 * 8;
+#pragma unroll 4
+    for (int64_t i = 8 * threadIdx.x; i < done; i += 8 * kThreads) {
+      Oct<T> o;
+      o.load(g + i);
+      float x[8];
+      o.get(x);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = static_cast<float>(x[e] * f);
+      Oct<O>::store(out + i, x);
+    }
+  }
+  for (int64_t i = done + threadIdx.x; i < n; i += kThreads) out[i] = from_f32<O>(static_cast<float>(to_f32(g[i]) * f));
+}
+
+__global__ __launch_bounds__(kThreads) void scale_kernel(const ClipArgs a) {
+  __shared__ double lds[kThreads / 64];
+  double v = 0.;
+#pragma unroll 4
+  for (int i = threadIdx.x; i < a.n_part; i += kThreads) v += a.part[i];
+  const double norm = sqrt(block_sum(v, lds));
+  // (a norm that is not finite leaves everything as it is)
+  const double f = norm > a.max_norm && norm < INFINITY ? a.max_norm / norm : 1.;
+  if (a.norm && blockIdx.x == 0 && threadIdx.x == 0) *a.norm = static_cast<float>(norm);
+  for (int64_t piece = blockIdx.x; piece < a.pieces; piece += gridDim.x) {
+    const Grad& t = a.t[tensor_of(a, piece)];
+    if (!t.out || (f == 1. && t.out == t.g)) continue;
+    const int64_t at = (piece - t.start) * kGradPiece, n = min<int64_t>(kGradPiece, live_of(t) - at);
+    if (n <= 0) continue;
+    if (t.flags & 1) {
+      const bf16_bits* g = static_cast<const bf16_bits*>(t.g) + at;
+      if (t.flags & 2) scale_piece(g, static_cast<bf16_bits*>(t.out) + at, n, f);
+      else scale_piece(g, static_cast<float*>(t.out) + at, n, f);
+    } else {
+      const float* g = static_cast<const float*>(t.g) + at;
+      if (t.flags & 2) scale_piece(g, static_cast<bf16_bits*>(t.out) + at, n, f);
+      else scale_piece(g, static_cast<float*>(t.out) + at, n, f);
+    }
+  }
+}
+
+}  // namespace
+
+hipError_t clip_sum(const ClipArgs& a, int grid, hipStream_t st) {
+  sum_kernel<<<grid, kThreads, 0, st>>>(a);
+  return hipGetLastError();
+}
+
+hipError_t clip_scale(const ClipArgs& a, int grid, hipStream_t st) {
+  scale_kernel<<<grid, kThreads, 0, st>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace layers
+}  // namespace stca

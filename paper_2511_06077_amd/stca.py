@@ -35,9 +35,15 @@ EXPORTED = ("stca_workspace_size", "stca_saved_size", "stca_saved_layout", "stca
             "stca_paper_launch_count", "stca_forward_paper_profiled", "stca_train_record_size", "stca_forward_train",
             "stca_backward_record", "stca_forward_noalloc", "stca_attn_workspace_size", "stca_attn_saved_size",
             "stca_attn_saved_layout", "stca_attn_forward", "stca_attn_backward", "stca_bias_edges",
-            "stca_cache_write", "stca_cache_read", "stca_cache_attn_workspace_size", "stca_cache_attn")
+            "stca_cache_write", "stca_cache_read", "stca_cache_attn_workspace_size", "stca_cache_attn",
+            "stca_embed_forward", "stca_embed_grad_workspace_size", "stca_embed_grad_dense", "stca_embed_grad_sparse",
+            "stca_norm_forward", "stca_norm_workspace_size", "stca_norm_backward", "stca_clip_workspace_size",
+            "stca_clip")
 STCA_CACHE_BF16, STCA_CACHE_INT8 = 0, 1
 CACHE_WS_BYTES = 256  # STCA_CACHE_WS_BYTES
+EMBED_FIELDS, EMBED_PARTS = 8, 4  # STCA_EMBED_FIELDS, STCA_EMBED_PARTS
+STCA_NORM_RMS, STCA_NORM_LAYER = 0, 1
+STCA_GATE_NONE, STCA_GATE_SIGMOID, STCA_GATE_SILU = 0, 1, 2
 NOALLOC_SCRATCH_BYTES = 256 << 20  # STCA_NOALLOC_SCRATCH_BYTES
 PAPER_WEIGHT_FIELDS = ("ffn_u", "ffn_v", "ffn_o", "wq", "wk", "wv", "wo", "wc", "wz", "z_u", "z_v", "z_o")
 
@@ -111,6 +117,49 @@ class stca_cache_batch_t(ctypes.Structure):
     _fields_ = [("n_requests", ctypes.c_int32), ("n_tgt", ctypes.c_int64), ("tgt_off", ctypes.c_void_p),
                 ("tgt_off_host", ctypes.c_void_p), ("lens", ctypes.c_void_p), ("max_len", ctypes.c_int32),
                 ("table", ctypes.c_void_p), ("table_ld", ctypes.c_int32)]
+
+
+class stca_embed_t(ctypes.Structure):
+    _fields_ = [("d", ctypes.c_int32), ("table_dtype", ctypes.c_int32), ("out_dtype", ctypes.c_int32),
+                ("scale", ctypes.c_float)]
+
+
+class stca_embed_field_t(ctypes.Structure):
+    _fields_ = [("table", ctypes.c_void_p), ("n_rows", ctypes.c_int64), ("ld", ctypes.c_int64),
+                ("ids", ctypes.c_void_p)]
+
+
+class stca_embed_grad_t(ctypes.Structure):
+    _fields_ = [("d", ctypes.c_int32), ("dtype", ctypes.c_int32), ("n_rows", ctypes.c_int64),
+                ("scale", ctypes.c_float)]
+
+
+class stca_embed_part_t(ctypes.Structure):
+    _fields_ = [("ids", ctypes.c_void_p), ("dout", ctypes.c_void_p), ("ld", ctypes.c_int64), ("n", ctypes.c_int64)]
+
+
+class stca_norm_t(ctypes.Structure):
+    _fields_ = [("d", ctypes.c_int32), ("dtype", ctypes.c_int32), ("kind", ctypes.c_int32), ("gate", ctypes.c_int32),
+                ("post", ctypes.c_int32), ("pre", ctypes.c_int32), ("scale", ctypes.c_float), ("eps", ctypes.c_float)]
+
+
+class stca_norm_in_t(ctypes.Structure):
+    _fields_ = [("x", ctypes.c_void_p), ("block", ctypes.c_void_p), ("gate", ctypes.c_void_p),
+                ("ldx", ctypes.c_int64), ("ldblock", ctypes.c_int64), ("ldgate", ctypes.c_int64),
+                ("pre_w", ctypes.c_void_p), ("pre_b", ctypes.c_void_p), ("post_w", ctypes.c_void_p),
+                ("post_b", ctypes.c_void_p), ("layer_scale", ctypes.c_void_p)]
+
+
+class stca_norm_grads_t(ctypes.Structure):
+    _fields_ = [("dx", ctypes.c_void_p), ("dblock", ctypes.c_void_p), ("dgate", ctypes.c_void_p),
+                ("lddx", ctypes.c_int64), ("lddblock", ctypes.c_int64), ("lddgate", ctypes.c_int64),
+                ("dpre_w", ctypes.c_void_p), ("dpre_b", ctypes.c_void_p), ("dpost_w", ctypes.c_void_p),
+                ("dpost_b", ctypes.c_void_p), ("dlayer_scale", ctypes.c_void_p)]
+
+
+class stca_grad_t(ctypes.Structure):
+    _fields_ = [("g", ctypes.c_void_p), ("out", ctypes.c_void_p), ("n", ctypes.c_int64), ("dtype", ctypes.c_int32),
+                ("out_dtype", ctypes.c_int32), ("count", ctypes.c_void_p), ("row", ctypes.c_int32)]
 
 
 class StcaError(RuntimeError):
@@ -227,7 +276,20 @@ def lib():
                  [P(stca_cache_t), P(stca_cache_rows_t), ctypes.c_int32, V, V, I64, I64, V, V, V]),
                 ("stca_cache_attn_workspace_size", SZ, [A, P(stca_cache_t), P(stca_cache_batch_t)]),
                 ("stca_cache_attn", ctypes.c_int,
-                 [A, P(stca_cache_t), P(stca_cache_batch_t), V, I64, V, V, V, V, SZ, V])):
+                 [A, P(stca_cache_t), P(stca_cache_batch_t), V, I64, V, V, V, V, SZ, V]),
+                ("stca_embed_forward", ctypes.c_int,
+                 [P(stca_embed_t), P(stca_embed_field_t), ctypes.c_int32, I64, V, I64, V, V]),
+                ("stca_embed_grad_workspace_size", SZ, [P(stca_embed_grad_t), I64]),
+                ("stca_embed_grad_dense", ctypes.c_int,
+                 [P(stca_embed_grad_t), P(stca_embed_part_t), ctypes.c_int32, V, I64, ctypes.c_int, V, SZ, V]),
+                ("stca_embed_grad_sparse", ctypes.c_int,
+                 [P(stca_embed_grad_t), P(stca_embed_part_t), ctypes.c_int32, V, V, V, V, SZ, V]),
+                ("stca_norm_forward", ctypes.c_int, [P(stca_norm_t), P(stca_norm_in_t), I64, V, I64, V, I64, V]),
+                ("stca_norm_workspace_size", SZ, [P(stca_norm_t), I64]),
+                ("stca_norm_backward", ctypes.c_int,
+                 [P(stca_norm_t), P(stca_norm_in_t), I64, V, I64, V, I64, P(stca_norm_grads_t), V, SZ, V]),
+                ("stca_clip_workspace_size", SZ, [ctypes.c_int32]),
+                ("stca_clip", ctypes.c_int, [P(stca_grad_t), ctypes.c_int32, ctypes.c_double, V, V, SZ, V])):
             getattr(L, name).restype, getattr(L, name).argtypes = res, args
         _lib = L
     return _lib
@@ -511,6 +573,91 @@ def stca_cache_attn(a, c, b, q, ldq: int, tgt_pos, bias, out, ws, ws_bytes: int,
                     check: bool = True) -> int:
     return _checked("stca_cache_attn", check, ctypes.byref(a), ctypes.byref(c), ctypes.byref(b), _ptr(q), ldq,
                     _ptr(tgt_pos), _ptr(bias), _ptr(out), _ptr(ws), int(ws_bytes), _ptr(stream))
+
+
+# ---- rows from ids, norms around a block, the norm of all gradients
+def embed(d: int, table_dtype: int, out_dtype: int, scale: float = 1.0) -> stca_embed_t:
+    return stca_embed_t(d, table_dtype, out_dtype, scale)
+
+
+def embed_fields(fields):
+    """fields: (table, n_rows, row stride or 0, ids) each."""
+    return (stca_embed_field_t * len(fields))(*((_ptr(t), n, ld, _ptr(ids)) for t, n, ld, ids in fields))
+
+
+def embed_grad(d: int, dtype: int, n_rows: int, scale: float = 1.0) -> stca_embed_grad_t:
+    return stca_embed_grad_t(d, dtype, n_rows, scale)
+
+
+def embed_parts(parts):
+    """parts: (ids, dout, row stride or 0, rows) each."""
+    return (stca_embed_part_t * len(parts))(*((_ptr(i), _ptr(g), ld, n) for i, g, ld, n in parts))
+
+
+def norm(d: int, dtype: int, kind: int, gate: int = STCA_GATE_NONE, post: bool = False, pre: bool = True,
+         scale: float = 1.0, eps: float = 1e-6) -> stca_norm_t:
+    return stca_norm_t(d, dtype, kind, gate, int(post), int(pre), scale, eps)
+
+
+def norm_in(x, block=None, gate=None, ldx: int = 0, ldblock: int = 0, ldgate: int = 0, pre_w=None, pre_b=None,
+            post_w=None, post_b=None, layer_scale=None) -> stca_norm_in_t:
+    return stca_norm_in_t(_ptr(x), _ptr(block), _ptr(gate), ldx, ldblock, ldgate, _ptr(pre_w), _ptr(pre_b),
+                          _ptr(post_w), _ptr(post_b), _ptr(layer_scale))
+
+
+def norm_grads(dx=None, dblock=None, dgate=None, lddx: int = 0, lddblock: int = 0, lddgate: int = 0, dpre_w=None,
+               dpre_b=None, dpost_w=None, dpost_b=None, dlayer_scale=None) -> stca_norm_grads_t:
+    return stca_norm_grads_t(_ptr(dx), _ptr(dblock), _ptr(dgate), lddx, lddblock, lddgate, _ptr(dpre_w),
+                             _ptr(dpre_b), _ptr(dpost_w), _ptr(dpost_b), _ptr(dlayer_scale))
+
+
+def grads(items):
+    """items: (g, out, elements, dtype, dtype of out, count, elements of a row) each."""
+    return (stca_grad_t * len(items))(*((_ptr(g), _ptr(o), n, t, u, _ptr(c), r) for g, o, n, t, u, c, r in items))
+
+
+def stca_embed_forward(e, fields, n: int, out, ldo: int = 0, ws=None, stream=None, check: bool = True) -> int:
+    return _checked("stca_embed_forward", check, ctypes.byref(e), fields, len(fields), n, _ptr(out), ldo, _ptr(ws),
+                    _ptr(stream))
+
+
+def stca_embed_grad_workspace_size(g, n: int) -> int:
+    return lib().stca_embed_grad_workspace_size(ctypes.byref(g), n)
+
+
+def stca_embed_grad_dense(g, parts, dtable, ld: int, accumulate: bool, ws, ws_bytes: int, stream=None,
+                          check: bool = True) -> int:
+    return _checked("stca_embed_grad_dense", check, ctypes.byref(g), parts, len(parts), _ptr(dtable), ld,
+                    int(accumulate), _ptr(ws), int(ws_bytes), _ptr(stream))
+
+
+def stca_embed_grad_sparse(g, parts, rows, values, count, ws, ws_bytes: int, stream=None, check: bool = True) -> int:
+    return _checked("stca_embed_grad_sparse", check, ctypes.byref(g), parts, len(parts), _ptr(rows), _ptr(values),
+                    _ptr(count), _ptr(ws), int(ws_bytes), _ptr(stream))
+
+
+def stca_norm_forward(m, given, n: int, h, ldh: int, y, ldy: int, stream=None, check: bool = True) -> int:
+    return _checked("stca_norm_forward", check, ctypes.byref(m), ctypes.byref(given), n, _ptr(h), ldh, _ptr(y), ldy,
+                    _ptr(stream))
+
+
+def stca_norm_workspace_size(m, n: int) -> int:
+    return lib().stca_norm_workspace_size(ctypes.byref(m), n)
+
+
+def stca_norm_backward(m, given, n: int, dh, lddh: int, dy, lddy: int, out, ws, ws_bytes: int, stream=None,
+                       check: bool = True) -> int:
+    return _checked("stca_norm_backward", check, ctypes.byref(m), ctypes.byref(given), n, _ptr(dh), lddh, _ptr(dy),
+                    lddy, ctypes.byref(out), _ptr(ws), int(ws_bytes), _ptr(stream))
+
+
+def stca_clip_workspace_size(n_grads: int) -> int:
+    return lib().stca_clip_workspace_size(n_grads)
+
+
+def stca_clip(items, max_norm: float, norm_out, ws, ws_bytes: int, stream=None, check: bool = True) -> int:
+    return _checked("stca_clip", check, items, len(items), max_norm, _ptr(norm_out), _ptr(ws), int(ws_bytes),
+                    _ptr(stream))
 
 
 class HipEvents:

@@ -1,0 +1,208 @@
+"""Norms around a block on the GPU against the float64 oracle: every form, odd
+widths, rows far from zero and of the largest values, strides, rows in place."""
+import numpy as np
+import pytest
+
+from layers_common import rounded, strided, worst
+from oracle import layers_oracle as O
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def torch():
+    import torch as t
+    assert t.cuda.is_available(), "GPU tests need a GPU"
+    return t
+
+
+FORMS = {
+    "pre": dict(),
+    "pre_plain": dict(pre=()),
+    "block": dict(block=True),
+    "block_only": dict(block=True, pre=False),
+    "sigmoid": dict(block=True, gate="sigmoid", post=("w",), ls=True),
+    "silu": dict(block=True, gate="silu", post=("w", "b"), pre=("w", "b"), ls=True),
+    "gate_only": dict(block=True, gate="silu", pre=False),
+    "post_plain": dict(block=True, post=(), pre=(), ls=True),
+    "bias_only": dict(block=True, post=("", "b"), pre=("", "b")),
+}
+
+
+def vectors(torch, rng, d, names):
+    """((tensors), (float64)) of a norm's parameters"""
+    got = [None if not n else rounded(torch, (1.0 if n == "w" else 0.0) + 0.3 * rng.standard_normal(d), "f32") for n in names]
+    return tuple(None if g is None else g[0] for g in got), [None if g is None else g[1] for g in got] + [None] * (2 - len(got))
+
+
+def build(torch, n, d, dtype, kind, form, seed=0, spread=None, eps=1e-6):
+    """Tensors and arguments of a call, and the oracle's results for it."""
+    rng = np.random.default_rng([n, d, seed])
+    f = dict(FORMS[form])
+    block, gate = f.get("block", False), f.get("gate")
+    t, a = {}, {}
+    for name in ["x", "dy", "dh"] + (["block"] if block else []) + (["gate"] if gate else []):
+        v = rng.standard_normal((n, d))
+        if spread is not None and name in ("x", "block"):
+            v = spread(rng, v)
+        t[name], a[name] = rounded(torch, v, dtype)
+    given, want = {}, {}
+    pre = f.get("pre", ("w",))
+    if pre is False:
+        given["pre"] = want["pre"] = False
+        t["dy"] = a["dy"] = None
+    else:
+        given["pre"], want["pre"] = vectors(torch, rng, d, pre)
+    if f.get("post") is not None:
+        given["post"], want["post"] = vectors(torch, rng, d, f["post"])
+    if f.get("ls"):
+        given["layer_scale"], want["ls"] = rounded(torch, 0.5 + 0.2 * rng.standard_normal(d), "f32")
+    scale = float(np.float32(0.7))
+    with np.errstate(over="ignore"):
+        ref = O.norm(a["x"], kind, float(np.float32(eps)), scale, a.get("block"), a.get("gate"), gate, dy=a["dy"], dh=a["dh"], **want)
+    from paper_2511_06077_amd.layers import BlockNorm
+    plan = BlockNorm(d, kind=kind, gate=gate, scale=scale, eps=eps, dtype=t["x"].dtype, backward=True)
+    for name in ("block", "gate"):
+        if name in t:
+            given[name] = t[name]
+    return plan, t, given, ref
+
+
+def check(got, ref, dtype, block):
+    h, y, g = got
+    e = {}
+    if block:
+        e["h"] = worst(h, ref["h"], ref["h_err"], dtype)
+    if y is not None:
+        e["y"] = worst(y, ref["y"], ref["y_err"], dtype)
+    for name, v, kind in (("dx", g.x, dtype), ("dblock", g.block, dtype), ("dgate", g.gate, dtype), ("pre_w", g.pre[0], "f32"),
+                          ("pre_b", g.pre[1], "f32"), ("post_w", g.post[0], "f32"), ("post_b", g.post[1], "f32"),
+                          ("ls", g.layer_scale, "f32")):
+        if v is not None:
+            e[name] = worst(v, ref[name], ref[name + "_err"], kind)
+    assert max(e.values()) <= 1.0, e
+
+
+def both(plan, t, given):
+    h, y = plan.forward(t["x"], **given)
+    return h, y, plan.backward(t["dy"], t["x"], dh=t["dh"], **given)
+
+
+@pytest.mark.parametrize("kind", ["rms", "layer"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("form", list(FORMS))
+@pytest.mark.parametrize("n,d", [(1, 256), (5, 8), (33, 72), (9, 264), (7, 1000), (3, 2000), (2, 4096)])
+def test_forms(torch, n, d, form, dtype, kind):
+    plan, t, given, ref = build(torch, n, d, dtype, kind, form)
+    check(both(plan, t, given), ref, dtype, "block" in given)
+
+
+@pytest.mark.parametrize("n,d", [(20000, 32), (9001, 64), (5000, 128), (9000, 256), (3000, 512), (2500, 1024)])
+def test_many_rows(torch, n, d):
+    """More rows than one round of the workgroups has, and the sums over them."""
+    plan, t, given, ref = build(torch, n, d, "bf16", "layer", "silu")
+    got = both(plan, t, given)
+    check(got, ref, "bf16", True)
+    again = plan.backward(t["dy"], t["x"], dh=t["dh"], **given)
+    for a, b in ((got[2].x, again.x), (got[2].pre[0], again.pre[0]), (got[2].post[1], again.post[1]),
+                 (got[2].layer_scale, again.layer_scale)):
+        assert torch.equal(a, b)
+
+
+SPREADS = {
+    "far_from_zero": lambda rng, v: 1000.0 + v,
+    "one_large": lambda rng, v: v * np.where(np.arange(v.shape[1]) == 3, 1e4, 1.0),
+    "scales_by_row": lambda rng, v: v * 2.0 ** rng.integers(-40, 40, size=(len(v), 1)),
+    "squares_leave_fp32": lambda rng, v: v * 2.0 ** np.where(np.arange(len(v)) % 3 == 0, 100.0, 0.0)[:, None],
+    "tiny": lambda rng, v: v * 1e-30,
+    "zeros": lambda rng, v: v * (np.arange(len(v)) % 2)[:, None],
+}
+
+
+@pytest.mark.parametrize("kind", ["rms", "layer"])
+@pytest.mark.parametrize("name", list(SPREADS))
+@pytest.mark.parametrize("d", [64, 264, 1000])
+def test_values(torch, d, name, kind):
+    for form in ("pre", "sigmoid"):
+        plan, t, given, ref = build(torch, 13, d, "f32", kind, form, spread=SPREADS[name], seed=3)
+        check(both(plan, t, given), ref, "f32", "block" in given)
+
+
+@pytest.mark.parametrize("d", [64, 264, 1000])
+def test_odd_values_stay_in_their_rows(torch, d):
+    for kind in ("rms", "layer"):
+        plan, t, given, ref = build(torch, 11, d, "f32", kind, "sigmoid", seed=5)
+        clean = both(plan, t, given)
+        t["x"][3, 1], given["block"][6, 2], given["gate"][8, 0] = float("nan"), float("inf"), float("nan")
+        h, y, g = both(plan, t, given)
+        for a, b in ((h, clean[0]), (y, clean[1]), (g.x, clean[2].x), (g.block, clean[2].block), (g.gate, clean[2].gate)):
+            keep = [i for i in range(11) if i not in (3, 6, 8)]
+            assert torch.equal(a[keep], b[keep])
+        for row in (3, 6, 8):
+            assert torch.isnan(y[row]).any()
+
+
+def test_strides_and_no_gradient_of_h(torch):
+    plan, t, given, _ = build(torch, 70, 200, "bf16", "layer", "silu")
+    want = both(plan, t, given)
+    loose = {k: strided(torch, v) if k in ("block", "gate") else v for k, v in given.items()}
+    got = both(plan, {k: strided(torch, v) for k, v in t.items()}, loose)
+    for a, b in zip(got[2][:3], want[2][:3]):
+        assert torch.equal(a, b)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    none = plan.backward(t["dy"], t["x"], dh=None, **given)
+    zero = plan.backward(t["dy"], t["x"], dh=torch.zeros_like(t["x"]), **given)
+    assert torch.equal(none.x, zero.x) and torch.equal(none.block, zero.block) and torch.equal(none.layer_scale, zero.layer_scale)
+
+
+def test_results_on_their_inputs(torch):
+    """h on x, y on block; dx on dh, dblock on dy, dgate on gate, with wider rows around."""
+    from paper_2511_06077_amd import stca
+    for n, d in ((2500, 64), (300, 1000)):
+        plan, t, given, _ = build(torch, n, d, "bf16", "rms", "sigmoid")
+        h, y, g = both(plan, t, given)
+        m = plan._forms[True, True]
+        fresh = {k: v.clone() for k, v in {**t, **{k: given[k] for k in ("block", "gate")}}.items()}
+        inp = stca.norm_in(fresh["x"], fresh["block"], fresh["gate"], pre_w=given["pre"][0], post_w=given["post"][0],
+                           layer_scale=given["layer_scale"])
+        s = plan.stream()
+        stca.stca_norm_forward(m, inp, n, fresh["x"], 0, fresh["block"], 0, s)
+        assert torch.equal(fresh["x"], h) and torch.equal(fresh["block"], y)
+        fresh["x"].copy_(t["x"]), fresh["block"].copy_(given["block"])
+        stca.stca_norm_backward(m, inp, n, fresh["dh"], 0, fresh["dy"], 0,
+                                stca.norm_grads(fresh["dh"], fresh["dy"], fresh["gate"]), plan.ws, plan.ws_bytes, s)
+        assert torch.equal(fresh["dh"], g.x) and torch.equal(fresh["dy"], g.block) and torch.equal(fresh["gate"], g.gate)
+
+
+def test_no_rows(torch):
+    from paper_2511_06077_amd.layers import BlockNorm
+    plan = BlockNorm(64, gate="silu", backward=True, dtype=torch.float32)
+    none, w = torch.empty((0, 64), device="cuda"), torch.ones(64, device="cuda")
+    h, y = plan.forward(none, block=none, gate=none, post=(w,), pre=(w,))
+    assert h.shape == y.shape == (0, 64)
+    g = plan.backward(none, none, dh=none, block=none, gate=none, post=(w, w), pre=(w,), layer_scale=w)
+    assert g.x.shape == (0, 64) and all(bool((v == 0).all()) for v in (g.pre[0], *g.post, g.layer_scale))
+
+
+def test_gradients_against_differences(torch):
+    """fp32 central differences of the forward at some coordinates of every input."""
+    plan, t, given, ref = build(torch, 3, 24, "f32", "layer", "silu", seed=9)
+    g = plan.backward(t["dy"], t["x"], dh=t["dh"], **given)
+    def f():
+        h, y = plan.forward(t["x"], **given)
+        return float((h.double() * t["dh"].double()).sum() + (y.double() * t["dy"].double()).sum())
+    size = 3 * 24 * 4.0  # of f's terms: each at most a few, off by some 40 U
+    for where, grad in ((t["x"], g.x), (given["block"], g.block), (given["gate"], g.gate), (given["pre"][0], g.pre[0]),
+                        (given["pre"][1], g.pre[1]), (given["post"][0], g.post[0]), (given["post"][1], g.post[1]),
+                        (given["layer_scale"], g.layer_scale)):
+        flat, gf = where.view(-1), grad.reshape(-1)
+        for i in (0, 7, flat.numel() - 1):
+            keep, step = float(flat[i]), 2.0 ** -7
+            flat[i] = keep + step
+            up, hi = f(), float(flat[i])
+            flat[i] = keep - step
+            down, lo = f(), float(flat[i])
+            flat[i] = keep
+            # rounding of f over the step, and the third derivative times step^2 / 6
+            bound = 80 * O.U * size / (hi - lo) + step * step * 20
+            assert abs((up - down) / (hi - lo) - float(gf[i])) <= bound
