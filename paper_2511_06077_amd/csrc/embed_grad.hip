@@ -374,8 +374,10 @@ __global__ __launch_bounds__(kThreads) void sum_kernel(const EmbedGradArgs a, co
         }
         base += total;
       }
-      row[i] = r;
-      src[i] = r >= 0 ? static_cast<int>(tok) : -1;
+      if (i < kTokens) {  // (a workgroup of wide rows has fewer tokens than threads)
+        row[i] = r;
+        src[i] = r >= 0 ? static_cast<int>(tok) : -1;
+      }
     }
     if (threadIdx.x == 0) {
       // rows of the neighbours on both sides, as far as they are those of the outermost tokens

@@ -95,6 +95,9 @@ GRADS = {
     "narrow": (np.random.default_rng(6).integers(0, 700, 30000), 700, 8),
     "wide": (np.random.default_rng(7).integers(0, 40, 900), 40, 1000),
     "widest": (np.random.default_rng(8).integers(0, 9, 300), 9, 8192),
+    # more workgroups than the card holds at once, of fewer tokens than threads
+    "many_workgroups": (np.random.default_rng(10).zipf(1.2, 300000) % 100000, 100000, 136),
+    "many_workgroups_256": (np.random.default_rng(11).integers(-1, 30000, 270000), 30000, 256),
     "digits_255": (np.random.default_rng(9).integers(0, 255, 5000), 255, 16),
     "digits_256": (np.random.default_rng(9).integers(0, 256, 5000), 256, 16),
     "digits_65536": (np.random.default_rng(9).integers(0, 65536, 9000), 65536, 16),
