@@ -41,7 +41,7 @@ stca_status_t check_grad(const stca_embed_grad_t* g, int64_t n) {
 }
 
 struct GradLayout {
-  size_t hdr, counts, bad, pairs[2], head_off, head_sum, slot[2], slot_val[2], total;
+  size_t hdr, counts, bad, pairs[2], tokens, head_sum, slot[2], slot_val[2], total;
 };
 
 GradLayout grad_layout(const stca_embed_grad_t* g, int64_t n) {
@@ -51,12 +51,12 @@ GradLayout grad_layout(const stca_embed_grad_t* g, int64_t n) {
   l.hdr = m.take(sizeof(WsHeader));
   if (n > 0) {
     if (!p.small) {
-      l.counts = m.take(4 * static_cast<size_t>(p.blocks) * 256);
+      l.counts = m.take(4 * 256 * 256);
       l.bad = m.take(4 * static_cast<size_t>(p.blocks));
     }
-    for (int i = 0; i < 2; ++i) l.pairs[i] = m.take(i < p.passes ? 8 * static_cast<size_t>(n) : 0);
-    l.head_off = m.take(p.head_blocks ? 4 * static_cast<size_t>(p.groups) : 0);
-    l.head_sum = m.take(4 * static_cast<size_t>(p.head_blocks));
+    for (int i = 0; i < 2; ++i) l.pairs[i] = m.take(!p.small && i < p.passes ? 8 * static_cast<size_t>(n) : 0);
+    l.tokens = m.take(8 * static_cast<size_t>(n));
+    l.head_sum = m.take(4 * static_cast<size_t>(p.heads));
     const int64_t groups[2] = {p.groups > 1 ? p.groups : 0, p.groups > 1 && p.next_groups > 1 ? p.next_groups : 0};
     for (int i = 0; i < 2; ++i) {
       l.slot[i] = m.take(16 * static_cast<size_t>(groups[i]));
@@ -95,7 +95,7 @@ stca_status_t embed_grad_call(const stca_embed_grad_t* g, const stca_embed_part_
   a->hdr = at<WsHeader>(ws, l.hdr);
   a->counts = at<int32_t>(ws, l.counts);
   a->bad = at<int32_t>(ws, l.bad);
-  a->head_off = at<int32_t>(ws, l.head_off);
+  a->tokens = at<int2>(ws, l.tokens);
   a->head_sum = at<int32_t>(ws, l.head_sum);
   for (int i = 0; i < 2; ++i) {
     a->pairs[i] = at<uint64_t>(ws, l.pairs[i]);

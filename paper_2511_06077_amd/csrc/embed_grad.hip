@@ -17,13 +17,15 @@ namespace layers {
 
 namespace {
 
-constexpr int kThreads = 512;
+constexpr int kThreads = 1024;   // of a sorting workgroup (512: 15 us a pass over 528384 tokens, 1024: 13)
 constexpr int kWaves = kThreads / 64;
 constexpr int kDigits = 256;
 constexpr int kMaxBlocks = 256;  // workgroups of a sort
-constexpr int kItems = 8;        // tokens a thread of a sort's tile
+constexpr int kItems = 4096 / kThreads;        // tokens a thread of a sort's tile
 constexpr int kSmall = kThreads * kItems;
-constexpr int kTeamTokens = 32;
+constexpr int kFirstThreads = 256;  // of a summing workgroup of the first level
+constexpr int kUpThreads = 1024;    // ... of the levels above: as few of them as may be
+constexpr int kNone = -2;        // no row of the result (-1: the last one of the numbering before)
 
 __device__ __forceinline__ int part_of(const EmbedGradArgs& a, int64_t i) {
   return (i >= a.end[0]) + (i >= a.end[1]) + (i >= a.end[2]);
@@ -56,7 +58,20 @@ __device__ __forceinline__ int lanes_below(uint64_t m) {
   return __builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(m >> 32), __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(m), 0));
 }
 
-// Exclusive prefix sums over the kThreads threads (a barrier before and after).
+// Sum over a wave, in every lane.
+__device__ __forceinline__ int wave_sum(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0xb1, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x4e, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x141, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x140, 0xf, 0xf, true);
+  const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+  x = r[0] + r[1];
+  const auto q = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+  return q[0] + q[1];
+}
+
+// Exclusive prefix sums over a workgroup's threads (a barrier before and after).
+template <int kWaves>
 __device__ __forceinline__ int block_prefix(int v, int* waves, int& total) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   int x = v;
@@ -93,31 +108,33 @@ __global__ __launch_bounds__(kThreads) void count_kernel(const EmbedGradArgs a, 
     atomicAdd(&cnt[id >> shift & mask], 1);
   }
   const int any = __syncthreads_or(bad);
-  for (int i = threadIdx.x; i < kDigits; i += kThreads) a.counts[blockIdx.x * kDigits + i] = cnt[i];
+  for (int i = threadIdx.x; i <= mask; i += kThreads) a.counts[i * kMaxBlocks + blockIdx.x] = cnt[i];
   if (pass == 0 && threadIdx.x == 0) a.bad[blockIdx.x] = any;
 }
 
 struct SortLds {
-  int cnt[kWaves][kDigits];  // of a wave's tokens of the tile, then where its first one goes
-  int base[kDigits];         // where the next token of a digit goes
+  int cnt[kWaves][kDigits];  // of a wave's tokens of the tile, then of the waves' before it
+  int start[kDigits];        // of a digit in the sorted tile
   int waves[kWaves];
+  uint64_t buf[kSmall];      // the sorted tile
 };
 
-// Ranks a tile's tokens by their digits, in order: `item`(it) gives the wave's
-// it-th 64 tokens, `put`(it, place) takes each token's place.
-template <typename Digit, typename Put>
-__device__ __forceinline__ void place_tile(SortLds& s, int items, int bits, Digit digit_of, Put put) {
-  const int wave = threadIdx.x >> 6;
+// Sorts a tile of up to kSmall tokens by a digit, in order, into s.buf: get(it, pair)
+// gives the wave's it-th 64 tokens.  Returns how many have the digit that is the
+// thread's number; s.start says where they begin.
+template <typename Get>
+__device__ __forceinline__ int sort_tile(SortLds& s, int items, int shift, int bits, Get get) {
+  const int wave = threadIdx.x >> 6, mask = (1 << bits) - 1;
   for (int i = threadIdx.x; i < kWaves * kDigits; i += kThreads) (&s.cnt[0][0])[i] = 0;
   __syncthreads();
-  int rank[kItems];
-  uint32_t digit[kItems];
+  uint64_t pair[kItems];
+  int rank[kItems], digit[kItems];
   bool valid[kItems];
 #pragma unroll
   for (int it = 0; it < kItems; ++it) {
-    valid[it] = false;
-    digit[it] = 0;
-    if (it < items) valid[it] = digit_of(it, digit[it]);
+    pair[it] = 0;
+    valid[it] = it < items && get(it, pair[it]);
+    digit[it] = static_cast<int>(static_cast<uint32_t>(pair[it] >> 32) >> shift) & mask;
   }
 #pragma unroll
   for (int it = 0; it < kItems; ++it) {
@@ -130,45 +147,70 @@ __device__ __forceinline__ void place_tile(SortLds& s, int items, int bits, Digi
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   }
   __syncthreads();
-  for (int d = threadIdx.x; d < kDigits; d += kThreads) {
-    int at = s.base[d];
+  const int d = threadIdx.x;
+  int all = 0, total;
+  if (d < kDigits) {
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) {
       const int c = s.cnt[w][d];
-      s.cnt[w][d] = at;
-      at += c;
+      s.cnt[w][d] = all;
+      all += c;
     }
-    s.base[d] = at;
   }
+  const int at = block_prefix<kWaves>(all, s.waves, total);
+  if (d < kDigits) s.start[d] = at;
   __syncthreads();
 #pragma unroll
   for (int it = 0; it < kItems; ++it)
-    if (it < items && valid[it]) put(it, s.cnt[wave][digit[it]] + rank[it]);
+    if (valid[it]) s.buf[s.start[digit[it]] + s.cnt[wave][digit[it]] + rank[it]] = pair[it];
   __syncthreads();
+  return all;
 }
 
 __global__ __launch_bounds__(kThreads) void scatter_kernel(const EmbedGradArgs a, const EmbedGradPlan p, int pass) {
   __shared__ SortLds s;
-  __shared__ int part[2][kThreads];  // totals of half of the blocks, and of those before this one
+  __shared__ int base[kDigits];    // where the next token of a digit goes
+  __shared__ int before[kDigits];  // of the digit, in the workgroups before this one
   const int shift = pass * p.bits, mask = (1 << p.bits) - 1;
   {
-    // threads t and t + 256 add digit t's counts of every other block
-    const int d = threadIdx.x % kDigits, half = threadIdx.x / kDigits;
-    int all = 0, before = 0;
-#pragma unroll 8
-    for (int b = half; b < p.blocks; b += kThreads / kDigits) {
-      const int c = a.counts[b * kDigits + d];
-      all += c;
-      before += b < static_cast<int>(blockIdx.x) ? c : 0;
+    // a wave takes every kWaves-th digit: its counts in all workgroups are one load,
+    // four a lane, and all of them are on their way together
+    constexpr int kEach = kDigits / kWaves;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, b = 4 * lane;
+    int4 c[kEach];
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+      const int d = wave + k * kWaves;
+      c[k] = make_int4(0, 0, 0, 0);
+      if (d <= mask && b < p.blocks) c[k] = *reinterpret_cast<const int4*>(a.counts + d * kMaxBlocks + b);
     }
-    part[0][threadIdx.x] = all;
-    part[1][threadIdx.x] = before;
+    const int me = static_cast<int>(blockIdx.x);
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+      const int d = wave + k * kWaves;
+      if (d > mask) {
+        if (lane == 0) base[d] = 0;
+        continue;
+      }
+      const int v[4] = {c[k].x, c[k].y, c[k].z, c[k].w};
+      int all = 0, low = 0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        all += b + e < p.blocks ? v[e] : 0;
+        low += b + e < min(me, p.blocks) ? v[e] : 0;
+      }
+      all = wave_sum(all);
+      low = wave_sum(low);
+      if (lane == 0) {
+        base[d] = all;
+        before[d] = low;
+      }
+    }
     __syncthreads();
     int total;
     const int t = threadIdx.x;
-    const int mine = t < kDigits ? part[0][t] + part[0][t + kDigits] : 0;
-    const int at = block_prefix(mine, s.waves, total);
-    if (t < kDigits) s.base[t] = at + part[1][t] + part[1][t + kDigits];
+    const int at = block_prefix<kWaves>(t < kDigits ? base[t] : 0, s.waves, total);
+    if (t < kDigits) base[t] = at + before[t];
   }
   if (pass == 0 && blockIdx.x == 0 && a.hdr) {
     int bad = 0;
@@ -187,94 +229,88 @@ __global__ __launch_bounds__(kThreads) void scatter_kernel(const EmbedGradArgs a
   for (int64_t tile = t0; tile < t1; tile += kSmall) {
     const int left = static_cast<int>(min<int64_t>(kSmall, t1 - tile));
     const int items = (left + kThreads - 1) / kThreads;  // of 64 tokens, a wave
-    uint64_t pair[kItems];
-    place_tile(
-        s, items, p.bits,
-        [&](int it, uint32_t& digit) {
-          const int64_t i = tile + wave * (items * 64) + it * 64 + lane;
-          if (i >= t1) return false;
-          bool bad = false;
-          pair[it] = from ? from[i] : pair_of(id_of(a, i, bad), i);
-          digit = static_cast<uint32_t>(pair[it] >> 32) >> shift & mask;
-          return true;
-        },
-        [&](int it, int place) { to[place] = pair[it]; });
+    const int all = sort_tile(s, items, shift, p.bits, [&](int it, uint64_t& pair) {
+      const int64_t i = tile + wave * (items * 64) + it * 64 + lane;
+      bool bad = false;
+      if (i < t1) pair = from ? from[i] : pair_of(id_of(a, i, bad), i);
+      return i < t1;
+    });
+    // neighbours in the sorted tile go to neighbouring places (stored one by one from
+    // where they were read, 64 places a store, the pass took 15 us for 528384 tokens)
+    for (int i = threadIdx.x; i < left; i += kThreads) {
+      const uint64_t pair = s.buf[i];
+      const int d = static_cast<int>(static_cast<uint32_t>(pair >> 32) >> shift) & mask;
+      to[base[d] + i - s.start[d]] = pair;
+    }
+    __syncthreads();
+    if (threadIdx.x < kDigits) base[threadIdx.x] += all;
   }
 }
 
 // All passes of up to kSmall tokens by one workgroup, in LDS.
 __global__ __launch_bounds__(kThreads) void sort_small_kernel(const EmbedGradArgs a, const EmbedGradPlan p) {
   __shared__ SortLds s;
-  __shared__ uint64_t buf[kSmall];  // (a pass holds it in registers before it writes)
   const int n = static_cast<int>(a.n), items = (n + kThreads - 1) / kThreads;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, mask = (1 << p.bits) - 1;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   bool bad = false;
-  for (int i = threadIdx.x; i < n; i += kThreads) buf[i] = pair_of(id_of(a, i, bad), i);
+  for (int pass = 0; pass < p.passes; ++pass)  // (a pass holds its tokens in registers before it writes them)
+    sort_tile(s, items, pass * p.bits, p.bits, [&](int it, uint64_t& pair) {
+      const int i = wave * (items * 64) + it * 64 + lane;
+      if (i < n) pair = pass ? s.buf[i] : pair_of(id_of(a, i, bad), i);
+      return i < n;
+    });
   const int any = __syncthreads_or(bad);
   if (threadIdx.x == 0 && a.hdr) {
     a.hdr->status = any ? STCA_ERR_INVALID_ARG : STCA_OK;
     a.hdr->range = 0;
   }
-  for (int pass = 0; pass < p.passes; ++pass) {
-    const int shift = pass * p.bits;
-    for (int i = threadIdx.x; i < kDigits; i += kThreads) s.base[i] = 0;
-    __syncthreads();
-    for (int i = threadIdx.x; i < n; i += kThreads) atomicAdd(&s.base[static_cast<uint32_t>(buf[i] >> 32) >> shift & mask], 1);
-    __syncthreads();
-    int total;
-    const int t = threadIdx.x;
-    const int at = block_prefix(t < kDigits ? s.base[t] : 0, s.waves, total);
-    if (t < kDigits) s.base[t] = at;
-    __syncthreads();
-    uint64_t pair[kItems];
-    place_tile(
-        s, items, p.bits,
-        [&](int it, uint32_t& digit) {
-          const int i = wave * (items * 64) + it * 64 + lane;
-          if (i >= n) return false;
-          pair[it] = buf[i];
-          digit = static_cast<uint32_t>(pair[it] >> 32) >> shift & mask;
-          return true;
-        },
-        [&](int it, int place) { buf[place] = pair[it]; });
+  // the rows of the result, and where there are distinct ids their list
+  const bool sparse = a.dtable == nullptr;
+  int base = 0;
+  for (int i0 = 0; i0 < n; i0 += kThreads) {
+    const int i = i0 + threadIdx.x;
+    const uint32_t key = i < n ? static_cast<uint32_t>(s.buf[i] >> 32) : a.n_rows;
+    int row = key < a.n_rows ? static_cast<int>(key) : kNone;
+    if (sparse) {
+      const int first = key < a.n_rows && (i == 0 || static_cast<uint32_t>(s.buf[i - 1] >> 32) != key);
+      int total;
+      const int x = block_prefix<kWaves>(first, s.waves, total);
+      if (row >= 0) row = base + x + first - 1;
+      if (first) a.rows[row] = static_cast<int32_t>(key);
+      base += total;
+    }
+    if (i < n) a.tokens[i] = make_int2(row, static_cast<int>(static_cast<uint32_t>(s.buf[i])));
   }
-  for (int i = threadIdx.x; i < n; i += kThreads) a.pairs[(p.passes - 1) & 1][i] = buf[i];
+  if (sparse && threadIdx.x == 0) *a.count = base;
 }
 
-// ---- the distinct ids before each summing workgroup's tokens
+// ---- rows of the result
 
-__device__ __forceinline__ uint32_t key_at(const uint64_t* pairs, int64_t i) {
-  return static_cast<uint32_t>(pairs[i] >> 32);
-}
-// Token i is the first one of a row.
-__device__ __forceinline__ bool head_at(const uint64_t* pairs, int64_t i, uint32_t n_rows) {
-  const uint32_t k = key_at(pairs, i);
-  return k < n_rows && (i == 0 || key_at(pairs, i - 1) != k);
-}
-
-__global__ __launch_bounds__(kThreads) void heads_kernel(const EmbedGradArgs a, const EmbedGradPlan p, int64_t per) {
+// A dense result's rows are the ids.  Of distinct ids, a workgroup numbers those
+// that begin among its tokens (of which it takes kThreads at a time) from 0, so
+// that a run begun before them has the number -1; head_sum holds how many begin.
+__global__ __launch_bounds__(kThreads) void rows_kernel(const EmbedGradArgs a, const EmbedGradPlan p) {
   __shared__ int waves[kWaves];
   const uint64_t* pairs = a.pairs[(p.passes - 1) & 1];
-  const int64_t g0 = blockIdx.x * per, g1 = min(p.groups, g0 + per);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  for (int64_t g = g0 + wave; g < g1; g += kWaves) {
-    int c = 0;
-    const int64_t t1 = min(a.n, (g + 1) * p.tokens);
-    for (int64_t i = g * p.tokens + lane; i < t1; i += 64) c += head_at(pairs, i, a.n_rows);
-#pragma unroll
-    for (int o = 32; o > 0; o /= 2) c += __shfl_xor(c, o);
-    if (lane == 0) a.head_off[g] = c;
-  }
-  __syncthreads();
-  int before = 0;
-  for (int64_t g = g0; g < g1; g += kThreads) {
-    const int64_t at = g + threadIdx.x;
+  const int64_t t0 = blockIdx.x * p.head_range, t1 = min(a.n, t0 + p.head_range);
+  int base = 0;
+  uint64_t next = t0 + threadIdx.x < t1 ? pairs[t0 + threadIdx.x] : 0, next_low = 0;
+  if (t0 + threadIdx.x < t1 && t0 + threadIdx.x > 0) next_low = pairs[t0 + threadIdx.x - 1];
+  for (int64_t i0 = t0; i0 < t1; i0 += kThreads) {
+    const int64_t i = i0 + threadIdx.x;
+    const uint64_t w = next, low = next_low;
+    if (i + kThreads < t1) {
+      next = pairs[i + kThreads];
+      next_low = pairs[i + kThreads - 1];
+    }
+    const uint32_t key = i < t1 ? static_cast<uint32_t>(w >> 32) : a.n_rows;
+    const int first = key < a.n_rows && (i == 0 || static_cast<uint32_t>(low >> 32) != key);
     int total;
-    const int x = block_prefix(at < g1 ? a.head_off[at] : 0, waves, total);
-    if (at < g1) a.head_off[at] = before + x;
-    before += total;
+    const int x = block_prefix<kWaves>(first, waves, total);
+    if (i < t1) a.tokens[i] = make_int2(key < a.n_rows ? base + x + first - 1 : kNone, static_cast<int>(static_cast<uint32_t>(w)));
+    base += total;
   }
-  if (threadIdx.x == 0) a.head_sum[blockIdx.x] = before;
+  if (threadIdx.x == 0) a.head_sum[blockIdx.x] = base;
 }
 
 // ---- sums
@@ -302,95 +338,86 @@ template <> struct Part<bf16_bits> {
   }
 };
 
+// Token i's row of dout.  (Looked up once a token, by one thread: by the lanes that
+// load it, the look-up's own loads were three of the four of a row.)
+template <typename T>
+__device__ __forceinline__ const T* dout_row(const EmbedGradArgs& a, int64_t i) {
+  const int q = part_of(a, i);
+  return static_cast<const T*>(a.dout[q]) + (i - (q ? a.end[q - 1] : 0)) * a.ld[q];
+}
+
 struct Level {
   int64_t n;        // what is added: tokens, or slots of the level before
   int64_t groups;   // workgroups of this level, each of which leaves two slots
   int in, out;      // buffers of slots
-  int blocks;       // of head_sum; 0: every workgroup counts for itself
-  int64_t per;      // workgroups of a block
+  int heads;        // workgroups that numbered distinct ids; 0: rows are known
 };
 
 // kFirst: the rows of dout in the order of the sorted tokens; else slots.  W:
-// features a lane, L: lanes a team.
-template <bool kFirst, typename T, int L>
-__global__ __launch_bounds__(kThreads) void sum_kernel(const EmbedGradArgs a, const EmbedGradPlan p, const Level lv) {
-  constexpr int W = Part<T>::kN, kTeams = kThreads / L, kTokens = kTeams * kTeamTokens;
-  constexpr int kBatch = 8;
+// features a lane, L: lanes a team, kTeam: tokens of a team.
+template <bool kFirst, typename T, int L, int kTeam>
+__global__ __launch_bounds__(kFirst ? kFirstThreads : kUpThreads) void sum_kernel(const EmbedGradArgs a, const EmbedGradPlan p, const Level lv) {
+  constexpr int kSumThreads = kFirst ? kFirstThreads : kUpThreads, kSumWaves = kSumThreads / 64;
+  constexpr int W = Part<T>::kN, kTeams = kSumThreads / L, kTokens = kTeams * kTeam;
+  constexpr int kBatch = kFirst ? 4 : 16;  // rows of a team on their way at a time
   __shared__ int row[kTokens];      // run of a token: its row of the result, -1: none
-  __shared__ int src[kTokens];      // where its value lies, -1: none
-  __shared__ float head[kTeams][L * W], tail[kTeams][L * W];
+  __shared__ const T* src[kTokens]; // its value's row, null: none
+  __shared__ float head[kTeams][L * W];
   __shared__ int state[kTeams];     // of a team's head: 0 none, 1 it ends there, 2 it goes on
-  __shared__ int edge[2], waves[kWaves];
+  __shared__ int edge[2], waves[kSumWaves];
   const int64_t t0 = static_cast<int64_t>(blockIdx.x) * kTokens;
   const int n = static_cast<int>(min<int64_t>(kTokens, lv.n - t0));
-  const uint64_t* pairs = kFirst ? a.pairs[(p.passes - 1) & 1] : nullptr;
-  const int2* slots = kFirst ? nullptr : a.slot[lv.in];
   const bool sparse = a.dtable == nullptr;
 
   if constexpr (kFirst) {
+    // (row, token) of the workgroup's tokens, which one workgroup numbered
+    const bool numbered = lv.heads > 0, keyed = !p.small && !numbered;
+    const uint64_t* pairs = a.pairs[(p.passes - 1) & 1];
     int base = 0;
-    if (sparse) {
-      // distinct ids before this workgroup's, and of all
-      int before = 0, all = 0, part = 0;
-      if (lv.blocks > 0) {
-        const int b = static_cast<int>(blockIdx.x / lv.per);
-        for (int i = threadIdx.x; i < lv.blocks; i += kThreads) {
-          const int c = a.head_sum[i];
-          before += i < b ? c : 0;
-          all += c;
-        }
-        part = a.head_off[blockIdx.x];
-      } else {
-        for (int64_t i = threadIdx.x; i < lv.n; i += kThreads) {
-          const int c = head_at(pairs, i, a.n_rows);
-          before += i < t0 ? c : 0;
-          all += c;
-        }
+    if (numbered) {
+      const int b = static_cast<int>(t0 / p.head_range);
+      int low = 0, all = 0;
+      for (int i = threadIdx.x; i < lv.heads; i += kSumThreads) {
+        const int c = a.head_sum[i];
+        all += c;
+        low += i < b ? c : 0;
       }
-      int total;
-      block_prefix(before, waves, total);
-      base = total + part;
-      block_prefix(all, waves, total);
-      if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *a.count = total;
-    }
-    for (int i0 = 0; i0 < kTokens; i0 += kThreads) {
-      const int i = i0 + threadIdx.x;
-      uint32_t key = a.n_rows;
-      int64_t tok = 0;
-      int first = 0;
-      if (i < n) {
-        const uint64_t w = pairs[t0 + i];
-        key = static_cast<uint32_t>(w >> 32);
-        tok = static_cast<uint32_t>(w);
-        first = sparse && head_at(pairs, t0 + i, a.n_rows);
-      }
-      int r = key < a.n_rows ? static_cast<int>(key) : -1;
-      if (sparse) {
+      block_prefix<kSumWaves>(low, waves, base);
+      if (blockIdx.x == 0 && blockIdx.y == 0) {
         int total;
-        const int x = block_prefix(first, waves, total);
-        if (r >= 0) {
-          r = base + x + first - 1;
-          if (first && blockIdx.y == 0) a.rows[r] = static_cast<int32_t>(key);
-        }
-        base += total;
+        block_prefix<kSumWaves>(all, waves, total);
+        if (threadIdx.x == 0) *a.count = total;
       }
-      if (i < kTokens) {  // (a workgroup of wide rows has fewer tokens than threads)
-        row[i] = r;
-        src[i] = r >= 0 ? static_cast<int>(tok) : -1;
-      }
+    }
+    auto at = [&](int64_t i) {
+      if (!keyed) return a.tokens[i];
+      const uint64_t w = pairs[i];
+      const uint32_t key = static_cast<uint32_t>(w >> 32);
+      return make_int2(key < a.n_rows ? static_cast<int>(key) : kNone, static_cast<int>(static_cast<uint32_t>(w)));
+    };
+    for (int i = threadIdx.x; i < kTokens; i += kSumThreads) {
+      int2 w = make_int2(kNone, -1);
+      if (i < n) w = at(t0 + i);
+      row[i] = w.x == kNone ? -1 : base + w.x;
+      src[i] = w.x == kNone ? nullptr : dout_row<T>(a, static_cast<uint32_t>(w.y));
     }
     if (threadIdx.x == 0) {
-      // rows of the neighbours on both sides, as far as they are those of the outermost tokens
-      const int64_t last = t0 + n - 1;
-      edge[0] = t0 > 0 && key_at(pairs, t0 - 1) == key_at(pairs, t0);
-      edge[1] = last + 1 < lv.n && key_at(pairs, last + 1) == key_at(pairs, last);
+      // whether the runs of the outermost tokens reach over the workgroup's borders
+      const int64_t after = t0 + n;
+      auto same = [&](int64_t i) {  // tokens i - 1 and i
+        const int r = at(i).x;
+        return numbered && i % p.head_range == 0 ? r == -1 : r == at(i - 1).x;
+      };
+      edge[0] = t0 > 0 && same(t0);
+      edge[1] = after < lv.n && same(after);
     }
   } else {
-    for (int i = threadIdx.x; i < kTokens; i += kThreads) {
+    const int2* slots = a.slot[lv.in];
+    for (int i = threadIdx.x; i < kTokens; i += kSumThreads) {
       int2 s = make_int2(-1, 0);
       if (i < n) s = slots[t0 + i];
       row[i] = s.x;
-      src[i] = s.x >= 0 && s.y ? static_cast<int>(t0 + i) : -1;
+      src[i] = s.x >= 0 && s.y ? reinterpret_cast<const T*>(a.slot_val[lv.in]) + (t0 + i) * a.d : nullptr;
     }
     if (threadIdx.x == 0) {
       const int64_t last = t0 + n - 1;
@@ -400,21 +427,16 @@ __global__ __launch_bounds__(kThreads) void sum_kernel(const EmbedGradArgs a, co
   }
   if (threadIdx.x < kTeams) state[threadIdx.x] = 0;
   __syncthreads();
-
+  if constexpr (kFirst) {
+    if (lv.heads > 0 && blockIdx.y == 0) {  // the list of the distinct ids
+      const uint64_t* pairs = a.pairs[(p.passes - 1) & 1];
+      for (int i = threadIdx.x; i < n; i += kSumThreads)
+        if (row[i] >= 0 && (i ? row[i - 1] != row[i] : !edge[0])) a.rows[row[i]] = static_cast<int32_t>(pairs[t0 + i] >> 32);
+    }
+  }
   const int lane = threadIdx.x % L, team = threadIdx.x / L;
   const int col = (static_cast<int>(blockIdx.y) * L + lane) * W;
   const bool live = col < a.d;
-  auto load = [&](int at) {
-    Part<T> v;
-    if constexpr (kFirst) {
-      const int64_t i = static_cast<uint32_t>(at);
-      const int q = part_of(a, i);
-      v.load(static_cast<const T*>(a.dout[q]) + (i - (q ? a.end[q - 1] : 0)) * a.ld[q] + col);
-    } else {
-      v.load(reinterpret_cast<const T*>(a.slot_val[lv.in]) + static_cast<int64_t>(at) * a.d + col);
-    }
-    return v;
-  };
   auto put = [&](int r, const float* x) {
     if (!live) return;
     float* to = sparse ? a.grads + static_cast<int64_t>(r) * a.d + col : a.dtable + static_cast<int64_t>(r) * a.ldt + col;
@@ -427,21 +449,21 @@ __global__ __launch_bounds__(kThreads) void sum_kernel(const EmbedGradArgs a, co
   };
 
   // the team's tokens
-  const int i0 = team * kTeamTokens, i1 = min(n, i0 + kTeamTokens);
+  const int i0 = team * kTeam, i1 = min(n, i0 + kTeam);
   bool open = false;  // the run at the team's end began here and goes on
+  float acc[W] = {};  // ... and its sum
   if (i0 < n) {
-    float acc[W] = {};
     int cur = row[i0];
     bool begun = i0 == 0 ? edge[0] != 0 : row[i0 - 1] == cur;  // before the team's first token
-    for (int i = i0; i < i1; i += kBatch) {
-      Part<T> v[kBatch];
-      bool have[kBatch];
+    auto fetch = [&](Part<T>* v, bool* have, int i) {
 #pragma unroll
       for (int k = 0; k < kBatch; ++k) {
-        const int s = i + k < i1 ? src[i + k] : -1;
-        have[k] = s != -1 && live;
-        if (have[k]) v[k] = load(s);
+        const T* s = i + k < i1 ? src[i + k] : nullptr;
+        have[k] = s && live;
+        if (have[k]) v[k].load(s + col);
       }
+    };
+    auto take = [&](const Part<T>* v, const bool* have, int i) {
 #pragma unroll
       for (int k = 0; k < kBatch; ++k) {
         if (i + k >= i1) break;
@@ -463,15 +485,21 @@ __global__ __launch_bounds__(kThreads) void sum_kernel(const EmbedGradArgs a, co
         }
         if (have[k]) v[k].add_to(acc);
       }
+    };
+    for (int i = i0; i < i1; i += kBatch) {
+      Part<T> v[kBatch];
+      bool have[kBatch];
+      fetch(v, have, i);
+      take(v, have, i);
     }
     if (cur >= 0) {
       const bool on = i1 < n ? row[i1] == cur : edge[1] != 0;
-      if (begun || on) {
-        float* to = begun ? head[team] : tail[team];
+      if (begun) {
 #pragma unroll
-        for (int e = 0; e < W; ++e) to[lane * W + e] = acc[e];
-        if (begun && lane == 0) state[team] = on ? 2 : 1;
-        open = !begun;
+        for (int e = 0; e < W; ++e) head[team][lane * W + e] = acc[e];
+        if (lane == 0) state[team] = on ? 2 : 1;
+      } else if (on) {
+        open = true;
       } else {
         put(cur, acc);
       }
@@ -481,20 +509,20 @@ __global__ __launch_bounds__(kThreads) void sum_kernel(const EmbedGradArgs a, co
 
   // runs over several teams: the team that began one adds the others' heads; the
   // first team also the run that it found begun
-  const int teams = (n + kTeamTokens - 1) / kTeamTokens;
-  auto join = [&](float* acc, int at) {  // true: the run ends in this workgroup
+  const int teams = (n + kTeam - 1) / kTeam;
+  auto join = [&](float* sum, int at) {  // true: the run ends in this workgroup
     for (; at < teams; ++at) {
 #pragma unroll
-      for (int e = 0; e < W; ++e) acc[e] += head[at][lane * W + e];
+      for (int e = 0; e < W; ++e) sum[e] += head[at][lane * W + e];
       if (state[at] == 1) return true;
     }
     return false;
   };
-  auto leave = [&](int slot, const float* acc) {
+  auto leave = [&](int slot, const float* x) {
     if (!live) return;
     float* to = a.slot_val[lv.out] + (2 * static_cast<int64_t>(blockIdx.x) + slot) * a.d + col;
 #pragma unroll
-    for (int e = 0; e < W; e += 4) *reinterpret_cast<f32x4*>(to + e) = f32x4{acc[e], acc[e + 1], acc[e + 2], acc[e + 3]};
+    for (int e = 0; e < W; e += 4) *reinterpret_cast<f32x4*>(to + e) = f32x4{x[e], x[e + 1], x[e + 2], x[e + 3]};
   };
   const bool note = lane == 0 && blockIdx.y == 0 && lv.groups > 1;
   int2* made = lv.groups > 1 ? a.slot[lv.out] + 2 * static_cast<int64_t>(blockIdx.x) : nullptr;
@@ -507,16 +535,13 @@ __global__ __launch_bounds__(kThreads) void sum_kernel(const EmbedGradArgs a, co
     made[1] = make_int2(r, !through);
   }
   if (team == 0 && state[0] != 0) {
-    float acc[W];
+    float sum[W];
 #pragma unroll
-    for (int e = 0; e < W; ++e) acc[e] = head[0][lane * W + e];
-    if (state[0] == 2) join(acc, 1);
-    leave(0, acc);
+    for (int e = 0; e < W; ++e) sum[e] = head[0][lane * W + e];
+    if (state[0] == 2) join(sum, 1);
+    leave(0, sum);
   }
   if (open) {
-    float acc[W];
-#pragma unroll
-    for (int e = 0; e < W; ++e) acc[e] = tail[team][lane * W + e];
     if (join(acc, team + 1)) put(row[i1 - 1], acc);
     else leave(1, acc);
   }
@@ -536,9 +561,16 @@ __global__ __launch_bounds__(256) void clear_kernel(const EmbedGradArgs a) {
   }
 }
 
+// Tokens of a team: enough that few runs cross a border and the teams' own cost
+// is spread, few where there are few, and where the levels above add sums.
+constexpr int kTeamFirst = 32, kTeamSmall = 8, kTeamUp = 16;
+
 template <bool kFirst, typename T, int L>
 hipError_t launch_sum(const EmbedGradArgs& a, const EmbedGradPlan& p, const Level& lv, int cols, hipStream_t st) {
-  sum_kernel<kFirst, T, L><<<dim3(static_cast<unsigned>(lv.groups), cols), kThreads, 0, st>>>(a, p, lv);
+  const dim3 grid(static_cast<unsigned>(lv.groups), cols);
+  if constexpr (!kFirst) sum_kernel<kFirst, T, L, kTeamUp><<<grid, kUpThreads, 0, st>>>(a, p, lv);
+  else if (p.small) sum_kernel<kFirst, T, L, kTeamSmall><<<grid, kFirstThreads, 0, st>>>(a, p, lv);
+  else sum_kernel<kFirst, T, L, kTeamFirst><<<grid, kFirstThreads, 0, st>>>(a, p, lv);
   return hipGetLastError();
 }
 
@@ -547,17 +579,17 @@ struct Shape {
   int lanes, cols;
   int64_t tokens;
 };
-Shape shape_of(int d, int W) {
+Shape shape_of(int d, int W, int threads, int team) {
   Shape s{8, 1, 0};
   while (s.lanes < 64 && s.lanes * W < d) s.lanes *= 2;
   s.cols = static_cast<int>(ceil_div(d, s.lanes * W));
-  s.tokens = kThreads / s.lanes * kTeamTokens;
+  s.tokens = threads / s.lanes * team;
   return s;
 }
 
 template <bool kFirst, typename T>
 hipError_t sum_level(const EmbedGradArgs& a, const EmbedGradPlan& p, const Level& lv, hipStream_t st) {
-  const Shape s = shape_of(a.d, Part<T>::kN);
+  const Shape s = shape_of(a.d, Part<T>::kN, 1, 1);
   if (s.lanes == 8) return launch_sum<kFirst, T, 8>(a, p, lv, s.cols, st);
   if (s.lanes == 16) return launch_sum<kFirst, T, 16>(a, p, lv, s.cols, st);
   if (s.lanes == 32) return launch_sum<kFirst, T, 32>(a, p, lv, s.cols, st);
@@ -574,11 +606,11 @@ EmbedGradPlan embed_grad_plan(int64_t n, uint32_t n_rows, int d, int dtype) {
   p.small = n <= kSmall;
   p.blocks = static_cast<int>(std::min<int64_t>(kMaxBlocks, std::max<int64_t>(1, ceil_div(n, kSmall / 2))));
   p.range = ceil_div(n, p.blocks);
-  const Shape s = shape_of(d, dtype == STCA_BF16 ? 8 : 4), up = shape_of(d, 4);
-  p.tokens = s.tokens;
-  p.groups = ceil_div(n, s.tokens);
-  p.next_groups = ceil_div(2 * p.groups, up.tokens);
-  p.head_blocks = p.small ? 0 : static_cast<int>(std::min<int64_t>(kMaxBlocks, p.groups));
+  const int64_t tokens = shape_of(d, dtype == STCA_BF16 ? 8 : 4, kFirstThreads, p.small ? kTeamSmall : kTeamFirst).tokens;
+  p.groups = ceil_div(n, tokens);
+  p.next_groups = ceil_div(2 * p.groups, shape_of(d, 4, kUpThreads, kTeamUp).tokens);
+  p.head_range = std::max<int64_t>(tokens, round_up(ceil_div(n, kMaxBlocks), tokens));
+  p.heads = p.small ? 0 : static_cast<int>(ceil_div(n, p.head_range));
   return p;
 }
 
@@ -599,14 +631,13 @@ hipError_t embed_grad(const EmbedGradArgs& a, int dtype, hipStream_t st) {
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  Level lv{a.n, p.groups, 0, 0, 0, 0};
-  if (!a.dtable && p.head_blocks > 0) {
-    lv.per = ceil_div(p.groups, p.head_blocks);
-    lv.blocks = static_cast<int>(ceil_div(p.groups, lv.per));
-    heads_kernel<<<lv.blocks, kThreads, 0, st>>>(a, p, lv.per);
+  Level lv{a.n, p.groups, 0, 0, 0};
+  if (!a.dtable && !p.small) {
+    lv.heads = p.heads;
+    rows_kernel<<<p.heads, kThreads, 0, st>>>(a, p);
   }
   e = dtype == STCA_BF16 ? sum_level<true, bf16_bits>(a, p, lv, st) : sum_level<true, float>(a, p, lv, st);
-  const int64_t up = shape_of(a.d, 4).tokens;
+  const int64_t up = shape_of(a.d, 4, kUpThreads, kTeamUp).tokens;
   while (e == hipSuccess && lv.groups > 1) {
     lv.n = 2 * lv.groups;
     lv.groups = ceil_div(lv.n, up);

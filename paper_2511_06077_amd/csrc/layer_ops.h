@@ -47,11 +47,11 @@ struct EmbedGradArgs {
   int32_t* count;
   // workspace
   WsHeader* hdr;
-  int32_t* counts;              // [blocks][digits]
+  int32_t* counts;              // [digits][256 blocks]
   int32_t* bad;                 // [blocks]
   uint64_t* pairs[2];           // id in the high half, token in the low one
-  int32_t* head_off;            // distinct ids before a workgroup's tokens, within its block of workgroups
-  int32_t* head_sum;            // ... of the blocks
+  int2* tokens;                 // row of the result and token, in sorted order (not of a long list for a dense result)
+  int32_t* head_sum;            // distinct ids that each numbering workgroup found
   int2* slot[2];                // per workgroup of a level two: run's row, whether there is a value
   float* slot_val[2];
 };
@@ -60,9 +60,9 @@ struct EmbedGradPlan {
   int blocks, passes, bits;     // sort: workgroups, digits and bits a digit
   int64_t range;                // tokens of a workgroup
   bool small;                   // sorted by one workgroup
-  int64_t tokens;               // of a summing workgroup
   int64_t groups, next_groups;  // summing workgroups of the first level and the next
-  int head_blocks;              // most entries of head_sum
+  int64_t head_range;           // tokens of a numbering workgroup: whole summing workgroups'
+  int heads;                    // numbering workgroups
 };
 EmbedGradPlan embed_grad_plan(int64_t n, uint32_t n_rows, int d, int dtype);
 hipError_t embed_grad(const EmbedGradArgs& a, int dtype, hipStream_t st);
