@@ -56,7 +56,7 @@ GradLayout grad_layout(const stca_embed_grad_t* g, int64_t n) {
     }
     for (int i = 0; i < 2; ++i) l.pairs[i] = m.take(!p.small && i < p.passes ? 8 * static_cast<size_t>(n) : 0);
     l.tokens = m.take(8 * static_cast<size_t>(n));
-    l.head_sum = m.take(4 * static_cast<size_t>(p.heads));
+    l.head_sum = m.take(p.small ? 0 : 4 * 256);
     const int64_t groups[2] = {p.groups > 1 ? p.groups : 0, p.groups > 1 && p.next_groups > 1 ? p.next_groups : 0};
     for (int i = 0; i < 2; ++i) {
       l.slot[i] = m.take(16 * static_cast<size_t>(groups[i]));
@@ -229,7 +229,9 @@ stca_status_t stca_embed_forward(const stca_embed_t* embed, const stca_embed_fie
 }
 
 size_t stca_embed_grad_workspace_size(const stca_embed_grad_t* grad, int64_t n) {
-  return check_grad(grad, n) == STCA_OK ? grad_layout(grad, n).total : 0;
+  if (check_grad(grad, n) != STCA_OK) return 0;
+  // (few ids are divided finer and may need more than many: a workspace for n serves fewer as well)
+  return std::max(grad_layout(grad, n).total, grad_layout(grad, std::min<int64_t>(n, kEmbedSmall)).total);
 }
 
 stca_status_t stca_embed_grad_dense(const stca_embed_grad_t* grad, const stca_embed_part_t* parts, int32_t n_parts,

@@ -44,21 +44,46 @@ __device__ __forceinline__ double block_sum(double v, double* lds) {
   return v;
 }
 
+// 16 bytes of a gradient.
+template <typename T> struct Piece;
+template <> struct Piece<float> {
+  static constexpr int kN = 4;
+  f32x4 v;
+  __device__ __forceinline__ void load(const float* p) { v = *reinterpret_cast<const f32x4*>(p); }
+  __device__ __forceinline__ void get(float* x) const {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = v[i];
+  }
+};
+template <> struct Piece<bf16_bits> {
+  static constexpr int kN = 8;
+  Oct<bf16_bits> v;
+  __device__ __forceinline__ void load(const bf16_bits* p) { v.load(p); }
+  __device__ __forceinline__ void get(float* x) const { v.get(x); }
+};
+
+constexpr int kBatch = 4;  // loads of a thread on their way at a time
+
 template <typename T>
 __device__ __forceinline__ double squares(const T* g, int64_t n) {
+  constexpr int N = Piece<T>::kN;
   double v[4] = {};
-  const bool wide = (reinterpret_cast<uintptr_t>(g) & 15u) == 0;
   int64_t done = 0;
-  if (wide) {
-    done = n / 8 * 8;
-#pragma unroll 4
-    for (int64_t i = 8 * threadIdx.x; i < done; i += 8 * kThreads) {
-      Oct<T> o;
-      o.load(g + i);
-      float x[8];
-      o.get(x);
+  if ((reinterpret_cast<uintptr_t>(g) & 15u) == 0) {
+    done = n / N * N;
+    for (int64_t i0 = N * threadIdx.x; i0 < done; i0 += kBatch * N * kThreads) {
+      Piece<T> p[kBatch];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e & 3] = fma(static_cast<double>(x[e]), static_cast<double>(x[e]), v[e & 3]);
+      for (int k = 0; k < kBatch; ++k)
+        if (i0 + k * N * kThreads < done) p[k].load(g + i0 + k * N * kThreads);
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k) {
+        if (i0 + k * N * kThreads >= done) break;
+        float x[N];
+        p[k].get(x);
+#pragma unroll
+        for (int e = 0; e < N; ++e) v[e & 3] = fma(static_cast<double>(x[e]), static_cast<double>(x[e]), v[e & 3]);
+      }
     }
   }
   for (int64_t i = done + threadIdx.x; i < n; i += kThreads) {
@@ -81,21 +106,44 @@ __global__ __launch_bounds__(kThreads) void sum_kernel(const ClipArgs a) {
   if (threadIdx.x == 0) a.part[blockIdx.x] = v;
 }
 
+// Past the caches: the next pass over the gradients finds these free of dirty lines
+// (243 MB clipped into other buffers: 80 us, 77 so, and the sums of squares before
+// them 66 and 44).
+template <int N>
+__device__ __forceinline__ void store(float* p, const float* x) {
+#pragma unroll
+  for (int e = 0; e < N; e += 4)
+    __builtin_nontemporal_store(f32x4{x[e], x[e + 1], x[e + 2], x[e + 3]}, reinterpret_cast<f32x4*>(p + e));
+}
+template <int N>
+__device__ __forceinline__ void store(bf16_bits* p, const float* x) {
+  typedef uint32_t words __attribute__((ext_vector_type(N / 2)));
+  words w;
+#pragma unroll
+  for (int e = 0; e < N / 2; ++e) w[e] = two_bf16(x[2 * e], x[2 * e + 1]);
+  __builtin_nontemporal_store(w, reinterpret_cast<words*>(p));
+}
+
 template <typename T, typename O>
 __device__ __forceinline__ void scale_piece(const T* g, O* out, int64_t n, double f) {
-  const bool wide = ((reinterpret_cast<uintptr_t>(g) | reinterpret_cast<uintptr_t>(out)) & 15u) == 0;
+  constexpr int N = Piece<T>::kN;
   int64_t done = 0;
-  if (wide) {
-    done = n / 8 * 8;
-#pragma unroll 4
-    for (int64_t i = 8 * threadIdx.x; i < done; i += 8 * kThreads) {
-      Oct<T> o;
-      o.load(g + i);
-      float x[8];
-      o.get(x);
+  if (((reinterpret_cast<uintptr_t>(g) | reinterpret_cast<uintptr_t>(out)) & 15u) == 0) {
+    done = n / N * N;
+    for (int64_t i0 = N * threadIdx.x; i0 < done; i0 += kBatch * N * kThreads) {
+      Piece<T> p[kBatch];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = static_cast<float>(x[e] * f);
-      Oct<O>::store(out + i, x);
+      for (int k = 0; k < kBatch; ++k)
+        if (i0 + k * N * kThreads < done) p[k].load(g + i0 + k * N * kThreads);
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k) {
+        if (i0 + k * N * kThreads >= done) break;
+        float x[N];
+        p[k].get(x);
+#pragma unroll
+        for (int e = 0; e < N; ++e) x[e] = static_cast<float>(x[e] * f);
+        store<N>(out + i0 + k * N * kThreads, x);
+      }
     }
   }
   for (int64_t i = done + threadIdx.x; i < n; i += kThreads) out[i] = from_f32<O>(static_cast<float>(to_f32(g[i]) * f));

@@ -21,8 +21,8 @@ constexpr int kThreads = 1024;   // of a sorting workgroup (512: 15 us a pass ov
 constexpr int kWaves = kThreads / 64;
 constexpr int kDigits = 256;
 constexpr int kMaxBlocks = 256;  // workgroups of a sort
-constexpr int kItems = 4096 / kThreads;        // tokens a thread of a sort's tile
-constexpr int kSmall = kThreads * kItems;
+constexpr int kItems = kEmbedSmall / kThreads;        // tokens a thread of a sort's tile
+constexpr int kSmall = kEmbedSmall;
 constexpr int kFirstThreads = 256;  // of a summing workgroup of the first level
 constexpr int kUpThreads = 1024;    // ... of the levels above: as few of them as may be
 constexpr int kNone = -2;        // no row of the result (-1: the last one of the numbering before)
@@ -444,7 +444,7 @@ __global__ __launch_bounds__(kFirst ? kFirstThreads : kUpThreads) void sum_kerne
     for (int e = 0; e < W; e += 4) {
       f32x4 y = f32x4{x[e], x[e + 1], x[e + 2], x[e + 3]} * a.scale;
       if (!sparse && a.accumulate) y += *reinterpret_cast<const f32x4*>(to + e);
-      *reinterpret_cast<f32x4*>(to + e) = y;
+      __builtin_nontemporal_store(y, reinterpret_cast<f32x4*>(to + e));
     }
   };
 

@@ -55,6 +55,7 @@ struct EmbedGradArgs {
   int2* slot[2];                // per workgroup of a level two: run's row, whether there is a value
   float* slot_val[2];
 };
+constexpr int kEmbedSmall = 4096;  // up to so many tokens are sorted by one workgroup
 // Sizes that the workspace and the launches agree on.
 struct EmbedGradPlan {
   int blocks, passes, bits;     // sort: workgroups, digits and bits a digit
@@ -96,7 +97,7 @@ struct Grad {
 };
 constexpr int kGradsPerLaunch = 64;
 constexpr int kGradPiece = 8192;    // elements of a piece
-constexpr int kGradGroups = 1024;   // workgroups of a launch
+constexpr int kGradGroups = 2048;   // workgroups of a launch
 struct ClipArgs {
   Grad t[kGradsPerLaunch];
   int32_t n_t;
@@ -130,8 +131,9 @@ template <> struct Oct<bf16_bits> {
     x[4] = lo_of(w.z), x[5] = hi_of(w.z), x[6] = lo_of(w.w), x[7] = hi_of(w.w);
   }
   static __device__ __forceinline__ void store(bf16_bits* p, const float* x) {
-    *reinterpret_cast<uint4*>(p) =
-        make_uint4(two_bf16(x[0], x[1]), two_bf16(x[2], x[3]), two_bf16(x[4], x[5]), two_bf16(x[6], x[7]));
+    typedef uint32_t words __attribute__((ext_vector_type(4)));
+    const words w = {two_bf16(x[0], x[1]), two_bf16(x[2], x[3]), two_bf16(x[4], x[5]), two_bf16(x[6], x[7])};
+    __builtin_nontemporal_store(w, reinterpret_cast<words*>(p));
   }
 };
 template <> struct Oct<float> {

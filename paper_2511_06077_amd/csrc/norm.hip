@@ -385,7 +385,7 @@ hipError_t pick(const NormArgs& a, int grid, bool backward, hipStream_t st) {
 }  // namespace
 
 int norm_partials(int64_t n, int d, int n_cu) {
-  return static_cast<int>(std::min<int64_t>(ceil_div(n, rows_of(d)), 4 * static_cast<int64_t>(n_cu)));
+  return static_cast<int>(std::min<int64_t>(ceil_div(n, rows_of(d)), 2 * static_cast<int64_t>(n_cu)));
 }
 
 hipError_t norm_forward(const NormArgs& a, int dtype, int n_cu, hipStream_t st) {

@@ -329,19 +329,26 @@ class GradientNorm(_Streamed):
             raise ValueError("out and counts: one for every gradient")
         if len(grads) > self.most:
             raise ValueError(f"{len(grads)} gradients, where the object was made for {self.most}")
+        codes = {torch.float32: stca.STCA_F32, torch.bfloat16: stca.STCA_BF16}
+        at = -1 if self.device.index is None else self.device.index  # (get_device() of the host's tensors is -1)
         items = []
         for i, (g, o, c) in enumerate(zip(grads, out, counts)):
-            n, row = g.numel(), 0
-            for t in (g, o):
-                if t is not None and (t.device != self.device or not t.is_contiguous() or t.numel() != n):
-                    raise ValueError(f"gradient {i}: contiguous tensors of one size on {self.device} are needed")
+            n, code, row = g.numel(), codes.get(g.dtype), 0
+            ok = code is not None and g.get_device() == at and g.is_contiguous()
+            p, to = 0, code
+            if o is g:
+                p = g.data_ptr()
+            elif o is not None:
+                p, to = o.data_ptr(), codes.get(o.dtype)
+                ok = ok and to is not None and o.get_device() == at and o.is_contiguous() and o.numel() == n
+            if not ok:
+                raise ValueError(f"gradient {i}: contiguous fp32 or bf16 tensors of one size on {self.device} are needed")
             if c is not None:
                 _flat(f"counts[{i}]", c, torch.int32, (1,), self.device)
                 if g.dim() == 0:
                     raise ValueError(f"counts[{i}]: the gradient has no rows")
                 row = max(1, n // max(1, g.shape[0]))
-            code = _dtype_code(g.dtype)
-            items.append((g, o, n, code, code if o is None else _dtype_code(o.dtype), c, row))
+            items.append((g.data_ptr(), p, n, code, to, 0 if c is None else c.data_ptr(), row))
         with self._on(stream):
             norm = torch.empty((), dtype=torch.float32, device=self.device)
             stca.stca_clip(stca.grads(items), self.max_norm, norm, self.ws, self.ws_bytes, self._at(stream))

@@ -7,7 +7,9 @@ fallback: if the library is missing, loading it raises.
 from __future__ import annotations
 
 import ctypes
+import itertools
 import os
+import struct
 from typing import Optional
 
 PKG = os.path.dirname(os.path.abspath(__file__))
@@ -289,7 +291,7 @@ def lib():
                 ("stca_norm_backward", ctypes.c_int,
                  [P(stca_norm_t), P(stca_norm_in_t), I64, V, I64, V, I64, P(stca_norm_grads_t), V, SZ, V]),
                 ("stca_clip_workspace_size", SZ, [ctypes.c_int32]),
-                ("stca_clip", ctypes.c_int, [P(stca_grad_t), ctypes.c_int32, ctypes.c_double, V, V, SZ, V])):
+                ("stca_clip", ctypes.c_int, [V, ctypes.c_int32, ctypes.c_double, V, V, SZ, V])):
             getattr(L, name).restype, getattr(L, name).argtypes = res, args
         _lib = L
     return _lib
@@ -611,9 +613,10 @@ def norm_grads(dx=None, dblock=None, dgate=None, lddx: int = 0, lddblock: int = 
                              _ptr(dpre_b), _ptr(dpost_w), _ptr(dpost_b), _ptr(dlayer_scale))
 
 
-def grads(items):
-    """items: (g, out, elements, dtype, dtype of out, count, elements of a row) each."""
-    return (stca_grad_t * len(items))(*((_ptr(g), _ptr(o), n, t, u, _ptr(c), r) for g, o, n, t, u, c, r in items))
+def grads(items) -> bytes:
+    """items: (g, out, elements, dtype, dtype of out, count, elements of a row) each, pointers as numbers
+    (0: none).  An array of stca_grad_t, packed at once: one by one its fields cost more than the call."""
+    return struct.pack("QQqiiQi4x" * len(items), *itertools.chain.from_iterable(items))
 
 
 def stca_embed_forward(e, fields, n: int, out, ldo: int = 0, ws=None, stream=None, check: bool = True) -> int:
@@ -656,7 +659,7 @@ def stca_clip_workspace_size(n_grads: int) -> int:
 
 
 def stca_clip(items, max_norm: float, norm_out, ws, ws_bytes: int, stream=None, check: bool = True) -> int:
-    return _checked("stca_clip", check, items, len(items), max_norm, _ptr(norm_out), _ptr(ws), int(ws_bytes),
+    return _checked("stca_clip", check, items, len(items) // ctypes.sizeof(stca_grad_t), max_norm, _ptr(norm_out), _ptr(ws), int(ws_bytes),
                     _ptr(stream))
 
 

@@ -155,8 +155,8 @@ def clip(items, max_norm=1.0, norm_out=0x100, ws=0x200000, ws_bytes=1 << 40):
     return stca.stca_clip(stca.grads(items), max_norm, norm_out, ws, ws_bytes, None, check=False)
 
 
-def g(at=0x1000000, out=0x2000000, n=100, dtype=F32, out_dtype=F32, count=None, row=0):
-    return at, out, n, dtype, out_dtype, count, row
+def g(at=0x1000000, out=0x2000000, n=100, dtype=F32, out_dtype=F32, count=0, row=0):
+    return at, out or 0, n, dtype, out_dtype, count, row
 
 
 def test_clip_arguments():
