@@ -10,6 +10,14 @@
 // and then two a workgroup, which the next level adds the same way.  So the work
 // is even, whether every id is another or all are the same, nothing is added
 // atomically, and the order of a row's sum depends on the tokens alone.
+//
+// Bound by the bytes of dout and of the distinct rows, which the first level moves
+// (528384 tokens of 256 fp32 features, 150 us for
+// 691 MB, 4.6 TB/s; 524288 bf16 ones of 16 ids 52 us, 5.2 TB/s); the sort before it
+// is latency, 18 us for every 8 bits of the ids, and the levels above 6 to 9 each.
+// What the first level measured (us, 528384 tokens): 512 threads a workgroup and 8
+// rows on their way 161, 256 and 4 157 (bf16, 16 ids: 66 and 52, registers for 8
+// waves a SIMD); the next batch fetched before one is added 178.
 #include "layer_ops.h"
 
 namespace stca {

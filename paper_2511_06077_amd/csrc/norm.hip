@@ -2,8 +2,10 @@
 //   t = post(o) act(g);  h = x + scale ls t;  y = pre(h)
 // and the gradients of all of it.  A team of lanes takes a row, eight features a
 // lane, and holds it in registers from the loads to the stores, so every row is
-// read and written once: bound by those bytes.  The backward recomputes what it
-// needs from x, o and g, which it has to read anyway; nothing is saved.
+// read and written once: bound by those bytes (524288 rows of 256 in bf16: the norm
+// alone 95 us, 5.6 TB/s; with block and gate 267 forward and 387 backward, 5.0 and
+// 5.6 TB/s).  The backward recomputes what it needs from x, o and g, which it has to
+// read anyway; nothing is saved.
 //
 // With u = (v - mean) r the unit row of a layer norm (mean = 0: of an rms norm),
 // a = w dy:  dv = r (a - mean(a) - u mean(a u)), without mean(a) for rms.
@@ -23,6 +25,13 @@ struct Team {
   static constexpr int kRows = kBlock / L;
   static constexpr int kWaves = L > 64 ? L / 64 : 1;
 };
+
+// Whether the next row's loads are on their way while a row is computed.  Where a
+// row's sums wait at barriers it pays (8191 rows of 2000: 71 -> 63 us backward, 38
+// -> 37 forward); where a wave has whole rows, the others hide the loads, and the
+// registers cost more (524288 of 256: 387 -> 399 and 267 -> 286).
+template <int L>
+constexpr bool kAhead = L > 64;
 
 // Sums over a team; of several waves through LDS, two buffers in turn, so that one
 // barrier a sum is enough.
@@ -176,13 +185,20 @@ __global__ __launch_bounds__(Team<L>::kBlock) void forward_kernel(const NormArgs
   qb.load(a.post_b, col, live, 0.f);
   ls.load(a.ls, col, live, 1.f);
   const int64_t step = static_cast<int64_t>(gridDim.x) * Team<L>::kRows;
+  Oct<T> nx, no, ng;
+  auto fetch = [&](int64_t i) {
+    const bool have = live && i < a.n;
+    row_of(a.x, a.ldx, i, col, have, nx);
+    row_of(a.block, a.ldb, i, col, have, no);
+    row_of(a.gate, a.ldg, i, col, have, ng);
+  };
+  if (kAhead<L>) fetch(static_cast<int64_t>(blockIdx.x) * Team<L>::kRows + team);
   for (int64_t base = static_cast<int64_t>(blockIdx.x) * Team<L>::kRows; base < a.n; base += step) {
     const int64_t i = base + team;
     const bool have = live && i < a.n;
-    Oct<T> ox, oo, og;
-    row_of(a.x, a.ldx, i, col, have, ox);
-    row_of(a.block, a.ldb, i, col, have, oo);
-    row_of(a.gate, a.ldg, i, col, have, og);
+    if (!kAhead<L>) fetch(i);
+    const Oct<T> ox = nx, oo = no, og = ng;
+    if (kAhead<L>) fetch(i + step);
     float h[8], u[8], r;
     ox.get(h);
     if (a.block) {
@@ -231,15 +247,22 @@ __global__ __launch_bounds__(Team<L>::kBlock) void backward_kernel(const NormArg
   ls.load(a.ls, col, live, 1.f);
   float sum[kSums][8] = {};
   const int64_t step = static_cast<int64_t>(gridDim.x) * kRows;
+  Oct<T> nx, no, ng, nh, ny;
+  auto fetch = [&](int64_t i) {
+    const bool have = live && i < a.n;
+    row_of(a.x, a.ldx, i, col, have, nx);
+    row_of(a.block, a.ldb, i, col, have, no);
+    row_of(a.gate, a.ldg, i, col, have, ng);
+    row_of(a.dh, a.lddh, i, col, have, nh);
+    row_of(a.dy, a.lddy, i, col, have, ny);
+  };
+  if (kAhead<L>) fetch(static_cast<int64_t>(blockIdx.x) * kRows + team);
   for (int64_t base = static_cast<int64_t>(blockIdx.x) * kRows; base < a.n; base += step) {
     const int64_t i = base + team;
     const bool have = live && i < a.n;
-    Oct<T> ox, oo, og, oh, oy;
-    row_of(a.x, a.ldx, i, col, have, ox);
-    row_of(a.block, a.ldb, i, col, have, oo);
-    row_of(a.gate, a.ldg, i, col, have, og);
-    row_of(a.dh, a.lddh, i, col, have, oh);
-    row_of(a.dy, a.lddy, i, col, have, oy);
+    if (!kAhead<L>) fetch(i);
+    const Oct<T> ox = nx, oo = no, og = ng, oh = nh, oy = ny;
+    if (kAhead<L>) fetch(i + step);
     float h[8], t[8], n[8], s[8], slope[8], uo[8], ro = 0.f;
     ox.get(h);
     if (a.block) {
@@ -384,6 +407,9 @@ hipError_t pick(const NormArgs& a, int grid, bool backward, hipStream_t st) {
 
 }  // namespace
 
+// Workgroups of a backward: as many as its registers let run at once, since each
+// leaves a row of partial sums (four a CU: 423 us for two's 405, and 82 for 73 of
+// wide rows, whose sums to join are then as long as a row's).
 int norm_partials(int64_t n, int d, int n_cu) {
   return static_cast<int>(std::min<int64_t>(ceil_div(n, rows_of(d)), 2 * static_cast<int64_t>(n_cu)));
 }

@@ -121,7 +121,7 @@ SPREADS = {
 
 @pytest.mark.parametrize("kind", ["rms", "layer"])
 @pytest.mark.parametrize("name", list(SPREADS))
-@pytest.mark.parametrize("d", [64, 264, 1000])
+@pytest.mark.parametrize("d", [64, 72, 256, 264, 1000])  # (teams of 8, 16, 32, 64 and 128 lanes)
 def test_values(torch, d, name, kind):
     for form in ("pre", "sigmoid"):
         plan, t, given, ref = build(torch, 13, d, "f32", kind, form, spread=SPREADS[name], seed=3)
