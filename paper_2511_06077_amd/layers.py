@@ -34,12 +34,18 @@ _KINDS = {"rms": stca.STCA_NORM_RMS, "layer": stca.STCA_NORM_LAYER}
 _GATES = {None: stca.STCA_GATE_NONE, "sigmoid": stca.STCA_GATE_SIGMOID, "silu": stca.STCA_GATE_SILU}
 
 
+def _there(t, device):
+    """t lies on `device`.  (get_device is -1 on the host; comparing devices costs a microsecond.)"""
+    return t.get_device() == (-1 if device.index is None else device.index)
+
+
 def _matrix(name, t, d, dtype, device, n=None):
     """(tensor, row stride) of rows [n][d]; rows may be strided."""
-    if not hasattr(t, "data_ptr") or t.dtype != dtype or t.device != device:
+    if not hasattr(t, "data_ptr") or t.dtype != dtype or not _there(t, device):
         raise ValueError(f"{name}: a {dtype} tensor on {device} is needed")
-    if t.dim() != 2 or t.shape[1] != d or (n is not None and t.shape[0] != n):
-        raise ValueError(f"{name}: rows [{'n' if n is None else n}][{d}] are needed, not {tuple(t.shape)}")
+    shape = t.shape
+    if len(shape) != 2 or shape[1] != d or (n is not None and shape[0] != n):
+        raise ValueError(f"{name}: rows [{'n' if n is None else n}][{d}] are needed, not {tuple(shape)}")
     if t.is_contiguous():
         return t, 0
     if t.stride(1) != 1 or (t.shape[0] > 1 and t.stride(0) < d):
@@ -48,7 +54,7 @@ def _matrix(name, t, d, dtype, device, n=None):
 
 
 def _vector(name, t, n, dtype, device):
-    if not hasattr(t, "data_ptr") or t.dtype != dtype or t.device != device or t.dim() != 1 or not t.is_contiguous() \
+    if not hasattr(t, "data_ptr") or t.dtype != dtype or not _there(t, device) or t.dim() != 1 or not t.is_contiguous() \
             or (n is not None and t.shape[0] != n):
         raise ValueError(f"{name}: a contiguous {dtype} tensor [{'n' if n is None else n}] on {device} is needed")
     return t
@@ -290,10 +296,10 @@ class BlockNorm(_Streamed):
         with self._on(stream):
             def rows(t):
                 return None if t is None else torch.empty((n, self.d), dtype=self.dtype, device=self.device)
-            def sums(t):
-                return None if t is None else torch.empty(self.d, dtype=torch.float32, device=self.device)
             dx, db, dg = rows(x), rows(block), rows(gate)
-            dp = [sums(t) for t in params]
+            wanted = sum(t is not None for t in params)
+            sums = iter(torch.empty((wanted, self.d), dtype=torch.float32, device=self.device).unbind(0) if wanted else ())
+            dp = [None if t is None else next(sums) for t in params]
             out = stca.norm_grads(dx, db, dg, 0, 0, 0, *dp)
             stca.stca_norm_backward(form, given, n, dh, lddh, dy, lddy, out, self.ws, self.ws_bytes, self._at(stream))
         return BlockNormGrads(dx, db, dg, (dp[0], dp[1]), (dp[2], dp[3]), dp[4])
@@ -330,7 +336,7 @@ class GradientNorm(_Streamed):
         if len(grads) > self.most:
             raise ValueError(f"{len(grads)} gradients, where the object was made for {self.most}")
         codes = {torch.float32: stca.STCA_F32, torch.bfloat16: stca.STCA_BF16}
-        at = -1 if self.device.index is None else self.device.index  # (get_device() of the host's tensors is -1)
+        at = -1 if self.device.index is None else self.device.index
         items = []
         for i, (g, o, c) in enumerate(zip(grads, out, counts)):
             n, code, row = g.numel(), codes.get(g.dtype), 0

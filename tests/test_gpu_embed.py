@@ -98,6 +98,9 @@ GRADS = {
     # more workgroups than the card holds at once, of fewer tokens than threads
     "many_workgroups": (np.random.default_rng(10).zipf(1.2, 300000) % 100000, 100000, 136),
     "many_workgroups_256": (np.random.default_rng(11).integers(-1, 30000, 270000), 30000, 256),
+    # several tiles a sorting workgroup
+    "several_tiles": (np.random.default_rng(12).integers(-1, 70000, 1300001), 70000, 8),
+    "several_tiles_one_id": (np.full(1100000, 2), 3, 16),
     "digits_255": (np.random.default_rng(9).integers(0, 255, 5000), 255, 16),
     "digits_256": (np.random.default_rng(9).integers(0, 256, 5000), 256, 16),
     "digits_65536": (np.random.default_rng(9).integers(0, 65536, 9000), 65536, 16),
