@@ -60,6 +60,12 @@ def _vector(name, t, n, dtype, device):
     return t
 
 
+def _like(x):
+    """Dense rows of x's shape and type."""
+    torch = _torch()
+    return torch.empty_like(x, memory_format=torch.contiguous_format)
+
+
 class _Streamed:
     def stream(self):
         return _torch().cuda.current_stream(self.device.index).cuda_stream
@@ -264,14 +270,11 @@ class BlockNorm(_Streamed):
         """(h, y) of rows [n][d]; h is x where there is no block.  pre, post: (weight,
         bias) or (weight,), fp32 [d]; () for a norm without them.  post=None: the block's
         rows as they are; pre=False: no y (None)."""
-        torch = _torch()
         want_y = pre is not False
         form, given, n, _ = self._given(x, block, gate, pre, post, layer_scale, want_y)
         with self._on(stream):
-            def new():
-                return torch.empty((n, self.d), dtype=self.dtype, device=self.device)
-            h = None if block is None else new()
-            y = new() if want_y else None
+            h = None if block is None else _like(x)
+            y = _like(x) if want_y else None
             stca.stca_norm_forward(form, given, n, h, 0, y, 0, self._at(stream))
         return (x if h is None else h), y
 
@@ -294,9 +297,7 @@ class BlockNorm(_Streamed):
         elif not want_y:
             raise ValueError("dh: needed where there is no y")
         with self._on(stream):
-            def rows(t):
-                return None if t is None else torch.empty((n, self.d), dtype=self.dtype, device=self.device)
-            dx, db, dg = rows(x), rows(block), rows(gate)
+            dx, db, dg = (None if t is None else _like(x) for t in (x, block, gate))
             wanted = sum(t is not None for t in params)
             sums = iter(torch.empty((wanted, self.d), dtype=torch.float32, device=self.device).unbind(0) if wanted else ())
             dp = [None if t is None else next(sums) for t in params]
