@@ -1,6 +1,7 @@
 // The norm of many gradients together, and every one times min(1, max_norm /
 // norm).  Squares are added, and the factor is applied, in fp64, so no finite
-// gradient is too large or too small, and a result is rounded once.  Two launches
+// gradient is too large or too small, and a result is rounded once, to its own type
+// (bf16 below 2^-126: to fp32's smallest numbers before).  Two launches
 // a list: sums of squares, one a workgroup, and the scaling, whose workgroups all
 // add up the same sums in the same order.  Bound by the bytes: every gradient is
 // read twice (the second time from the last-level cache as far as it holds them)
@@ -124,6 +125,21 @@ __device__ __forceinline__ void store(bf16_bits* p, const float* x) {
   __builtin_nontemporal_store(w, reinterpret_cast<words*>(p));
 }
 
+// A product in fp64, as a float that rounds to O as the product does: for bf16 what
+// fp32 has no bits for is gathered in the last one that it has, since rounded to
+// fp32 the product may come to lie in the middle of two bf16 numbers.  (61.7 million
+// bf16 elements into others: 41 us with and without.)
+template <typename O>
+__device__ __forceinline__ float narrow(double x) {
+  if constexpr (sizeof(O) == 2) {
+    uint64_t w = __builtin_bit_cast(uint64_t, x);
+    constexpr uint64_t kLow = (uint64_t(1) << 29) - 1;
+    w = (w & ~kLow) | (w & kLow ? kLow + 1 : 0);
+    x = __builtin_bit_cast(double, w);
+  }
+  return static_cast<float>(x);
+}
+
 template <typename T, typename O>
 __device__ __forceinline__ void scale_piece(const T* g, O* out, int64_t n, double f) {
   constexpr int N = Piece<T>::kN;
@@ -141,12 +157,12 @@ __device__ __forceinline__ void scale_piece(const T* g, O* out, int64_t n, doubl
         float x[N];
         p[k].get(x);
 #pragma unroll
-        for (int e = 0; e < N; ++e) x[e] = static_cast<float>(x[e] * f);
+        for (int e = 0; e < N; ++e) x[e] = narrow<O>(x[e] * f);
         store<N>(out + i0 + k * N * kThreads, x);
       }
     }
   }
-  for (int64_t i = done + threadIdx.x; i < n; i += kThreads) out[i] = from_f32<O>(static_cast<float>(to_f32(g[i]) * f));
+  for (int64_t i = done + threadIdx.x; i < n; i += kThreads) out[i] = from_f32<O>(narrow<O>(to_f32(g[i]) * f));
 }
 
 __global__ __launch_bounds__(kThreads) void scale_kernel(const ClipArgs a) {

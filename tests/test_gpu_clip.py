@@ -149,3 +149,33 @@ def test_nothing_to_clip(torch):
     from paper_2511_06077_amd.layers import GradientNorm
     assert float(GradientNorm(1.0).clip([])) == 0.0
     assert float(GradientNorm(1.0).clip([torch.zeros(0, device="cuda"), torch.zeros((4, 3), device="cuda")])) == 0.0
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("at", [0, 1])
+def test_bf16_results_are_rounded_once(torch, dtype, at):
+    """Products a little beside the middle of two bf16 numbers, nearer to it than fp32 can
+    tell: rounded to fp32 they are the middle, and from there to the even number, which is
+    the wrong one.  Aligned views and others."""
+    from paper_2511_06077_amd.layers import GradientNorm
+    k = np.arange(2, 128, dtype=np.float64)
+    if dtype == "f32":
+        # factors of 1 -+ 2^-40 of an odd multiple of half a step (2^-8), k even and odd
+        g = np.concatenate([1 + (2 * k + 1) * 2.0 ** -8, -(1 + (2 * k + 1) * 2.0 ** -8)])
+        factors = [1 - 2.0 ** -40]
+    else:
+        # 128 * factor is the middle of 65 + 66 halves, or of 64 and 64.5, and a little more or less
+        g = np.concatenate([np.full(100, 128.0), np.full(27, -128.0)])
+        factors = [m / 128 * (1 + s * 2.0 ** -40) for m in (64.25, 64.75, 65.25, 97.25) for s in (1, -1)]
+    store = torch.zeros(len(g) + at, dtype=dtype_of(torch, dtype), device="cuda")
+    t = store[at:]
+    t.copy_(torch.from_numpy(g))
+    assert np.array_equal(host([t])[0], g)
+    norm = float(np.sqrt(np.sum(g.astype(np.longdouble) ** 2)))
+    for f in factors:
+        out = torch.zeros(len(g) + at, dtype=torch.bfloat16, device="cuda")[at:]
+        GradientNorm(norm * f).clip([t], out=[out])
+        # in fp64 exact to 2^-52, twice; the middles are 2^-41 away
+        want = g * f
+        step = 2.0 ** (np.floor(np.log2(np.abs(want))) - 7)
+        assert np.array_equal(host([out])[0], np.rint(want / step) * step), f
