@@ -88,12 +88,16 @@ def norm(x, kind, eps, scale, block=None, gate=None, act=None, pre=(None, None),
         if act:
             p = np.where(gate >= 0, 1 / (1 + np.exp(-np.abs(gate))), np.exp(-np.abs(gate)) / (1 + np.exp(-np.abs(gate))))
             rest = np.where(gate >= 0, np.exp(-np.abs(gate)) / (1 + np.exp(-np.abs(gate))), 1 / (1 + np.exp(-np.abs(gate))))
-            # the exponent is rounded (1.5 U |g|), exp2 and the reciprocal are within 2 U, a few products
-            rel = (2 * np.abs(gate) + 12) * U
+            # the exponential is off by 2 U of exp2, U of its correction and 0.05 U |g| of what that leaves (4 U
+            # at the end of fp32), the small one of s and 1 - s by U of 1 + it, 2 U of the reciprocal and U of a
+            # product more, of which the first is nothing at |g| > 17, and a SiLU by another product's: below 12 U.
+            # An exponential below 2^-126 may be zero.
+            rel = 12 * U
+            none = (1 + np.abs(gate)) * 2.0 ** -126
             s = p * gate if act == "silu" else p
             slope = p + gate * p * rest if act == "silu" else p * rest
-            s_err = rel * np.abs(s) + 1e-37
-            slope_err = 2 * rel * (p + np.abs(gate) * p * rest if act == "silu" else p * rest) + 1e-37
+            s_err = rel * np.abs(s) + none
+            slope_err = 2 * rel * (p + np.abs(gate) * p * rest if act == "silu" else p * rest) + none
         t, t_err = n * s, n_err * np.abs(s) + np.abs(n) * s_err + U * np.abs(n * s)
         k = scale * (np.ones(d) if ls is None else ls)
         h = x + k * t

@@ -145,9 +145,14 @@ __device__ __forceinline__ void unit_grad(Reduce<L>& red, const float* a, const 
   for (int e = 0; e < 8; ++e) g[e] = r * (a[e] - s - u[e] * m);
 }
 
-// s(g) and 1 - s(g), each to its own last bits
+// s(g) and 1 - s(g), the small one of them within 11 halves of a step too: what the
+// exponent loses where -|g| log2(e) is rounded, up to |g| 2^-24 of the result, is put
+// back as the factor 1 + rest; fp32's ln 2 leaves |g| 2^-28.4 of it.  exp2 gives zero
+// below 2^-126, and keeps it where the exponent is not finite (fminf takes the number).
 __device__ __forceinline__ void sigmoid(float g, float& s, float& rest) {
-  const float e = __builtin_amdgcn_exp2f(-fabsf(g) * kLog2e);
+  const float x = -fabsf(g), power = x * kLog2e;
+  float e = __builtin_amdgcn_exp2f(power);
+  e = fmaf(e, fminf(fmaf(power, -kLn2, x), 1.f), e);
   const float p = __builtin_amdgcn_rcpf(1.f + e), q = e * p;
   s = g < 0.f ? q : p;
   rest = g < 0.f ? p : q;

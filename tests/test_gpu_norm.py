@@ -206,3 +206,52 @@ def test_gradients_against_differences(torch):
             # rounding of f over the step, and the third derivative times step^2 / 6
             bound = 80 * O.U * size / (hi - lo) + step * step * 20
             assert abs((up - down) / (hi - lo) - float(gf[i])) <= bound
+
+
+def doubles(t):
+    return None if t is None else t.double().cpu().numpy()
+
+
+def oracle(t, given, kind, act, eps=1e-6, rows=slice(None)):
+    """The oracle's results for rows of a call's tensors."""
+    def pair(p):
+        return p if p is None or p is False else tuple(map(doubles, (*p, None, None)[:2]))
+    def some(v):
+        return None if v is None else doubles(v[rows])
+    return O.norm(some(t["x"]), kind, float(np.float32(eps)), float(np.float32(0.7)), some(given.get("block")),
+                  some(given.get("gate")), act, pre=pair(given["pre"]), post=pair(given.get("post")),
+                  ls=doubles(given.get("layer_scale")), dy=some(t["dy"]), dh=some(t["dh"]))
+
+
+@pytest.mark.parametrize("act", ["sigmoid", "silu"])
+@pytest.mark.parametrize("form", ["full", "gate_only"])
+@pytest.mark.parametrize("d", [72, 1000])
+def test_gates_far_from_zero(torch, d, form, act):
+    """Gates up to where the sigmoid leaves fp32, of either sign: the small one of s and
+    1 - s, and a SiLU's slope, keep fp32's accuracy."""
+    from paper_2511_06077_amd.layers import BlockNorm
+    _, t, given, _ = build(torch, 29, d, "f32", "rms", "sigmoid" if form == "full" else "gate_only", seed=4)
+    plan = BlockNorm(d, kind="rms", gate=act, scale=float(np.float32(0.7)), dtype=torch.float32, backward=True)
+    rng = np.random.default_rng(d)
+    gate = rng.uniform(-95, 95, size=(29, d))
+    gate[:, :8] = [0.0, -0.0, 88.0, -88.0, 87.3, -87.3, 1e-30, -20.0]
+    given["gate"], _ = rounded(torch, gate, "f32")
+    if form == "full":
+        # nothing else in the way of what is small: h is the gated block's alone
+        t["x"].zero_()
+        t["dh"].zero_()
+    check(both(plan, t, given), oracle(t, given, "rms", act), "f32", True)
+
+
+def test_gates_without_end(torch):
+    """sigmoid(inf) = 1 and sigmoid(-inf) = 0, with no slope; silu(inf) stays infinite; a NaN stays one."""
+    from paper_2511_06077_amd.layers import BlockNorm
+    x, o = torch.zeros((4, 64), device="cuda"), torch.ones((4, 64), device="cuda")
+    gate = torch.tensor([float("inf"), -float("inf"), float("nan"), 3e38], device="cuda")[:, None].repeat(1, 64)
+    sig = BlockNorm(64, gate="sigmoid", dtype=torch.float32, backward=True)
+    h, _ = sig.forward(x, block=o, gate=gate, pre=False)
+    assert bool((h[[0, 3]] == 1).all()) and bool((h[1] == 0).all()) and bool(torch.isnan(h[2]).all())
+    g = sig.backward(None, x, dh=o, block=o, gate=gate, pre=False)
+    assert bool((g.gate[[0, 1, 3]] == 0).all()) and bool(torch.isnan(g.gate[2]).all())
+    h, _ = BlockNorm(64, gate="silu", dtype=torch.float32).forward(x, block=o, gate=gate, pre=False)
+    assert bool(torch.isposinf(h[0]).all()) and bool(torch.isnan(h[2]).all()) and bool((h[3] == gate[3]).all())
