@@ -75,6 +75,16 @@ def affine(u, u_err, w, b, d):
     return u * w + b, u_err * np.abs(w) + 2 * U * (np.abs(u * w) + np.abs(b)), w
 
 
+def sum_depth(n, d):
+    """Additions behind one another in a gradient of [d]: a lane's rows (of teams of
+    d / 8 lanes, 256 lanes a workgroup or a team, two workgroups a CU of 256), its
+    workgroup's teams, and two roundings more: the residual scale, the fp64 sum's."""
+    lanes = max(8, 1 << (-(-d // 8) - 1).bit_length())
+    teams = 256 // lanes if lanes <= 64 else 1
+    groups = min(-(-n // teams), 512)
+    return -(-n // max(1, groups * teams)) + teams + 2
+
+
 def norm(x, kind, eps, scale, block=None, gate=None, act=None, pre=(None, None), post=None, ls=None, dy=None, dh=None):
     """dict of values and (name + "_err") bounds on the error before rounding."""
     out, d = {}, x.shape[1]
@@ -108,7 +118,7 @@ def norm(x, kind, eps, scale, block=None, gate=None, act=None, pre=(None, None),
         out["y"], out["y_err"], w = affine(u, u_err, *pre, d)
     if dy is None and dh is None:
         return out
-    depth = (-(-len(x) // 1024) + 40) * U  # of a sum over the rows
+    depth = sum_depth(*x.shape) * U
     def total(name, term, err):
         out[name], out[name + "_err"] = term.sum(0), err.sum(0) + depth * np.abs(term).sum(0)
     g = np.zeros_like(x) if dh is None else dh

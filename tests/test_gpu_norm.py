@@ -255,3 +255,34 @@ def test_gates_without_end(torch):
     assert bool((g.gate[[0, 1, 3]] == 0).all()) and bool(torch.isnan(g.gate[2]).all())
     h, _ = BlockNorm(64, gate="silu", dtype=torch.float32).forward(x, block=o, gate=gate, pre=False)
     assert bool(torch.isposinf(h[0]).all()) and bool(torch.isnan(h[2]).all()) and bool((h[3] == gate[3]).all())
+
+
+# ---- more rows than the workgroups take at once
+
+def launched(torch, d):
+    """(rows a workgroup takes at once, rows of a forward's and of a backward's first turn)"""
+    cus = torch.cuda.get_device_properties(0).multi_processor_count
+    rows = 256 // max(8, 1 << (-(-d // 8) - 1).bit_length()) if d <= 512 else 1
+    return rows, 16 * cus * rows, 2 * cus * rows
+
+
+@pytest.mark.parametrize("n,d", [(1100, 2000), (1100, 4096), (2100, 512), (17000, 64)])
+def test_sums_over_later_turns(torch, n, d):
+    """The gradients of [d] where workgroups of the backward have a second turn and more."""
+    assert n > launched(torch, d)[2]
+    plan, t, given, ref = build(torch, n, d, "bf16", "layer", "silu", seed=6)
+    check(both(plan, t, given), ref, "bf16", True)
+
+
+@pytest.mark.parametrize("n,d", [(200000, 520), (1500000, 64)])
+def test_sums_at_their_bound(torch, n, d):
+    """A long sum whose every term but the first of a workgroup's is half a step of it, and lost."""
+    from paper_2511_06077_amd.layers import BlockNorm
+    first = launched(torch, d)[2]
+    dy = torch.full((n, d), 2.0 ** -24, dtype=torch.bfloat16, device="cuda")
+    dy[:first] = 1.0
+    x = torch.ones((n, d), dtype=torch.bfloat16, device="cuda")
+    plan = BlockNorm(d, backward=True)
+    got = plan.backward(dy, x, pre=(None, torch.zeros(d, device="cuda"))).pre[1]
+    want = np.full(d, first + (n - first) * 2.0 ** -24)
+    assert worst(got, want, O.sum_depth(n, d) * O.U * want, "f32") <= 1.0

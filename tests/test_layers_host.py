@@ -314,3 +314,23 @@ def test_oracle_clip():
     norm, f = O.clip([np.array([3.0]), np.array([[4.0, 0.0]])], 1.0)
     assert norm == 5.0 and f == 0.2
     assert O.clip([np.array([3.0])], 3.0)[1] == 1.0 and O.clip([np.array([np.inf])], 3.0)[1] == 1.0
+
+
+@pytest.mark.parametrize("n,d", [(1, 8), (700, 64), (20000, 32), (2500, 1024), (41001, 520), (200000, 4096), (1500000, 72)])
+def test_oracle_bounds_the_sums_over_rows(n, d):
+    """A norm's sums of [d] as they are divided: a lane's rows one after the other, a
+    workgroup's lanes, then fp64; with terms that are lost beside the first one of a lane."""
+    cus, lanes = 256, max(8, 1 << (d // 8 - 1).bit_length())
+    teams = 256 // lanes if lanes <= 64 else 1
+    groups = min(-(-n // teams), 2 * cus)
+    turn = groups * teams
+    terms = np.full(-(-n // turn) * turn, 2.0 ** -24, dtype=np.float32)
+    terms[:turn], terms[n:] = 1.0, 0.0
+    lane = np.zeros(turn, dtype=np.float32)
+    for k in range(0, len(terms), turn):
+        lane += terms[k:k + turn]
+    group = np.zeros(groups, dtype=np.float32)
+    for k in range(teams):
+        group += lane.reshape(groups, teams)[:, k]
+    got, want = float(np.float32(group.sum(dtype=np.float64))), float(terms.sum(dtype=np.float64))
+    assert abs(got - want) <= (O.sum_depth(n, d) + 1) * O.U * want
