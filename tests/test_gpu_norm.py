@@ -266,6 +266,77 @@ def launched(torch, d):
     return rows, 16 * cus * rows, 2 * cus * rows
 
 
+WIDE = [(64, "bf16"), (72, "f32"), (256, "bf16"), (512, "bf16"), (520, "f32"), (1000, "bf16"), (2000, "bf16"), (2000, "f32"),
+        (4096, "bf16"), (4096, "f32")]  # (teams of 8, 16, 32, 64, 128, 256 and 512 lanes)
+
+
+def large(torch, n, d, dtype, seed=0):
+    """Tensors of n rows, drawn on the GPU, for the form with everything in it."""
+    gen = torch.Generator(device="cuda").manual_seed(1000 * seed + d)
+    kind = torch.bfloat16 if dtype == "bf16" else torch.float32
+    def normal(shape, middle=0.0, gain=1.0):
+        return middle + gain * torch.randn(shape, generator=gen, device="cuda")
+    t = {k: normal((n, d)).to(kind) for k in ("x", "dy", "dh")}
+    given = {k: normal((n, d)).to(kind) for k in ("block", "gate")}
+    given.update(pre=(normal(d, 1.0, 0.3), normal(d, 0.0, 0.3)), post=(normal(d, 1.0, 0.3), normal(d, 0.0, 0.3)),
+                 layer_scale=normal(d, 0.5, 0.2))
+    return t, given
+
+
+@pytest.mark.parametrize("kind", ["rms", "layer"])
+@pytest.mark.parametrize("d,dtype", WIDE)
+def test_rows_of_later_turns(torch, d, dtype, kind):
+    """A workgroup's second turn of rows, forward and backward, gives bit for bit what a call
+    of those rows alone gives, and some of them are compared with the oracle."""
+    from paper_2511_06077_amd.layers import BlockNorm
+    rows, first, _ = launched(torch, d)
+    n = first + 37 * rows + min(rows - 1, 3)
+    t, given = large(torch, n, d, dtype)
+    plan = BlockNorm(d, kind=kind, gate="silu", scale=float(np.float32(0.7)), dtype=t["x"].dtype, backward=True)
+    h, y, g = both(plan, t, given)
+    whole = (h, y, g.x, g.block, g.gate)
+    def part(at):
+        cut = {**given, **{k: given[k][at] for k in ("block", "gate")}}
+        ph, py, pg = both(plan, {k: v[at] for k, v in t.items()}, cut)
+        return ph, py, pg.x, pg.block, pg.gate
+    for at in (slice(0, first // 2), slice(first // 2, first), slice(first, n)):  # (each a forward's one turn)
+        for a, b in zip(whole, part(at)):
+            assert torch.equal(a[at], b)
+    # single turns of the backward too: where its second one begins, and the last rows
+    for a0 in (launched(torch, d)[2] - 5, n - 11):
+        at = slice(a0, a0 + 11)
+        for a, b in zip(whole, part(at)):
+            assert torch.equal(a[at], b)
+        ref = oracle(t, given, kind, "silu", rows=at)
+        for name, v in zip(("h", "y", "dx", "dblock", "dgate"), whole):
+            assert worst(v[at], ref[name], ref[name + "_err"], dtype) <= 1.0, name
+
+
+@pytest.mark.parametrize("d,dtype", [(64, "f32"), (256, "bf16"), (512, "f32"), (1000, "f32"), (1000, "bf16"), (2000, "bf16"),
+                                     (4096, "f32")])
+def test_results_on_their_inputs_in_later_turns(torch, d, dtype):
+    """h on x, y on block, and y on gate; dx on dh, dblock on dy, dgate on gate: with the
+    next row of a team on its way while this one is written."""
+    from paper_2511_06077_amd import stca
+    from paper_2511_06077_amd.layers import BlockNorm
+    rows, first, _ = launched(torch, d)
+    n = first + 5 * rows + 1
+    t, given = large(torch, n, d, dtype, seed=1)
+    plan = BlockNorm(d, kind="layer", gate="sigmoid", dtype=t["x"].dtype, backward=True)
+    h, y, g = both(plan, t, given)
+    m, s = plan._forms[True, True], plan.stream()
+    for y_on in ("block", "gate"):
+        f = {k: v.clone() for k, v in {**t, **{k: given[k] for k in ("block", "gate")}}.items()}
+        inp = stca.norm_in(f["x"], f["block"], f["gate"], 0, 0, 0, *given["pre"], *given["post"], given["layer_scale"])
+        stca.stca_norm_forward(m, inp, n, f["x"], 0, f[y_on], 0, s)
+        assert torch.equal(f["x"], h) and torch.equal(f[y_on], y)
+    f = {k: v.clone() for k, v in {**t, **{k: given[k] for k in ("block", "gate")}}.items()}
+    inp = stca.norm_in(f["x"], f["block"], f["gate"], 0, 0, 0, *given["pre"], *given["post"], given["layer_scale"])
+    stca.stca_norm_backward(m, inp, n, f["dh"], 0, f["dy"], 0, stca.norm_grads(f["dh"], f["dy"], f["gate"]), plan.ws,
+                            plan.ws_bytes, s)
+    assert torch.equal(f["dh"], g.x) and torch.equal(f["dy"], g.block) and torch.equal(f["gate"], g.gate)
+
+
 @pytest.mark.parametrize("n,d", [(1100, 2000), (1100, 4096), (2100, 512), (17000, 64)])
 def test_sums_over_later_turns(torch, n, d):
     """The gradients of [d] where workgroups of the backward have a second turn and more."""
