@@ -220,3 +220,48 @@ def test_odd_values_stay_in_their_gradients(torch):
         k = torch.from_numpy(np.bincount(ids[ids >= 0], minlength=5)).float().cuda()
         for r in (0, 1, 4):
             assert bool((values[r] == k[r]).all())
+
+
+@pytest.mark.parametrize("dtype,out", [("bf16", "bf16"), ("f32", "bf16"), ("bf16", "f32")])
+@pytest.mark.parametrize("fields", [4, 5, 6, 7])
+@pytest.mark.parametrize("n,d", [(1, 64), (333, 264)])
+def test_fields_of_several_groups(torch, n, d, fields, dtype, out):
+    """Four fields are looked up together; of more, what is left after them."""
+    from paper_2511_06077_amd.layers import EmbeddingSum
+    rng = np.random.default_rng([n, d, fields])
+    rows = tuple(int(r) for r in rng.integers(1, 40, size=fields))
+    t, f = zip(*(rounded(torch, rng.standard_normal((r, d)), dtype) for r in rows))
+    ids = [rng.integers(-1, r, size=n) for r in rows]
+    e = EmbeddingSum(rows, d, scale=0.5, dtype=t[0].dtype, out_dtype=torch.bfloat16 if out == "bf16" else torch.float32)
+    ref, mag = O.embed(f, ids, 0.5)
+    assert worst(e.forward(t, [ids_of(torch, i) for i in ids]), ref, (fields + 1) * O.U * mag, out) <= 1.0
+    assert e.device_status() == 0
+    ids[-1][n - 1] = rows[-1]  # (an id behind the last table)
+    ref, mag = O.embed(f, ids, 0.5)
+    assert worst(e.forward(t, [ids_of(torch, i) for i in ids]), ref, (fields + 1) * O.U * mag, out) <= 1.0
+    assert e.device_status() != 0
+
+
+@pytest.mark.parametrize("d,dtype", [(256, "f32"), (520, "bf16"), (8, "bf16"), (64, "f32")])
+def test_rows_of_later_turns(torch, d, dtype):
+    """More rows than 32 workgroups a CU take at once, of four rows a team: exact, with one
+    field; with five, what a call of those rows alone gives."""
+    from paper_2511_06077_amd.layers import EmbeddingSum
+    pieces = d // (4 if dtype == "f32" else 8)
+    lanes = min(64, max(8, 1 << (pieces - 1).bit_length()))
+    first = 32 * torch.cuda.get_device_properties(0).multi_processor_count * (256 // lanes) * 4
+    n = first + 9001
+    gen = torch.Generator(device="cuda").manual_seed(d)
+    rows = (1000, 3, 77, 1, 500)
+    kind = torch.bfloat16 if dtype == "bf16" else torch.float32
+    tables = [torch.randn((r, d), generator=gen, device="cuda").to(kind) for r in rows]
+    ids = [torch.randint(-1, r, (n,), generator=gen, device="cuda").int() for r in rows]
+    got = EmbeddingSum(rows[0], d, dtype=kind, out_dtype=kind).forward(tables[0], ids[0])
+    want = torch.where((ids[0] >= 0)[:, None], tables[0][ids[0].clamp(min=0).long()], 0)
+    assert torch.equal(got, want)
+    del want
+    e = EmbeddingSum(rows, d, scale=0.3, dtype=kind, out_dtype=kind)
+    got = e.forward(tables, ids)
+    for at in (slice(0, first // 2), slice(first // 2, first), slice(first, n)):
+        assert torch.equal(got[at], e.forward(tables, [i[at] for i in ids]))
+    assert e.device_status() == 0
