@@ -41,7 +41,9 @@ def unit(v, kind, eps, err):
     layer norm's differences carry 2 U of their own and 18 U of the row's
     deviation: in all at most 40 U (|u| + 1).  What v is off by moves u by r err, the
     mean and the scale."""
-    c = v - v.mean(-1, keepdims=True) if kind == "layer" else v
+    c = v
+    for _ in range(4 if kind == "layer" else 0):  # (a mean that is rounded is not all of it)
+        c = c - c.mean(-1, keepdims=True)
     with np.errstate(over="ignore", invalid="ignore"):
         r = 1.0 / np.sqrt((c * c).mean(-1, keepdims=True) + eps)
     u = c * r

@@ -73,35 +73,42 @@ struct Reduce {
   }
 };
 
-// The unit row u of v (zero in lanes behind the row) and r.  Values whose squares
-// leave fp32 are taken 2^-80 as large: eps is nothing beside them.
-template <int L>
+// The unit row u of v (zero in lanes behind the row) and r, from values `by` as large.
+// False: it has to be taken again with more turns, and `by` may be smaller then.
+template <int L, int kTurns>
 __device__ __forceinline__ bool unit_of(Reduce<L>& red, const float* v, bool live, int layer, float inv_d, float eps,
-                                        float by, float* u, float& r) {
+                                        float& by, float* u, float& r) {
   float x[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) x[e] = live ? v[e] * by : 0.f;
   float var;
+  bool rough = false;
   if (layer) {
     float s = 0.f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) s += x[e];
-    const float mean = red.one(s) * inv_d;
+    float mean = red.one(s) * inv_d;
     // the differences' own mean corrects for the rounding of the first one, which
-    // a row far from zero would see
-    float off = 0.f, sq = 0.f;
+    // a row far from zero would see; where that is more than the deviation, as in a
+    // row of one value, the variance would be what is left of the rounding: again,
+    // each turn with 2^-18 of the mean before or less
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      x[e] = live ? x[e] - mean : 0.f;
-      off += x[e];
-      sq = fmaf(x[e], x[e], sq);
+    for (int turn = 0; turn < kTurns; ++turn) {
+      float off = 0.f, sq = 0.f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        x[e] = live ? x[e] - mean : 0.f;
+        off += x[e];
+        sq = fmaf(x[e], x[e], sq);
+      }
+      red.two(off, sq);
+      mean = off * inv_d;
+      var = fmaxf(fmaf(sq, inv_d, -mean * mean), 0.f);
+      if (!(sq <= 1e37f)) var = sq;
     }
-    red.two(off, sq);
-    off *= inv_d;
-    var = fmaxf(fmaf(sq, inv_d, -off * off), 0.f);
-    if (!(sq <= 1e37f)) var = sq;
+    rough = mean * mean > var;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = live ? x[e] - off : 0.f;
+    for (int e = 0; e < 8; ++e) x[e] = live ? x[e] - mean : 0.f;
   } else {
     float sq = 0.f;
 #pragma unroll
@@ -109,18 +116,30 @@ __device__ __forceinline__ bool unit_of(Reduce<L>& red, const float* v, bool liv
     sq = red.one(sq);
     var = !(sq <= 1e37f) ? sq : sq * inv_d;
   }
+  if (kTurns > 1 && by != 1.f && var == 0.f) {  // all values the same
+#pragma unroll
+    for (int e = 0; e < 8; ++e) u[e] = 0.f;
+    r = __frsqrt_rn(eps);
+    return true;
+  }
   r = __frsqrt_rn(var + fmaxf(eps * by * by, 1e-37f));
 #pragma unroll
   for (int e = 0; e < 8; ++e) u[e] = x[e] * r;
   r *= by;
-  return var <= 1e37f;
+  if (!(var <= 1e37f)) by = 0x1p-80f;
+  return var <= 1e37f && !rough;
 }
 
+// Values whose squares leave fp32 are taken 2^-80 as large: eps is nothing beside
+// their variance, if they have one.  The second take, for either reason, is out of the
+// way of the others without a loop of its own (layer norms backward, 131071 rows of
+// 264 in fp32 260 us, in a loop 267; 524288 of 256 in bf16 431 and 440).
 template <int L>
 __device__ __forceinline__ void unit_row(Reduce<L>& red, const float* v, bool live, int layer, float inv_d, float eps,
                                          float* u, float& r) {
-  if (unit_of<L>(red, v, live, layer, inv_d, eps, 1.f, u, r)) return;  // (the same in the whole team)
-  unit_of<L>(red, v, live, layer, inv_d, eps, 0x1p-80f, u, r);
+  float by = 1.f;
+  if (unit_of<L, 1>(red, v, live, layer, inv_d, eps, by, u, r)) return;  // (the same in the whole team)
+  unit_of<L, 6>(red, v, live, layer, inv_d, eps, by, u, r);
 }
 
 // Gradient of a unit row, from a = the gradient of u.

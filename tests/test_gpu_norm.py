@@ -357,3 +357,20 @@ def test_sums_at_their_bound(torch, n, d):
     got = plan.backward(dy, x, pre=(None, torch.zeros(d, device="cuda"))).pre[1]
     want = np.full(d, first + (n - first) * 2.0 ** -24)
     assert worst(got, want, O.sum_depth(n, d) * O.U * want, "f32") <= 1.0
+
+
+@pytest.mark.parametrize("d", [72, 264, 1000, 2000])
+def test_rows_of_one_value(torch, d):
+    """A layer norm of rows whose values are all the same, and of such rows with one that is a
+    step of fp32 off: far from zero, where the mean's rounding is more than the deviation."""
+    values = np.float32([1.0, -300.0, 1e4, 1e5, 1e6 + 0.25, -3e7, 1e8, 7e12, 1e18, -3e19, 1e30, 3e38])
+    def spread(rng, v):
+        v[:] = np.repeat(values, 2)[:, None]
+        v[1::2, 1] = np.nextafter(values, np.float32(0)).astype(np.float64)
+        return v
+    for form in ("pre", "sigmoid"):
+        plan, t, given, ref = build(torch, 2 * len(values), d, "f32", "layer", form, spread=spread, seed=8)
+        if form == "sigmoid":  # (the block's rows are such, and the next norm's are others)
+            t["x"].copy_(t["dh"])
+            ref = oracle(t, given, "layer", "sigmoid")
+        check(both(plan, t, given), ref, "f32", "block" in given)
