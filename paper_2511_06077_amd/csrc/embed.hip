@@ -1,10 +1,10 @@
 // Rows from ids: out_i = scale sum_f T_f[id_f(i)], fp32 sums in the order of the
-// fields, rounded once.  Bound by the rows' bytes (524288 rows of 256 from three
-// fp32 tables, 1.6 GB through the caches, 0.37 read and 0.27 written beyond them:
-// 147 us).  A team of lanes takes a row, 16
-// bytes of a table's row a lane, and several rows at once: first the ids of all of
-// them and of up to four fields, then their rows, so that one look-up's latency is
-// paid for many rows.
+// fields, rounded once.  Rows of the tables come through L2, which each XCD has for
+// itself (a window of 524288 rows of 256 from three fp32 tables, 153 us: 1.6 GB
+// through it, 0.38 read past it, some of that from the last-level cache, and 0.27
+// written).  A team of lanes takes a row, 16 bytes of a table's row a lane, and
+// several rows at once: first the ids of all of them and of up to four fields, then
+// their rows, so that one look-up's latency is paid for many rows.
 #include "layer_ops.h"
 
 namespace stca {
@@ -13,7 +13,7 @@ namespace layers {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kRows = 4;  // rows of a team at a time (window of 524288 rows, three fp32 tables: 2 169 us, 4 165, 8 183)
+constexpr int kRows = 4;  // rows of a team at a time (the window: 2 160 us, 4 153, 8 171)
 
 // 16 bytes of a table's row: kN features.
 template <typename T> struct Piece;
@@ -40,8 +40,8 @@ template <> struct Piece<bf16_bits> {
   }
 };
 
-// The rows are written past the caches, which keep the tables' rows: 152 us for the
-// window, 165 otherwise.
+// The rows are written past the caches, which keep the tables' rows: 153 us for the
+// window, 167 otherwise.
 template <int N>
 __device__ __forceinline__ void store(float* p, const float* x) {
 #pragma unroll

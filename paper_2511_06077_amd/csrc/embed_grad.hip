@@ -15,9 +15,10 @@
 // (528384 tokens of 256 fp32 features, 150 us for
 // 691 MB, 4.6 TB/s; 524288 bf16 ones of 16 ids 52 us, 5.2 TB/s); the sort before it
 // is latency, 18 us for every 8 bits of the ids, and the levels above 6 to 9 each.
-// What the first level measured (us, 528384 tokens): 512 threads a workgroup and 8
-// rows on their way 161, 256 and 4 157 (bf16, 16 ids: 66 and 52, registers for 8
-// waves a SIMD); the next batch fetched before one is added 178.
+// What the first level measured before its results were written past the caches (us,
+// 528384 tokens; 157 then): 512 threads a workgroup and 8 rows on their way 161 for
+// 256 and 4 (bf16, 16 ids: 66 for 52, registers for 8 waves a SIMD); the next batch
+// fetched before one is added 178.
 #include "layer_ops.h"
 
 namespace stca {

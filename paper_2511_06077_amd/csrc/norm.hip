@@ -3,8 +3,8 @@
 // and the gradients of all of it.  A team of lanes takes a row, eight features a
 // lane, and holds it in registers from the loads to the stores, so every row is
 // read and written once: bound by those bytes (524288 rows of 256 in bf16: the norm
-// alone 95 us, 5.6 TB/s; with block and gate 267 forward and 387 backward, 5.0 and
-// 5.6 TB/s).  The backward recomputes what it needs from x, o and g, which it has to
+// alone 95 us, 5.6 TB/s; with block and gate 268 forward and 390 backward, 5.0 and
+// 5.5 TB/s).  The backward recomputes what it needs from x, o and g, which it has to
 // read anyway; nothing is saved.
 //
 // With u = (v - mean) r the unit row of a layer norm (mean = 0: of an rms norm),
@@ -432,8 +432,8 @@ hipError_t pick(const NormArgs& a, int grid, bool backward, hipStream_t st) {
 }  // namespace
 
 // Workgroups of a backward: as many as its registers let run at once, since each
-// leaves a row of partial sums (four a CU: 423 us for two's 405, and 82 for 73 of
-// wide rows, whose sums to join are then as long as a row's).
+// leaves a row of partial sums (four a CU, with the sums' joining: 407 us for two's
+// 402, and 76 for 69 of 8191 rows of 2000).
 int norm_partials(int64_t n, int d, int n_cu) {
   return static_cast<int>(std::min<int64_t>(ceil_div(n, rows_of(d)), 2 * static_cast<int64_t>(n_cu)));
 }

@@ -20,7 +20,9 @@ computation happens in libstca.so.
 An object's workspace belongs to one stream at a time: calls, or replays of
 captured graphs, that may overlap need an object each.  stream= (a handle) is the
 stream of a call in place of the current one, as if it were made under
-torch.cuda.stream: the inputs have to be ready on it, and results belong to it.
+torch.cuda.stream: the inputs have to be ready on it, and so has the object, whose
+workspace is made (and cleared, where it holds a status) on the stream that is
+current then; results belong to it.
 """
 from __future__ import annotations
 
